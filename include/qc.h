@@ -360,6 +360,131 @@ int32_t qc_attend_static(int32_t device, void* cuda_stream, const void* q_dev, c
                          const void* v_dev, void* out_dev, int32_t n_seqs, int32_t n_tokens,
                          int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float softmax_scale);
 
+/* ---- A cache in 4 bits ------------------------------------------------------------------------
+ *
+ * The paper has no counterpart to these calls; they make the same use of a cache possible in 27 % of the
+ * memory.  Each is complete in itself: device memory is the caller's, nothing is kept between calls, every
+ * number that changes from step to step (lengths, page ids, slots) is read on the device, so a step may be
+ * captured into a graph once and replayed while its sequences grow.  All calls are asynchronous on
+ * `cuda_stream`; the calling thread's current device is the same afterwards.
+ *
+ * A token axis is a stream, as everywhere here: a stack with lazy layers has a text and a visual one.  One page
+ * table serves all layers of a stream.  A layer has a pool for K and one for V per stream, both of n_pages pages
+ * addressed by the table's page ids; a lazy layer has no pool for visual K (in GLA for no K): it names its
+ * leader's.
+ *
+ * Device data that does not fit (an id out of range, too few pages) is met on the device: nothing outside the
+ * given memory is touched, and a QC_ERR_* code is left in a status word that the caller may read when it likes
+ * (the largest code stays; it is never cleared by the calls). */
+#define QC_TABLE_MAX_BATCH 4096   /* sequences listed in one call */
+#define QC_TABLE_MAX_SEQS 65536   /* rows of a page table */
+#define QC_QUANT_MAX_HEADS 1024
+#define QC_QUANT_MAX_QUERIES 16   /* query tokens of one sequence in one qc_quant_attend */
+
+/* Page table of one stream, all arrays int32 on the device. */
+typedef struct qc_table {
+  int32_t max_seqs;     /* rows */
+  int32_t max_pages;    /* pages a row has room for */
+  int32_t page_size;    /* tokens of a page: 16, 32 or 64 */
+  int32_t n_pages;      /* pages there are; n_pages * page_size < 2^31 */
+  int32_t* pages_dev;   /* [max_seqs][max_pages], -1 where a sequence has no page */
+  int32_t* lens_dev;    /* [max_seqs] tokens */
+  int32_t* free_dev;    /* [n_pages] the free pages, as a stack: the next one taken is free[state[0] - 1] */
+  int32_t* state_dev;   /* [4]: number of free pages, status word, two reserved */
+} qc_table;
+
+/* Empty table: no tokens, all pages free (0 is taken first), status QC_OK. */
+int32_t qc_table_reset(int32_t device, void* cuda_stream, const qc_table* table);
+
+/* n_new_dev[i] (null: 1) more tokens for row seq_ids_dev[i] (null: i) of the table, i < n_seqs.  Pages are
+ * taken in the order of the list, then of the tokens.
+ *   starts_dev [n_seqs + 1]  the new tokens are numbered through the list: sequence i's are starts[i] .. starts[i + 1] - 1
+ *   slots_dev  [max_slots]   where token t goes: page id * page_size + place in the page; -1 behind the last token
+ * All or nothing: on an id out of range or a negative count (QC_ERR_INVALID_ARG), an id listed twice or lengths
+ * and free pages that cannot be (QC_ERR_STATE), too few free pages or a row without room (QC_ERR_OOM_PAGES), or
+ * more than max_slots tokens (QC_ERR_INVALID_ARG), the status word is set, the table stays as it was, starts are 0
+ * and slots -1. */
+int32_t qc_table_extend(int32_t device, void* cuda_stream, const qc_table* table, int32_t n_seqs, const int32_t* seq_ids_dev,
+                        const int32_t* n_new_dev, int32_t max_slots, int32_t* starts_dev, int32_t* slots_dev);
+
+/* Row seq_ids_dev[i] keeps its first n_keep_dev[i] tokens (null: 0, the sequence is released; more than it has: all).
+ * Pages that become empty are free again, in an order that the same qc_table_extend takes them back in.  All or
+ * nothing as above. */
+int32_t qc_table_trim(int32_t device, void* cuda_stream, const qc_table* table, int32_t n_seqs, const int32_t* seq_ids_dev,
+                      const int32_t* n_keep_dev);
+
+/* Shape of a pool: one tensor (K or V) of one layer and stream. */
+typedef struct qc_quant_shape {
+  int32_t n_kv_heads;   /* 1..QC_QUANT_MAX_HEADS */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t page_size;    /* 16, 32 or 64 */
+  int32_t n_pages;      /* n_pages * page_size < 2^31 */
+} qc_quant_shape;
+
+/* n_pages * n_kv_heads * page_size * (head_dim / 2 + 4).  A row (token, head) is held as lo = its smallest element,
+ * r = bf16(15 / (largest - lo)) and codes rint((x - lo) * r) in 4 bits, and stands for lo + code / r.  A row whose
+ * range is below 2^-100 stands for lo throughout (r = 0); one with an element that is infinite or no number, or with
+ * a range that is not finite, stands for NaN throughout.
+ * A page is the codes [n_kv_heads][page_size / 16][8 * head_dim bytes], then [n_kv_heads][page_size] words of lo as
+ * bf16 (low half) and r as bf16.  Inside a block of 16 tokens, in bytes of two elements, the even one low:
+ *   K, 128 wide  [token % 2][token / 2][d / 32][d / 2 % 16]      V, 128 wide  [d / 8 % 2][d / 16][token / 4][d / 2 % 4][token % 4]
+ *   K,  64 wide  [token / 2][d / 16][token % 2][d / 2 % 8]       V,  64 wide  [d / 8][token / 4][d / 2 % 4][token % 4] */
+int32_t qc_quant_pool_bytes(const qc_quant_shape* shape, size_t* bytes);
+
+/* Quantise rows and store them: row t of k_dev / v_dev (bf16 [n_tokens][n_kv_heads][head_dim], tokens k_stride /
+ * v_stride elements apart, heads dense) at slots_dev[t].  A slot that is negative or not in the pool is left out.
+ * Either pair (k_dev, k_pool_dev), (v_dev, v_pool_dev) may be null.  Pointers 16-byte aligned, strides multiples of 8.
+ * Slots are distinct; of rows with the same slot, what that row holds afterwards is not specified. */
+int32_t qc_quant_append(int32_t device, void* cuda_stream, const qc_quant_shape* shape, int32_t n_tokens,
+                        const int32_t* slots_dev, const void* k_dev, int64_t k_stride, const void* v_dev, int64_t v_stride,
+                        void* k_pool_dev, void* v_pool_dev);
+
+/* What the rows at slots_dev stand for, as bf16 [n_tokens][n_kv_heads][head_dim] (dense): what the attention of a
+ * later prompt chunk is computed on.  Rows of slots that are negative or not in the pool are left as they are. */
+int32_t qc_quant_read(int32_t device, void* cuda_stream, const qc_quant_shape* shape, int32_t n_tokens,
+                      const int32_t* slots_dev, const void* k_pool_dev, const void* v_pool_dev, void* k_out_dev,
+                      void* v_out_dev);
+
+/* One stream as qc_quant_attend reads it. */
+typedef struct qc_quant_stream {
+  const void* q_dev;           /* bf16 [n_tokens][n_q_heads][head_dim], tokens q_stride elements apart (0: one row for all) */
+  int64_t q_stride;
+  const void* k_pool_dev;
+  const void* v_pool_dev;
+  const int32_t* pages_dev;    /* of the stream's table */
+  const int32_t* lens_dev;
+  int32_t max_pages, n_pages;
+} qc_quant_stream;
+
+typedef struct qc_quant_attend_args {
+  int32_t n_q_heads, n_kv_heads, head_dim, page_size;
+  int32_t n_seqs, max_seqs;      /* sequences of the call; rows of the tables */
+  int32_t n_tokens;              /* query tokens: rows of q and out */
+  int32_t max_queries;           /* most query tokens of one sequence, 1..QC_QUANT_MAX_QUERIES */
+  int32_t causal;                /* 1: the queries' own tokens are the last of the text stream, and a query sees none behind its own */
+  float softmax_scale;           /* 0 => 1/sqrt(head_dim) */
+  const int32_t* seq_ids_dev;    /* [n_seqs] table row of each sequence; null: i */
+  const int32_t* starts_dev;     /* [n_seqs + 1] query tokens of each sequence, as qc_table_extend numbers them; null: one each */
+  const qc_quant_stream* text;
+  const qc_quant_stream* visual; /* null: one stream */
+  void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim] */
+  float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
+  void* workspace_dev;           /* qc_quant_workspace_bytes; need not be cleared; one call at a time */
+  size_t workspace_bytes;
+  int32_t* status_dev;           /* optional status word */
+} qc_quant_attend_args;
+
+int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes);
+
+/* Attention of each sequence's query tokens over its cached rows: one softmax over the visual stream's keys scored by
+ * visual->q_dev and the text stream's keys scored by text->q_dev (an ordinary layer, VLA_EQ8: the same queries twice;
+ * VLA_QC: the Q Cache on the leader's visual K; GLA: the Q Cache on both of the leader's).  V is what the pools hold.
+ * A query that sees no key gets 0 and lse minus infinity.  Rows of out that belong to no listed sequence are left as
+ * they are, and so are those of a sequence whose row or query numbers are out of range (QC_ERR_INVALID_ARG in the status
+ * word).  A page id that is not in the pool is not followed: its keys count as absent (QC_ERR_BAD_PAGE).  A length
+ * beyond the table's room is cut to it (QC_ERR_PLAN). */
+int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend_args* args);
+
 const char* qc_status_string(int32_t status);
 
 #ifdef __cplusplus

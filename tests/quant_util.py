@@ -1,0 +1,96 @@
+"""Seeded caches in 4 bits for the tests, with the oracle's view of what they hold and how far an output may be off."""
+
+import math
+
+import numpy as np
+import torch
+
+from oracle import quant_cache as O
+from paper_2602_01901_b200 import quant
+
+DEV = "cuda"
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def rows(n, heads, head_dim, g, spread=1.0):
+    """bf16 rows on the CPU: channels and tokens of different size."""
+    channel = torch.exp(0.5 * spread * torch.randn(heads, head_dim, generator=g))
+    token = torch.exp(0.4 * spread * torch.randn(n, 1, 1, generator=g))
+    return (torch.randn(n, heads, head_dim, generator=g) * channel * token).bfloat16()
+
+
+def held(x):
+    """What the cache holds of bf16 rows [n, heads, head_dim]: fp64 lo, step, codes, values, by the oracle's rule row by row."""
+    a = x.double().numpy().reshape(-1, x.shape[-1])
+    lo, step, codes = np.empty(len(a)), np.empty(len(a)), np.empty(a.shape)
+    for i, row in enumerate(a):
+        lo[i], r, codes[i] = O.quantise(row)
+        step[i] = 1.0 / r if r else 0.0
+    lead = x.shape[:-1]
+    lo, step, codes = lo.reshape(lead), step.reshape(lead), codes.reshape(x.shape)
+    return {"lo": lo, "step": step, "codes": codes, "values": lo[..., None] + step[..., None] * codes}
+
+
+def fill(table, ids, lens, page, pools, k, v, device=DEV):
+    """Stores rows k, v (lists of bf16 [len, heads, head_dim], one per sequence) in one call."""
+    n_new = torch.tensor(lens, dtype=torch.int32, device=device)
+    starts, slots = quant.table_extend(table, n_new, seq_ids=ids, max_slots=sum(lens))
+    if sum(lens):
+        quant.append(pools[0], pools[1], slots, torch.cat(k).to(device), torch.cat(v).to(device), page)
+    return starts, slots
+
+
+def bound(queries, keys, values, scale, out, weights):
+    """How far an output row may be from the one in 64 bits, element by element, and its lse; `weights`: the softmax's.
+
+    A score is s * sum q (c - 8) + mid * sum q.  Its products are exact and summed in fp32: every one of the D + 8 steps
+    is off by 2^-23 of the sum's largest magnitude at most (an adder that cuts off), as are the four roundings around it;
+    |score| is bounded with absolute values.  The exponential adds 2^-22 of itself and the rounding of its argument.  The
+    weights p s are rounded to fp16 (2^-11) before the product with c - 8; the sums over L keys, in fp32, are off by
+    2^-23 per step of what they add up; the output is rounded to bf16 (2^-8).
+    """
+    n = sum(len(k["step"]) for k in keys)
+    e = 0.0
+    for q, k in zip(queries, keys):
+        if len(k["step"]):
+            part = np.abs(k["codes"] - 8) @ np.abs(q) * k["step"] + np.abs(k["lo"] + 8 * k["step"]) * np.abs(q).sum()
+            e = max(e, float(part.max()) * scale * (q.size + 12) * 2.0 ** -23)
+    size = np.concatenate([np.abs(v["lo"] + 8 * v["step"])[:, None] + v["step"][:, None] * np.abs(v["codes"] - 8) for v in values]) if n else np.zeros((1, out.size))
+    mass = weights @ size if n else np.zeros(out.size)
+    rel = 2 * e + 2.0 ** -21 + (n + 64) * 2.0 ** -23
+    return 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + 2 * rel) * mass + 1e-37, e + 2.0 ** -20 + (n + 64) * 2.0 ** -23
+
+
+def check_attend(out, lse, starts, ids, lens, q, k_held, v_held, group, scale, causal=True, visual=None):
+    """Every output row against the oracle.  q bf16 [tokens, heads, d] on the CPU; k_held, v_held: per sequence what
+    ``held`` gives; visual: (q, k_held, v_held)."""
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    qs = q.double().numpy()
+    heads = qs.shape[1]
+    cut = lambda h, n, kvh: {name: a[:n, kvh] for name, a in h.items()}
+    for i in range(len(lens)):
+        a, b = starts[i], starts[i + 1]
+        for t in range(a, b):
+            seen = max(0, lens[i] - (b - 1 - t)) if causal else lens[i]
+            for h in range(heads):
+                kvh = h // group
+                keys, values, queries = [cut(k_held[i], seen, kvh)], [cut(v_held[i], seen, kvh)], [qs[t, h]]
+                if visual is not None:
+                    n = len(visual[1][i]["lo"])
+                    keys.append(cut(visual[1][i], n, kvh)), values.append(cut(visual[2][i], n, kvh)), queries.append(visual[0].double().numpy()[t, h])
+                streams = [(x, k["values"], v["values"]) for x, k, v in zip(queries, keys, values)]
+                want, want_lse = O.attention(qs[t, h], streams, scale)
+                where = f"sequence {i} query {t - a} head {h}"
+                if not np.isfinite(want_lse) and want_lse < 0:
+                    assert np.all(out[t, h] == 0) and lse[t, h] == -math.inf, where
+                    continue
+                logit = np.concatenate([k["values"] @ x * scale for x, k in zip(queries, keys)])
+                weights = np.exp(logit - want_lse)
+                tol, tol_lse = bound(queries, keys, values, scale, want, weights)
+                assert np.all(np.abs(out[t, h] - want) <= tol), (where, np.max(np.abs(out[t, h] - want) / tol))
+                assert abs(lse[t, h] - want_lse) <= tol_lse + 2.0 ** -23 * abs(want_lse), (where, lse[t, h], want_lse)
