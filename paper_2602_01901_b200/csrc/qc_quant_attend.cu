@@ -1,19 +1,18 @@
 // Attention of a step's queries over a cache in 4 bits.
 //
-// A row of K or V stands for lo + s c (s = 1 / r, codes c in 0..15), that is mid + s (c - 8) with mid = lo + 8 s, so
-//   q . k_j       = s_j sum_d q_d (c_jd - 8) + mid_j sum_d q_d
-//   sum_j p_j v_j = sum_j (p_j s_j)(c_jd - 8) + sum_j p_j mid_j
-// and the only large sums run over codes, which are exact in 16 bits: a code becomes an fp16 number by an AND and an
-// OR into the mantissa of 1024 (1024 + c, or 1024 + 16 c from the upper half of a byte) and one packed operation that
-// takes the constant off.  The queries are exact in fp16 as well once a power of two has brought the unit's
-// largest element below 2^12 (bf16 has fewer bits; what is 2^-25 of the largest loses bits, which no score shows).  The
-// weights p_j s_j are rounded to fp16 (2^-12) after a division by a power of two not below the warp's largest s.
-// Everything else is fp32.
+// A row of K or V stands for lo + s c (s = 1 / r, codes c in 0..15), so
+//   q . k_j       = s_j sum_d q_d c_jd + lo_j sum_d q_d
+//   sum_j p_j v_j = sum_j (p_j s_j)(c_jd - 8) + sum_j p_j (lo_j + 8 s_j)
+// and the long sums run over codes, which take next to no conversion: masked out of a word they are fp16 numbers already,
+// c * 2^-24 (subnormal ones, whose steps are equal), or 16 times that from the upper half of a byte.  The queries are exact in
+// fp16 once a power of two has brought the row's largest element below 2^15 (bf16 has fewer bits; what is below 2^-24 of the
+// largest loses some).  The weights p_j s_j are rounded to fp16 (2^-11) after a division by a power of two not below the
+// largest s so far.  Everything else is fp32.  The 8 is taken off tile by tile, as a product with ones: sums of c alone
+// would grow with the keys, and the tensor cores' adder, which cuts off, would leave a part of them behind.
 //
 // Products are m16n8k16 with the keys (for K) and the elements (for V) as rows and up to eight query rows as columns:
-// the heads of a group times the sequence's queries.  The pages are laid out for this (qc_quant.cuh): operands come
-// from global memory in whole 16-byte vectors in lane order, and a product's scores become the next one's weights by
-// two transposes in registers.
+// the heads of a group times the sequence's queries.  The pages are laid out for this (qc_quant.cuh): a lane's operands
+// are whole 16-byte vectors, and a product's scores become the next one's weights by two transposes in registers.
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -26,8 +25,10 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kAttWarps = 4;
-constexpr float kLeastStep = 3.9443045261050590e-31f;   // 2^-101, below every step but 0
+constexpr int kAttWarps = 8;
+constexpr int kUnitCost = 3;         // what a unit costs besides its tiles, in tiles
+constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
+constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
 
 struct StreamArgs {
   const uint16_t* q;
@@ -39,314 +40,424 @@ struct StreamArgs {
   int32_t max_pages, n_pages;
 };
 
+struct Border;
+
 struct AttendArgs {
-  StreamArgs text, visual;
+  StreamArgs stream[2];   // text, visual
   const int32_t* ids;
   const int32_t* starts;
   uint16_t* out;
   float* lse;
-  float* part;          // [splits][units][8 * NT][D + 2]
+  float* part;          // [teams][2][8 * NT * (D + 2)] pieces of units that reach over a border
+  Border* borders;      // [teams]
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, max_seqs, n_tokens, max_queries, causal, has_visual;
-  int32_t n_splits, row_tiles;
-  int64_t page_bytes;
+  int32_t n_borders;
+  float inv_group;
+  uint32_t page_units, head_units;   // bytes of a page, and of a head's codes in it, / 64
+  int64_t page_bytes, code_bytes;
   float scale_log2;
 };
 
-__device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
+__device__ __forceinline__ float4 lds_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
 }
-__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
+__device__ __forceinline__ void sts_f4(uint32_t addr, float2 a, float2 b) {
+  asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y) : "memory");
+}
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const uint8_t* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
 }
-// Bits 0-3 and 16-19 (lower) or 4-7 and 20-23 (upper) of x as two fp16 numbers c - 8.
-__device__ __forceinline__ uint32_t lower_codes(uint32_t x) { return sub_h2((x & 0x000f000fu) | 0x64006400u, 0x64086408u); }   // 1024 + c - 1032
-__device__ __forceinline__ uint32_t upper_codes(uint32_t x) {
-  return fma_h2((x & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);   // (1024 + 16 c) / 16 - 72
+// D = A B + C, fp16 operands (subnormal ones count), fp32 sums
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
+                                              float c2, float c3) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
-__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+constexpr uint32_t kLower = 0x000f000fu, kUpper = 0x00f000f0u;   // codes as two fp16 numbers: c * 2^-24, and c * 2^-20
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
-
-// The codes of a block of 16 tokens that a lane holds: for K the words of its even and its odd token, for V the
-// words of its element pairs.
-template <int D>
-struct Block {
-  uint4 w[D / 64];
-};
-template <int D>
-__device__ __forceinline__ void load_block(Block<D>& b, const uint8_t* p, int lane, bool on) {
-#pragma unroll
-  for (int i = 0; i < D / 64; ++i)
-    b.w[i] = on ? __ldg(reinterpret_cast<const uint4*>(p + i * 512 + lane * 16)) : make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t a) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
 }
 
-// One unit: up to 8 * NT query rows of one (sequence, KV head) that share their keys.  A warp's running state.
+// A warp's running state over the keys of one unit: up to 8 * NT query rows of one (sequence, KV head), its columns.
 template <int D, int NT>
 struct Rows {
-  float acc[NT][D / 16][4];
-  float m[NT][2], l[NT][2], z[NT][2];
-  float n;                 // the power of two that the weights were divided by
+  float acc[NT][D / 16][4];  // times 2^-24 (even elements) and 2^-20 (odd ones)
+  float ref[NT][2];          // what a column's scores (before the scale) are relative to; 0 before the first key that it sees
+  float l[NT][2], z[NT][2];  // this lane's part of sum p and sum p mid
+  uint32_t step;             // bits of the power of two that the weights were divided by
+  uint32_t seen;             // columns that have seen a key, a bit per (nt, x)
+  bool all_seen;             // every column of the warp has
 };
 
 template <int D, int NT>
 struct Query {
-  uint32_t b[NT][D / 16][2];   // operands of the score products
-  float sum[NT][2];            // sum of the elements, for the columns 2 t and 2 t + 1
-  float scale;                 // softmax scale * log2 e * the power of two that was taken out
+  uint32_t b[NT][D / 16][2];   // operands of the score products: lower codes' elements, and a 16th of the upper ones'
+  float sum[NT][2];            // sum of the elements times 2^-24, for the columns 2 t and 2 t + 1
+  float scale[NT][2];          // softmax scale * log2 e * the powers of two that were taken out
 };
 
-// Row r of the unit is query r / group of the sequence, head r % group of the KV head.
+// Row r of a unit is query r / group of the sequence, head r % group of the KV head.
+__device__ __forceinline__ int query_of(const AttendArgs& A, int r) { return static_cast<int>((static_cast<float>(r) + 0.5f) * A.inv_group); }
+
 template <int D, int NT>
 __device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A, const StreamArgs& S, int64_t token0, int head0, int row0,
                                            int n_rows, int lane) {
   const int g = lane >> 2, t = lane & 3;
-  uint4 raw[NT][D / 32];
-  float top = 0.f;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + nt * 8 + g;
+    const int r = row0 + nt * 8 + g, query = query_of(A, r);
     const bool on = r < n_rows;
-    const uint16_t* q = S.q + (token0 + r / A.group) * S.q_stride + static_cast<int64_t>(head0 + r % A.group) * D + t * (D / 4);
+    const uint16_t* q = S.q + (token0 + query) * S.q_stride + static_cast<int64_t>(head0 + r - query * A.group) * D + t * (D / 4);
+    uint4 raw[D / 32];
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      raw[nt][i] = on ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
-      float f[8];
-      bf16x8_to_f32(raw[nt][i], f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(f[j]));
+      raw[i] = on ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
+      top = max_bf16x2(top, max_bf16x2(max_bf16x2(raw[i].x & 0x7fff7fffu, raw[i].y & 0x7fff7fffu), max_bf16x2(raw[i].z & 0x7fff7fffu, raw[i].w & 0x7fff7fffu)));
     }
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  // 2^e with top * 2^-e in [2^11, 2^12); a zero or subnormal top counts as 2^-100, an infinite one as 2^127
-  const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127) - 11;
-  const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -111 <= e <= 116
-  Q.scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int top_exp = static_cast<int>(max(top & 0xffffu, top >> 16) >> 7);   // of the row's largest element
+    // 2^e with that element times 2^-e in [2^14, 2^15); a zero or subnormal one counts as 2^-90, the largest as 2^100
+    const int e = min(max(top_exp - 127, -90), 100) - 14;
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -104 <= e <= 86
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       float f[8];
-      bf16x8_to_f32(raw[nt][i], f);
+      bf16x8_to_f32(raw[i], f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        f[j] = __half2float(__float2half_rn(f[j] * down));
-        sum += f[j];
-      }
+      for (int j = 0; j < 8; ++j) f[j] *= down;
+      sum += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
       Q.b[nt][2 * i][0] = pack_f16x2(f[0], f[4]);
-      Q.b[nt][2 * i][1] = pack_f16x2(f[1], f[5]);
+      Q.b[nt][2 * i][1] = pack_f16x2(f[1] * 0.0625f, f[5] * 0.0625f);
       Q.b[nt][2 * i + 1][0] = pack_f16x2(f[2], f[6]);
-      Q.b[nt][2 * i + 1][1] = pack_f16x2(f[3], f[7]);
+      Q.b[nt][2 * i + 1][1] = pack_f16x2(f[3] * 0.0625f, f[7] * 0.0625f);
     }
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    Q.sum[nt][0] = __shfl_sync(0xffffffffu, sum, t * 8);
-    Q.sum[nt][1] = __shfl_sync(0xffffffffu, sum, t * 8 + 4);
-  }
-}
-
-// Scores of a block: c[0], c[1] the lane's even token for columns 2 t and 2 t + 1, c[2], c[3] its odd one.
-template <int D, int NT>
-__device__ __forceinline__ void score_block(const Block<D>& k, const Query<D, NT>& Q, float (&c)[NT][4]) {
-  uint32_t even[D / 32], odd[D / 32];
-  if constexpr (D == 128) {
-    even[0] = k.w[0].x, even[1] = k.w[0].y, even[2] = k.w[0].z, even[3] = k.w[0].w;
-    odd[0] = k.w[1].x, odd[1] = k.w[1].y, odd[2] = k.w[1].z, odd[3] = k.w[1].w;
-  } else {
-    even[0] = k.w[0].x, even[1] = k.w[0].y, odd[0] = k.w[0].z, odd[1] = k.w[0].w;
-  }
+    sum *= 5.9604644775390625e-8f;      // 2^-24
+    if (top_exp > 127 + 100) sum = NAN;      // (a row with an element of 2^101 or more, or an infinite one, has no scores)
+    const float scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + 24 + e) << 23);
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
-#pragma unroll
-  for (int w = 0; w < D / 32; ++w) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t xe = h ? even[w] >> 8 : even[w], xo = h ? odd[w] >> 8 : odd[w];
-      const uint32_t a0 = lower_codes(xe), a1 = lower_codes(xo), a2 = upper_codes(xe), a3 = upper_codes(xo);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16_16816(c[nt], a0, a1, a2, a3, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1]);
+    for (int x = 0; x < 2; ++x) {
+      Q.sum[nt][x] = __shfl_sync(0xffffffffu, sum, t * 8 + 4 * x);
+      Q.scale[nt][x] = __shfl_sync(0xffffffffu, scale, t * 8 + 4 * x);
     }
   }
 }
 
-// One tile of keys from key0 on; `len` keys are there, column x of tile nt sees those before lim[nt][x].
+// ---- tiles on their way -------------------------------------------------------------------------------
+//
+// A warp fetches its tiles into a ring of its own: three places for the codes of a tile of K or of V, in the order K, V,
+// K, V, ..., so that while one is worked on the next two are on their way, and two places for the parameters
+// (K's, then V's) of a tile, which come with its K.  A lane's 16-byte copies are the vectors that it reads later itself;
+// the parameters are read by other lanes.
+template <int D>
+struct Ring {
+  static constexpr int kCodes = kTile * D / 2;
+  static constexpr int kParams = kTile * 8;
+  static constexpr int kBytes = 3 * kCodes + 2 * kParams;
+};
+
+// Where the tile after the one that is worked on comes from.
+struct Fetch {
+  uint32_t at[kTile / 16];   // its blocks' codes in the pool, in units of 64 bytes
+  uint32_t on;               // blocks that are there, a bit each
+  int32_t id;                // lane 4 b + i: page id of block b (of the tile whose ids were asked for last)
+  uint32_t id_on;
+};
+
+// Asks for the page ids of a tile: lane 4 b + i has block b's (lanes from 16 on the same again).
+__device__ __forceinline__ void fetch_ids(Fetch& F, const AttendArgs& A, const StreamArgs& S, const int32_t* table, int key0, int len, int lane) {
+  const int key = key0 + ((lane >> 2) & 3) * 16;
+  F.id_on = key < len;
+  F.id = F.id_on ? __ldg(table + (key >> A.page_shift)) : 0;
+}
+
+// Requests the codes of a tile of K and the parameters of K and V.
+template <int D>
+__device__ __forceinline__ void fetch_keys(Fetch& F, const AttendArgs& A, const StreamArgs& S, int kvh, int key0, uint32_t codes, uint32_t params, int lane) {
+  const bool bad = F.id_on && static_cast<uint32_t>(F.id) >= static_cast<uint32_t>(S.n_pages);   // a page that is none is not followed
+  if (bad && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_BAD_PAGE));
+  const uint32_t there = __ballot_sync(0xffffffffu, F.id_on && !bad);
+  F.on = (there & 1u) | (there >> 3 & 2u) | (there >> 6 & 4u) | (there >> 9 & 8u);
+  const int32_t id = F.id_on && !bad ? F.id : 0;      // what is not there is fetched from page 0 and never looked at
+  const int mask = A.page - 1;
+#pragma unroll
+  for (int b = 0; b < kTile / 16; ++b) {
+    const uint32_t page = static_cast<uint32_t>(__shfl_sync(0xffffffffu, id, 4 * b));
+    F.at[b] = page * A.page_units + kvh * A.head_units + ((key0 + 16 * b) & mask) / 16 * (D / 8);
+    const uint8_t* src = S.k_pool + static_cast<uint64_t>(F.at[b]) * 64 + lane * 16;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) cp_async_16(codes + b * (8 * D) + i * 512 + lane * 16, src + i * 512);
+  }
+  const int in_page = (key0 + ((lane >> 2) & 3) * 16) & mask;
+  cp_async_16(params + lane * 16, (lane < 16 ? S.k_pool : S.v_pool) + static_cast<uint64_t>(static_cast<uint32_t>(id)) * A.page_bytes + A.code_bytes +
+                                      static_cast<uint32_t>((kvh * A.page + in_page) * 4 + (lane & 3) * 16));
+}
+
+template <int D>
+__device__ __forceinline__ void fetch_values(const Fetch& F, const StreamArgs& S, uint32_t codes, int lane) {
+#pragma unroll
+  for (int b = 0; b < kTile / 16; ++b) {
+    const uint8_t* src = S.v_pool + static_cast<uint64_t>(F.at[b]) * 64 + lane * 16;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) cp_async_16(codes + b * (8 * D) + i * 512 + lane * 16, src + i * 512);
+  }
+}
+
+// ---- a tile -----------------------------------------------------------------------------------------------
+
+// The products of a tile of K with the queries: c[b][nt], for the lane's even token of block b (0, 1: columns 2 t, 2 t + 1)
+// and its odd one (2, 3), times 2^-24.
 template <int D, int NT>
-__device__ __forceinline__ void attend_tile(Rows<D, NT>& R, const Query<D, NT>& Q, const AttendArgs& A, const StreamArgs& S, const int32_t* table,
-                                            int kvh, int key0, int len, const int32_t (&lim)[NT][2], int least_lim, int lane) {
+__device__ __forceinline__ void score_tile(float (&c)[kTile / 16][NT][4], const Query<D, NT>& Q, uint32_t codes, int lane) {
+#pragma unroll
+  for (int b = 0; b < kTile / 16; ++b) {
+    uint32_t even[D / 32], odd[D / 32];
+    const uint4 k0 = lds128(codes + b * (8 * D) + lane * 16);
+    if constexpr (D == 128) {
+      const uint4 k1 = lds128(codes + b * (8 * D) + 512 + lane * 16);
+      even[0] = k0.x, even[1] = k0.y, even[2] = k0.z, even[3] = k0.w;
+      odd[0] = k1.x, odd[1] = k1.y, odd[2] = k1.z, odd[3] = k1.w;
+    } else {
+      even[0] = k0.x, even[1] = k0.y, odd[0] = k0.z, odd[1] = k0.w;
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) c[b][nt][0] = c[b][nt][1] = c[b][nt][2] = c[b][nt][3] = 0.f;
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t xe = h ? even[w] >> 8 : even[w], xo = h ? odd[w] >> 8 : odd[w];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          mma_f16_16816(c[b][nt], xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1], c[b][nt][0], c[b][nt][1],
+                        c[b][nt][2], c[b][nt][3]);
+      }
+  }
+}
+
+__device__ __forceinline__ float step_of(uint32_t params) {
+  const float r = __uint_as_float(params & 0xffff0000u);
+  float s;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(r));   // (off by 2^-23 of itself)
+  return r == 0.f ? 0.f : s;
+}
+
+// What the parameters of a tile's rows say, each worked out by one lane: lane l has the rows 4 l .. 4 l + 3 of 128, K's and then
+// V's.  (s, lo) for K, (s, lo + 8 s) for V; those of V rows that are not there may be whatever was there before
+// and count as 0.
+struct RowValues {
+  float2 v[4];
+};
+__device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, uint32_t on, int left, bool masked, int lane) {
+  const uint4 raw = lds128(params + lane * 16);
+  const uint32_t p[4] = {raw.x, raw.y, raw.z, raw.w};
+  const bool is_v = lane >= 16;
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float s = step_of(p[i]);
+    const float lo = __uint_as_float(p[i] << 16);
+    float m = is_v ? fmaf(8.f, s, lo) : lo;
+    if (masked && is_v && (!(on >> (lane >> 2 & 3) & 1u) || (lane & 15) * 4 + i >= left)) s = m = 0.f;
+    top = fmaxf(top, s);
+    r.v[i] = make_float2(s, m);
+  }
+  return is_v ? top : 0.f;
+}
+
+// Weights of a tile's scores, as operands of the value products.  `rows`: what rows_of found, in shared memory; `top`: the
+// largest step that this lane saw.  `masked`: the tile has keys that are not there, or that some column does not see; `left` keys are there from its first
+// on, `back` of them are behind the unit's first query.
+template <int D, int NT>
+__device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16][NT][4], uint32_t (&w)[kTile / 16][NT][2], const Query<D, NT>& Q,
+                                           uint32_t rows, float top, uint32_t on, const AttendArgs& A, int left, int row0, int back, bool masked, int lane) {
   constexpr int kBlocks = kTile / 16;
   const int g = lane >> 2;
-  Block<D> kb[kBlocks], vb[kBlocks];
-  uint2 kp[kBlocks], vp[kBlocks];
-  bool on[kBlocks];
-  const size_t code_bytes = static_cast<size_t>(A.hkv) * A.page * (D / 2);
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b) {
-    const int key = key0 + 16 * b;
-    on[b] = key < len;
-    const int32_t id = on[b] ? table[key >> A.page_shift] : 0;
-    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(S.n_pages)) {   // not followed
-      if (lane == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_BAD_PAGE));
-      on[b] = false;
-    }
-    const int in_page = key & (A.page - 1);
-    const size_t base = static_cast<size_t>(on[b] ? id : 0) * A.page_bytes;
-    const size_t code = base + (static_cast<size_t>(kvh) * A.page + in_page) * (D / 2);
-    const size_t word = base + code_bytes + (static_cast<size_t>(kvh) * A.page + in_page + 2 * g) * 4;
-    load_block<D>(kb[b], S.k_pool + code, lane, on[b]);
-    kp[b] = on[b] ? __ldg(reinterpret_cast<const uint2*>(S.k_pool + word)) : make_uint2(0, 0);
-    load_block<D>(vb[b], S.v_pool + code, lane, on[b]);
-    vp[b] = on[b] ? __ldg(reinterpret_cast<const uint2*>(S.v_pool + word)) : make_uint2(0, 0);
-  }
-
-  float s[kBlocks][NT][4];
-#pragma unroll
-  for (int b = 0; b < kBlocks; ++b) {
-    score_block<D, NT>(kb[b], Q, s[b]);
-    const float s0 = quant_step(kp[b].x), s1 = quant_step(kp[b].y);
-    const float m0 = fmaf(8.f, s0, __uint_as_float(kp[b].x << 16)) * Q.scale, m1 = fmaf(8.f, s1, __uint_as_float(kp[b].y << 16)) * Q.scale;
-    const float f0 = s0 * Q.scale, f1 = s1 * Q.scale;
+    const float4 k = lds_f4(rows + b * 128 + g * 16);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      s[b][nt][0] = fmaf(f0, s[b][nt][0], m0 * Q.sum[nt][0]);
-      s[b][nt][1] = fmaf(f0, s[b][nt][1], m0 * Q.sum[nt][1]);
-      s[b][nt][2] = fmaf(f1, s[b][nt][2], m1 * Q.sum[nt][0]);
-      s[b][nt][3] = fmaf(f1, s[b][nt][3], m1 * Q.sum[nt][1]);
+      c[b][nt][0] = fmaf(k.x, c[b][nt][0], fmaf(k.y, Q.sum[nt][0], -R.ref[nt][0]));
+      c[b][nt][1] = fmaf(k.x, c[b][nt][1], fmaf(k.y, Q.sum[nt][1], -R.ref[nt][1]));
+      c[b][nt][2] = fmaf(k.z, c[b][nt][2], fmaf(k.w, Q.sum[nt][0], -R.ref[nt][0]));
+      c[b][nt][3] = fmaf(k.z, c[b][nt][3], fmaf(k.w, Q.sum[nt][1], -R.ref[nt][1]));
     }
   }
-  const bool all_on = on[0] && on[1] && on[2] && on[3];
-  const bool masked = key0 + kTile > least_lim || !all_on;   // the same for the whole warp
   if (masked) {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int x = 0; x < 2; ++x) {
+        // keys of the tile that the column sees
+        const int seen = left - max(0, back - query_of(A, row0 + nt * 8 + 2 * (lane & 3) + x));
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (!on[b] || key0 + 16 * b + 2 * g + (x >> 1) >= lim[nt][x & 1]) s[b][nt][x] = -INFINITY;
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (!(on >> b & 1u) || 16 * b + 2 * g + i >= seen) c[b][nt][2 * i + x] = -INFINITY;
+      }
   }
-  // a row that no column sees has no part in anything: its parameters may be whatever was there before
-  float step[kBlocks][2], mid[kBlocks][2];
-  uint32_t top = 0;
-#pragma unroll
-  for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t p = i ? vp[b].y : vp[b].x;
-      step[b][i] = quant_step(p);
-      mid[b][i] = fmaf(8.f, step[b][i], __uint_as_float(p << 16));
-      if (masked && (!on[b] || key0 + 16 * b + 2 * g + i >= len)) step[b][i] = mid[b][i] = 0.f;
-      top = max(top, __float_as_uint(fminf(step[b][i], 1e38f)));
-    }
-  top = __reduce_max_sync(0xffffffffu, top);
-  // larger scores or steps than before: everything so far is put on the new reference
-  bool more = __uint_as_float(top) > R.n;
+  // scores above what they are relative to, or larger steps than before: everything so far is put on a new reference
+  bool more = !R.all_seen || __float_as_uint(top) > R.step;
   float high[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      float h = s[0][nt][x];
+      float h = fmaxf(c[0][nt][x], c[0][nt][x + 2]);
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) h = fmaxf(h, fmaxf(s[b][nt][x], s[b][nt][x + 2]));
+      for (int b = 1; b < kBlocks; ++b) h = max3(h, c[b][nt][x], c[b][nt][x + 2]);
       high[nt][x] = h;
-      more |= h > R.m[nt][x];
+      more |= h > 0.f;
     }
   if (__any_sync(0xffffffffu, more)) {
-    const float n_new = fmaxf(R.n, __uint_as_float((top & 0x7f800000u) + 0x00800000u));
-    const float down = R.n / n_new;
+    // the next power of two; a step that is no number, or beyond 2^126, makes its row's outputs no numbers anyway
+    const uint32_t top_bits = __reduce_max_sync(0xffffffffu, __float_as_uint(fminf(top, 8.5e37f)));
+    const uint32_t now = max(R.step, top_bits > R.step ? (top_bits & 0x7f800000u) + 0x00800000u : 0u);
+    const float down = now - R.step >= (126u << 23) ? 0.f : __uint_as_float((127u << 23) - (now - R.step));   // old / new
+    R.step = now;
+    bool all = true;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        const uint32_t bit = 1u << (2 * nt + x);
         float h = high[nt][x];
         h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 4));
         h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 8));
         h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 16));
-        h = fmaxf(h, R.m[nt][x]);
-        const float corr = h == R.m[nt][x] ? 1.f : exp2f(R.m[nt][x] - h);   // (both minus infinity: nothing so far)
-        R.m[nt][x] = h;
+        const bool known = R.seen & bit, any = h > -INFINITY;
+        const float delta = (known ? h > 0.f : any) ? h : 0.f;
+        const float corr = known ? exp2f(-delta * Q.scale[nt][x]) : 1.f;      // (nothing so far: nothing to put on another reference)
+        R.ref[nt][x] += delta;
+        if (any) R.seen |= bit;
+        all &= (R.seen & bit) != 0;
         R.l[nt][x] *= corr;
         R.z[nt][x] *= corr;
         const float f = corr * down;
 #pragma unroll
         for (int mb = 0; mb < D / 16; ++mb) R.acc[nt][mb][x] *= f, R.acc[nt][mb][x + 2] *= f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) c[b][nt][x] -= delta, c[b][nt][x + 2] -= delta;
       }
-    R.n = n_new;
+    R.all_seen = __all_sync(0xffffffffu, all);
   }
-  // weights
-  const float up = 32768.f / R.n;      // p s / n <= 1: the largest weight is 2^15
-  uint32_t w[kBlocks][NT][2];
+  const float up = __uint_as_float(((127u + 127u + 15u) << 23) - R.step);      // 2^15 / step: the largest weight is 2^15
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b) {
-    const float u0 = step[b][0] * up, u1 = step[b][1] * up;
+    const float4 v = lds_f4(rows + kTile * 8 + b * 128 + g * 16);
+    const float u0 = v.x * up, u1 = v.z * up, mid[2] = {v.y, v.w};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float p[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const float m = R.m[nt][x & 1];
-        p[x] = ex2_approx(s[b][nt][x] - (m == -INFINITY ? 0.f : m));
+        p[x] = ex2_approx(c[b][nt][x] * Q.scale[nt][x & 1]);
         R.l[nt][x & 1] += p[x];
-        // (a value that is no number counts only where it is seen)
-        R.z[nt][x & 1] = fmaf(p[x], masked && p[x] == 0.f ? 0.f : mid[b][x >> 1], R.z[nt][x & 1]);
       }
-      w[b][nt][0] = movmatrix_trans(pack_f16x2(p[0] * u0, p[1] * u0));
-      w[b][nt][1] = movmatrix_trans(pack_f16x2(p[2] * u1, p[3] * u1));
+      if (!masked) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) R.z[nt][x & 1] = fmaf(p[x], mid[x >> 1], R.z[nt][x & 1]);
+      } else {      // (a value that is no number counts only where it is seen)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) R.z[nt][x & 1] = fmaf(p[x], p[x] == 0.f ? 0.f : mid[x >> 1], R.z[nt][x & 1]);
+      }
+      w[b][nt][0] = transpose_8x8(pack_f16x2(p[0] * u0, p[1] * u0));
+      w[b][nt][1] = transpose_8x8(pack_f16x2(p[2] * u1, p[3] * u1));
     }
   }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[kTile / 16][NT][2], uint32_t codes, int lane) {
+  constexpr int kBlocks = kTile / 16;
+  // - 8 * the weights' sums, of even elements' codes, and of odd ones' (which are 16 times as large)
+  float less[NT][4];
 #pragma unroll
-  for (int mb = 0; mb < D / 16; ++mb)
+  for (int nt = 0; nt < NT; ++nt) {
+    less[nt][0] = less[nt][1] = less[nt][2] = less[nt][3] = 0.f;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)      // rows of 8 * 2^-24 and of 128 * 2^-24, negative
+      mma_f16_16816(less[nt], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, w[b][nt][0], w[b][nt][1], less[nt][0], less[nt][1], less[nt][2], less[nt][3]);
+  }
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    uint32_t x[kBlocks][4];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      const uint4& v = vb[b].w[mb / 4];
-      const uint32_t x = mb % 4 == 0 ? v.x : mb % 4 == 1 ? v.y : mb % 4 == 2 ? v.z : v.w;
-      const uint32_t a0 = lower_codes(x), a1 = upper_codes(x), a2 = lower_codes(x >> 8), a3 = upper_codes(x >> 8);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16_16816(R.acc[nt][mb], a0, a1, a2, a3, w[b][nt][0], w[b][nt][1]);
+      const uint4 v = lds128(codes + b * (8 * D) + i * 512 + lane * 16);
+      x[b][0] = v.x, x[b][1] = v.y, x[b][2] = v.z, x[b][3] = v.w;
     }
-}
-
-// Writes D finished elements of a row: lane g's run of D / 8.
-template <int D>
-__device__ __forceinline__ void store_run(uint16_t* row, int g, const float (&o)[D / 8]) {
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i)
-    reinterpret_cast<uint4*>(row + g * (D / 8))[i] = make_uint4(pack_bf16x2(o[8 * i], o[8 * i + 1]), pack_bf16x2(o[8 * i + 2], o[8 * i + 3]),
-                                                                pack_bf16x2(o[8 * i + 4], o[8 * i + 5]), pack_bf16x2(o[8 * i + 6], o[8 * i + 7]));
+    for (int j = 0; j < 4; ++j) {
+      float sum[NT][4];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        const uint32_t lo = x[b][j], hi = lo >> 8;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float(&c)[4] = b == 0 ? less[nt] : sum[nt];
+          mma_f16_16816(sum[nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1], c[0], c[1], c[2], c[3]);
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) R.acc[nt][4 * i + j][k] += sum[nt][k];
+    }
+  }
 }
 
-// What a part with reference ms and a sum counts for on reference m.  Minus infinity with a sum means that its scores were
-// no numbers.
-__device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : exp2f(ms - m); }
+// ---- the batch's work as one row -------------------------------------------------------------------------
+//
+// Sequence after sequence, unit after unit (KV head, then rows of queries), tile after tile (the visual stream's, then the
+// text's).  A unit costs its tiles and kUnitCost more.  The row is cut into equal ranges, one per team of 1, 2, 4 or 8 warps, so that
+// the teams end together whatever the lengths are; a team takes a unit's tiles in turn, warp by warp.  A unit inside one
+// range is finished there; of one that reaches over a border each team leaves its sums, and the launch that follows puts
+// them together, in the order of the teams.  Where units are short next to that launch, or next to a range, a team
+// takes those that begin in its range whole, and nothing is left to put together.
 
-struct UnitPlace {
-  int64_t token0;    // the sequence's first query
-  int32_t n_rows;    // query rows of the (sequence, KV head); 0: nothing to do
-  int32_t queries;
-  int32_t row;       // row of the page tables
+struct Place {       // one sequence
+  int64_t token0;    // its first query
+  int32_t n_rows;    // query rows per KV head; 0: nothing to do
+  int32_t queries, row;
+  int32_t len[2], tiles_v, tiles;
 };
 
-__device__ __forceinline__ UnitPlace place_of(const AttendArgs& A, int seq, bool report) {
-  UnitPlace u{0, 0, 0, 0};
+__device__ __forceinline__ int length_of(const AttendArgs& A, const StreamArgs& S, int row, bool report) {
+  const int64_t len = __ldg(S.lens + row), room = static_cast<int64_t>(S.max_pages) << A.page_shift;
+  if (len >= 0 && len <= room) return static_cast<int>(len);
+  if (report && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
+  return len < 0 ? 0 : static_cast<int>(room);
+}
+
+__device__ __forceinline__ Place place_of(const AttendArgs& A, int seq, bool report) {
+  Place u{};
   int64_t a = seq, b = seq + 1;
-  if (A.starts) a = A.starts[seq], b = A.starts[seq + 1];
-  u.row = A.ids ? A.ids[seq] : seq;
+  if (A.starts) a = __ldg(A.starts + seq), b = __ldg(A.starts + seq + 1);
+  u.row = A.ids ? __ldg(A.ids + seq) : seq;
   if (a < 0 || b < a || b > A.n_tokens || b - a > A.max_queries || u.row < 0 || u.row >= A.max_seqs) {
     if (report && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_INVALID_ARG));
     return u;
@@ -354,138 +465,334 @@ __device__ __forceinline__ UnitPlace place_of(const AttendArgs& A, int seq, bool
   u.token0 = a;
   u.queries = static_cast<int32_t>(b - a);
   u.n_rows = u.queries * A.group;
+  if (u.n_rows == 0) return u;
+  u.len[0] = length_of(A, A.stream[0], u.row, report);
+  u.len[1] = A.has_visual ? length_of(A, A.stream[1], u.row, report) : 0;
+  u.tiles_v = (u.len[1] + kTile - 1) / kTile;
+  u.tiles = max(1, u.tiles_v + (u.len[0] + kTile - 1) / kTile);   // (without any key there still is a row to write)
   return u;
 }
 
-__device__ __forceinline__ int length_of(const AttendArgs& A, const StreamArgs& S, int row, bool report) {
-  const int64_t len = S.lens[row], room = static_cast<int64_t>(S.max_pages) << A.page_shift;
-  if (len >= 0 && len <= room) return static_cast<int>(len);
-  if (report && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
-  return len < 0 ? 0 : static_cast<int>(room);
+// What a part with reference ms and a sum counts for on reference m.  Minus infinity with a sum means that its scores were
+// no numbers.
+__device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : exp2f(ms - m); }
+
+template <int D>
+__device__ __forceinline__ void write_row(const AttendArgs& A, size_t row, float m, float l, const float (&o)[D / 32], int lane) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (D == 128) {
+    reinterpret_cast<uint2*>(A.out + row * D)[lane] = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+  } else {
+    reinterpret_cast<uint32_t*>(A.out + row * D)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
+  }
+  if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
-// Grid: (splits, KV heads x row tiles, sequences).
-template <int D, int NT>
-__global__ void __launch_bounds__(kAttWarps * 32) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
-  __shared__ float sm_acc[kAttWarps][8 * NT][D];
-  __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x, kvh = blockIdx.y / A.row_tiles, row0 = blockIdx.y % A.row_tiles * (8 * NT), seq = blockIdx.z;
-  pdl_launch_dependents();
-  const UnitPlace u = place_of(A, seq, threadIdx.x == 0);
-  if (row0 >= u.n_rows) return;
-  const int len_t = length_of(A, A.text, u.row, threadIdx.x == 0);
-  const int len_v = A.has_visual ? length_of(A, A.visual, u.row, threadIdx.x == 0) : 0;
-  const int tiles_v = (len_v + kTile - 1) / kTile, tiles = tiles_v + (len_t + kTile - 1) / kTile;
-  const int per = (tiles + A.n_splits - 1) / A.n_splits;
-  const int first = split * per, last = min(tiles, first + per);
-
-  Rows<D, NT> R;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) R.m[nt][x] = -INFINITY, R.l[nt][x] = R.z[nt][x] = 0.f;
-#pragma unroll
-    for (int mb = 0; mb < D / 16; ++mb) R.acc[nt][mb][0] = R.acc[nt][mb][1] = R.acc[nt][mb][2] = R.acc[nt][mb][3] = 0.f;
+template <int D>
+__device__ __forceinline__ void load_run(const float* p, float (&o)[D / 32], int lane) {   // this lane's elements of a row
+  if constexpr (D == 128) {
+    const float4 v = reinterpret_cast<const float4*>(p)[lane];
+    o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+  } else {
+    const float2 v = reinterpret_cast<const float2*>(p)[lane];
+    o[0] = v.x, o[1] = v.y;
   }
-  R.n = kLeastStep;
-  int tile = first + warp;
-#pragma unroll 1
-  for (int part = 0; part < 2; ++part) {
-    const bool visual = part == 0;
-    const int begin = visual ? 0 : tiles_v, end = min(last, visual ? tiles_v : tiles);
-    if (tile >= end) continue;
-    const StreamArgs& S = visual ? A.visual : A.text;
-    const int len = visual ? len_v : len_t;
+}
+
+// A unit that reaches over the border behind a team's range: what puts its pieces together has to know.
+struct __align__(16) Border {
+  int64_t token0;
+  int32_t kvh, row0, n_rows;     // n_rows: of the sequence; 0: no unit begins here and reaches over
+  int32_t last;                  // the last team with a piece
+  int32_t place;                 // of the first piece: 0 if it is the team's first unit, else 1 (later teams': 0)
+  int32_t pad;
+};
+static_assert(sizeof(Border) == 32, "Border layout");
+
+// A piece: columns of D elements, then (reference, sum) of each column.
+template <int D, int NT>
+__device__ __forceinline__ float* piece_at(const AttendArgs& A, int team, int place) {
+  return A.part + (static_cast<size_t>(team) * 2 + place) * (8 * NT * (D + 2));
+}
+
+__device__ __forceinline__ void team_barrier(int team, int threads) {
+  if (threads == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory");
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+  using R_ = Ring<D>;
+  constexpr int kRow = D + 4;            // of a column's sums in shared memory
+  static_assert(8 * NT * kRow * 4 <= R_::kBytes, "a warp's sums take its ring's place");
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint32_t scan[kAttWarps];
+  __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
+  __shared__ uint32_t longest_, units_;
+  uint32_t* before = reinterpret_cast<uint32_t*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] what the sequences before cost
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) before[0] = longest_ = units_ = 0;
+  __syncthreads();
+  uint64_t total = 0;
+  for (int i0 = 0; i0 < A.n_seqs; i0 += kAttWarps * 32) {
+    const int i = i0 + threadIdx.x;
+    uint64_t mine = 0;
+    if (i < A.n_seqs) {
+      const Place u = place_of(A, i, blockIdx.x == 0);
+      const uint32_t units = A.hkv * ((u.n_rows + 8 * NT - 1) / (8 * NT));
+      mine = static_cast<uint64_t>(u.tiles + kUnitCost) * units;
+      if (units) atomicMax(&longest_, static_cast<uint32_t>(u.tiles)), atomicAdd(&units_, units);
+    }
+    const bool big = mine > (1u << 22);
+    uint32_t x = big ? 0u : static_cast<uint32_t>(mine);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) scan[warp] = x;
+    const bool any_big = __syncthreads_or(big);
+    uint32_t base = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < kAttWarps; ++w) {
+      if (w < warp) base += scan[w];
+      sum += scan[w];
+    }
+    if (i < A.n_seqs) before[i + 1] = static_cast<uint32_t>(total) + base + x;
+    total += sum;
+    if (any_big || total > (1u << 30)) {      // a batch of more than 2^36 rows
+      if (blockIdx.x == 0 && threadIdx.x == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
+      total = 0;
+      break;
+    }
+    __syncthreads();
+  }
+  const uint32_t cost = static_cast<uint32_t>(total), units = units_, longest = longest_;
+  // warps of a team: no more than the average unit has tiles, unless there are warps for more
+  const uint32_t n_warps = gridDim.x * kAttWarps, tiles_all = cost - units * kUnitCost;
+  uint32_t team_warps = 1;
+  while (team_warps < kAttWarps && (units * team_warps * 2 <= tiles_all || units * team_warps * 2 <= n_warps)) team_warps *= 2;
+  const uint32_t n_teams = n_warps / team_warps;
+  const int threads = team_warps * 32, in_block = warp / team_warps, member = warp % team_warps, team0 = in_block * team_warps;
+  const uint32_t team = blockIdx.x * (kAttWarps / team_warps) + in_block;
+  uint32_t per = (cost + n_teams - 1) / n_teams;
+  const bool whole_units = longest <= max(team_warps * kWholeTiles, per / 8);
+  if (!whole_units) per = max(per, team_warps + kUnitCost);
+  if (member == 0 && lane == 0) {
+    const Border none{};
+    A.borders[team] = none;
+  }
+  for (uint32_t i = blockIdx.x * kAttWarps + warp + n_teams; lane == 0 && i < n_warps; i += n_warps) {
+    const Border none{};
+    A.borders[i] = none;
+  }
+  uint32_t at = min(static_cast<uint64_t>(team) * per, static_cast<uint64_t>(cost));
+  const uint32_t end = min(cost, at + per);
+  if (at >= end) return;
+  int seq = 0;
+  {   // the last sequence that begins at or before the range
+    int lo = 0, hi = A.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before[mid] <= at) lo = mid;
+      else hi = mid - 1;
+    }
+    seq = lo;
+  }
+  const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
+  int done = 0;      // units so far
+  while (at < end) {
+    while (before[seq + 1] <= at) ++seq;
+    const Place u = place_of(A, seq, false);
+    const int row_tiles = (u.n_rows + 8 * NT - 1) / (8 * NT), unit_cost = u.tiles + kUnitCost;
+    int unit = (at - before[seq]) / unit_cost, first = 0, last = u.tiles;
+    uint32_t unit_at = before[seq] + unit * unit_cost;
+    if (whole_units) {
+      if (unit_at < at) {      // it begins before the range: the next one
+        at = unit_at + unit_cost;
+        continue;
+      }
+    } else {
+      first = max(0, static_cast<int>(at - unit_at) - kUnitCost);
+      last = min(u.tiles, static_cast<int>(end - unit_at) - kUnitCost);
+    }
+    at = unit_at + unit_cost;
+    if (first >= last) continue;
+    const int kvh = unit / row_tiles, row0 = (unit - kvh * row_tiles) * (8 * NT);
+
+    Rows<D, NT> R;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) R.ref[nt][x] = R.l[nt][x] = R.z[nt][x] = 0.f;
+#pragma unroll
+      for (int mb = 0; mb < D / 16; ++mb) R.acc[nt][mb][0] = R.acc[nt][mb][1] = R.acc[nt][mb][2] = R.acc[nt][mb][3] = 0.f;
+    }
+    R.step = kLeastStep;
+    R.seen = 0;
+    R.all_seen = false;
+
     Query<D, NT> Q;
-    load_query<D, NT>(Q, A, S, u.token0, kvh * A.group, row0, u.n_rows, lane);
-    int32_t lim[NT][2], least = INT32_MAX;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) Q.scale[nt][0] = Q.scale[nt][1] = 0.f;
+    int stream = -1;           // of the queries at hand
+    Fetch F;
+    // a tile's stream, and its first key
+    const auto stream_of = [&](int tile) { return tile < u.tiles_v ? 1 : 0; };
+    const auto key_of = [&](int tile) { return (tile < u.tiles_v ? tile : tile - u.tiles_v) * kTile; };
+    const auto ids = [&](int tile) {
+      if (tile >= last) return;
+      const StreamArgs& S = A.stream[stream_of(tile)];
+      fetch_ids(F, A, S, S.pages + static_cast<size_t>(u.row) * S.max_pages, key_of(tile), tile < u.tiles_v ? u.len[1] : u.len[0], lane);
+    };
+    const auto keys = [&](int tile, int slot, int par) {
+      if (tile < last) fetch_keys<D>(F, A, A.stream[stream_of(tile)], kvh, key_of(tile), ring + slot * R_::kCodes, ring + 3 * R_::kCodes + par * R_::kParams, lane);
+      cp_async_commit_group();
+    };
+    const auto values = [&](int tile, int slot) {
+      if (tile < last) fetch_values<D>(F, A.stream[stream_of(tile)], ring + slot * R_::kCodes, lane);
+      cp_async_commit_group();
+    };
+    int tile = first + member, slot = 0, par = 0;
+    const int stride = team_warps;
+    ids(tile);
+    keys(tile, 0, 0);
+    uint32_t on = F.on;
+    values(tile, 1);
+    ids(tile + stride);
+    for (; tile < last; tile += stride) {
+      const int now = stream_of(tile), after = tile + stride;
+      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
+      const uint32_t on_now = on;
+      keys(after, slot2, par ^ 1);      // the place of the V before
+      on = F.on;
+      if (stream != now) {
+        // (scores are in the units of the stream's queries, and so is what they are relative to)
+        float was[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) was[nt][0] = Q.scale[nt][0], was[nt][1] = Q.scale[nt][1];
+        load_query<D, NT>(Q, A, A.stream[now], u.token0, kvh * A.group, row0, u.n_rows, lane);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            if (stream >= 0 && R.ref[nt][x] != 0.f) R.ref[nt][x] *= was[nt][x] / Q.scale[nt][x];
+        stream = now;
+      }
+      const int left = (now ? u.len[1] : u.len[0]) - key_of(tile), back = now || !A.causal ? 0 : u.queries - 1;
+      const bool masked = left - back < kTile || on_now != 15u;
+      const uint32_t scratch = ring + slot * R_::kCodes;      // K's place, once its codes are read
+      float c[kTile / 16][NT][4];
+      uint32_t w[kTile / 16][NT][2];
+      cp_async_wait_group<2>();
+      __syncwarp();
+      score_tile<D, NT>(c, Q, scratch, lane);
+      __syncwarp();
+      float top;
+      {
+        RowValues rows;
+        top = rows_of(rows, ring + 3 * R_::kCodes + par * R_::kParams, on_now, left, masked, lane);
+        sts_f4(scratch + lane * 32, rows.v[0], rows.v[1]);
+        sts_f4(scratch + lane * 32 + 16, rows.v[2], rows.v[3]);
+      }
+      __syncwarp();
+      weigh_tile<D, NT>(R, c, w, Q, scratch, top, on_now, A, left, row0, back, masked, lane);
+      __syncwarp();
+      values(after, slot);
+      ids(after + stride);
+      cp_async_wait_group<2>();
+      __syncwarp();
+      add_values<D, NT>(R, w, ring + slot1 * R_::kCodes, lane);
+      __syncwarp();
+      slot = slot2;
+      par ^= 1;
+    }
+    cp_async_wait_all();
+    __syncwarp();
+    // the team's sums meet in shared memory
+    const float unit_step = __uint_as_float(R.step) * (1.f / 32768.f);
+    constexpr float kEven = 16777216.f, kOdd = 1048576.f;
+    float* mine = reinterpret_cast<float*>(smem + warp * R_::kBytes);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int r = row0 + nt * 8 + 2 * t + x;
-        lim[nt][x] = !visual && A.causal && r < u.n_rows ? len - (u.queries - 1 - r / A.group) : len;
-        least = min(least, lim[nt][x]);
+        float l = R.l[nt][x], z = R.z[nt][x];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o), z += __shfl_xor_sync(0xffffffffu, z, o);
+        const int col = nt * 8 + 2 * t + x;
+        if (g == 0) sm_m[warp][col] = R.seen >> (2 * nt + x) & 1u ? R.ref[nt][x] * Q.scale[nt][x] : -INFINITY, sm_l[warp][col] = l;
+        if (row0 + col < u.n_rows) {
+          float* dst = mine + col * kRow + g * (D / 8);
+#pragma unroll
+          for (int mb = 0; mb < D / 16; mb += 2)
+            *reinterpret_cast<float4*>(dst + 2 * mb) = make_float4(fmaf(R.acc[nt][mb][x] * kEven, unit_step, z), fmaf(R.acc[nt][mb][x + 2] * kOdd, unit_step, z),
+                                                                   fmaf(R.acc[nt][mb + 1][x] * kEven, unit_step, z), fmaf(R.acc[nt][mb + 1][x + 2] * kOdd, unit_step, z));
+        }
       }
-    least = min(least, __shfl_xor_sync(0xffffffffu, least, 1));
-    least = min(least, __shfl_xor_sync(0xffffffffu, least, 2));
-    const int32_t* table = S.pages + static_cast<size_t>(u.row) * S.max_pages;
-    for (; tile < end; tile += kAttWarps)
-      attend_tile<D, NT>(R, Q, A, S, table, kvh, (tile - begin) * kTile, len, lim, least, lane);
-  }
-  // the warps' sums meet in shared memory
-  const float unit = R.n * (1.f / 32768.f);
+    team_barrier(in_block, threads);
+    const int n_here = min(8 * NT, u.n_rows - row0);
+    const bool whole = first == 0 && last == u.tiles;
+    float* piece = piece_at<D, NT>(A, team, done == 0 ? 0 : 1);
+    for (int col = member; col < n_here; col += stride) {
+      float m = -INFINITY, l = 0.f, o[D / 32] = {};
+      for (int w = team0; w < team0 + stride; ++w) m = fmaxf(m, sm_m[w][col]);
+      for (int w = team0; w < team0 + stride; ++w) {
+        if (sm_l[w][col] == 0.f) continue;
+        const float f = weight_of(sm_m[w][col], m);
+        l = fmaf(sm_l[w][col], f, l);
+        float v[D / 32];
+        load_run<D>(reinterpret_cast<const float*>(smem + w * R_::kBytes) + col * kRow, v, lane);
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float l = R.l[nt][x], z = R.z[nt][x];
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o), z += __shfl_xor_sync(0xffffffffu, z, o);
-      const int col = nt * 8 + 2 * t + x;
-      if (g == 0) sm_m[warp][col] = R.m[nt][x], sm_l[warp][col] = l;
-#pragma unroll
-      for (int mb = 0; mb < D / 16; ++mb) {
-        sm_acc[warp][col][g * (D / 8) + 2 * mb] = fmaf(R.acc[nt][mb][x], unit, z);
-        sm_acc[warp][col][g * (D / 8) + 2 * mb + 1] = fmaf(R.acc[nt][mb][x + 2], unit, z);
+        for (int i = 0; i < D / 32; ++i) o[i] = fmaf(v[i], f, o[i]);
+      }
+      if (whole) {
+        const int r = row0 + col, query = query_of(A, r);
+        write_row<D>(A, static_cast<size_t>(u.token0 + query) * A.hq + kvh * A.group + r - query * A.group, m, l, o, lane);
+      } else {
+        if constexpr (D == 128) reinterpret_cast<float4*>(piece + col * D)[lane] = make_float4(o[0], o[1], o[2], o[3]);
+        else reinterpret_cast<float2*>(piece + col * D)[lane] = make_float2(o[0], o[1]);
+        if (lane == 0) reinterpret_cast<float2*>(piece + 8 * NT * D)[col] = make_float2(m, l);
       }
     }
-  __syncthreads();
-  const int n_here = min(8 * NT, u.n_rows - row0);
-  for (int col = warp; col < n_here; col += kAttWarps) {
-    float m = -INFINITY, l = 0.f, o[D / 32] = {};
-#pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) m = fmaxf(m, sm_m[w][col]);
-#pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) {
-      if (sm_l[w][col] == 0.f) continue;
-      const float f = weight_of(sm_m[w][col], m);
-      l = fmaf(sm_l[w][col], f, l);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) o[i] = fmaf(sm_acc[w][col][i * 32 + lane], f, o[i]);
+    if (member == 0 && lane == 0 && first == 0 && last < u.tiles) {      // it goes on behind the range
+      Border b{};
+      b.token0 = u.token0, b.kvh = kvh, b.row0 = row0, b.n_rows = u.n_rows;
+      b.last = (unit_at + unit_cost - 1) / per;
+      b.place = done == 0 ? 0 : 1;
+      A.borders[team] = b;
     }
-    const int r = row0 + col;
-    if (A.n_splits == 1) {
-      const size_t row = static_cast<size_t>(u.token0 + r / A.group) * A.hq + kvh * A.group + r % A.group;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) A.out[row * D + i * 32 + lane] = f32_to_bf16_rne(o[i] * inv);
-      if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-    } else {
-      const size_t row = (static_cast<size_t>(split) * A.n_tokens * A.hq) + static_cast<size_t>(u.token0 + r / A.group) * A.hq + kvh * A.group + r % A.group;
-      float* dst = A.part + row * (D + 2);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) dst[i * 32 + lane] = o[i];
-      if (lane == 0) dst[D] = m, dst[D + 1] = l;
-    }
+    ++done;
+    if (at < end) team_barrier(in_block, threads);      // the rings' places are free again
   }
 }
 
-// One warp per output row: the splits' sums on a common reference.
-template <int D>
-__global__ void __launch_bounds__(128) quant_merge_kernel(const __grid_constant__ AttendArgs A) {
-  const int lane = threadIdx.x & 31, seq = blockIdx.y;
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 5);   // (query, head) of the sequence
+// Puts the pieces of the units that reach over borders together: a warp per border and column.
+template <int D, int NT>
+__global__ void __launch_bounds__(256) quant_merge_kernel(const __grid_constant__ AttendArgs A, int32_t cols) {
+  const int lane = threadIdx.x & 31, at = blockIdx.x * 8 + (threadIdx.x >> 5), team = at / cols, col = at - team * cols;
   pdl_wait();
-  const UnitPlace u = place_of(A, seq, false);
-  if (i >= u.queries * A.hq) return;
-  const size_t row = static_cast<size_t>(u.token0) * A.hq + i, step = static_cast<size_t>(A.n_tokens) * A.hq * (D + 2);
-  const float* src = A.part + row * (D + 2);
-  float m = -INFINITY, l = 0.f, o[D / 32] = {};
-  for (int s = 0; s < A.n_splits; ++s) m = fmaxf(m, src[s * step + D]);
-  for (int s = 0; s < A.n_splits; ++s) {
-    const float ms = src[s * step + D], ls = src[s * step + D + 1];
-    if (ls == 0.f) continue;
-    const float f = weight_of(ms, m);
-    l = fmaf(ls, f, l);
+  if (team >= A.n_borders) return;
+  const Border b = A.borders[team];
+  if (col < min(8 * NT, b.n_rows - b.row0)) {
+    float m = -INFINITY, l = 0.f, o[D / 32] = {};
+    for (int i = team; i <= b.last; ++i)
+      m = fmaxf(m, reinterpret_cast<const float2*>(piece_at<D, NT>(A, i, i == team ? b.place : 0) + 8 * NT * D)[col].x);
+    for (int i = team; i <= b.last; ++i) {
+      const float* piece = piece_at<D, NT>(A, i, i == team ? b.place : 0);
+      const float2 ml = reinterpret_cast<const float2*>(piece + 8 * NT * D)[col];
+      if (ml.y == 0.f) continue;
+      const float f = weight_of(ml.x, m);
+      l = fmaf(ml.y, f, l);
+      float v[D / 32];
+      load_run<D>(piece + col * D, v, lane);
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) o[j] = fmaf(src[s * step + j * 32 + lane], f, o[j]);
+      for (int j = 0; j < D / 32; ++j) o[j] = fmaf(v[j], f, o[j]);
+    }
+    const int r = b.row0 + col, query = query_of(A, r);
+    write_row<D>(A, static_cast<size_t>(b.token0 + query) * A.hq + b.kvh * A.group + r - query * A.group, m, l, o, lane);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int j = 0; j < D / 32; ++j) A.out[row * D + j * 32 + lane] = f32_to_bf16_rne(o[j] * inv);
-  if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 bool off(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
@@ -512,24 +819,33 @@ int32_t check_sizes(const qc_quant_attend_args* a) {
   return QC_OK;
 }
 
-int splits_for(const qc_quant_attend_args* a, int row_tiles) {
-  const int64_t units = static_cast<int64_t>(a->n_seqs) * a->n_kv_heads * row_tiles;
-  int64_t pages = a->text ? a->text->max_pages : 0;
-  if (a->visual) pages += a->visual->max_pages;
-  const int64_t tiles = (pages * a->page_size + kTile - 1) / kTile;
-  int64_t n = (148 * 4 + units - 1) / units;
-  if (n > (tiles + kAttWarps - 1) / kAttWarps) n = (tiles + kAttWarps - 1) / kAttWarps;
-  return static_cast<int>(n < 1 ? 1 : n > 64 ? 64 : n);
-}
-
 int row_tile_of(const qc_quant_attend_args* a) { return a->max_queries * (a->n_q_heads / a->n_kv_heads) > 8 ? 2 : 1; }
 
+constexpr int kMostTeams = 2560;   // of one warp each; the workspace is sized for it
+
 template <int D, int NT>
-cudaError_t launch(const AttendArgs& A, cudaStream_t stream) {
-  quant_attend_kernel<D, NT><<<dim3(A.n_splits, A.hkv * A.row_tiles, A.n_seqs), kAttWarps * 32, 0, stream>>>(A);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || A.n_splits == 1) return e;
-  return launch_pdl(quant_merge_kernel<D>, dim3((A.max_queries * A.hq + 3) / 4, A.n_seqs), dim3(128), 0, stream, A);
+cudaError_t launch(AttendArgs& A, int device, int cols, cudaStream_t stream) {
+  const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 4;
+  static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
+  cudaError_t e;
+  if (device >= 64 || configured[device] < smem) {
+    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (device < 64) configured[device] = smem;
+  }
+  int sms = 0;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return e;
+  int blocks = sms * (NT == 1 ? 2 : 1);
+  if (blocks > kMostTeams / kAttWarps) blocks = kMostTeams / kAttWarps;
+  A.n_borders = blocks * kAttWarps;
+  quant_attend_kernel<D, NT><<<blocks, kAttWarps * 32, smem, stream>>>(A);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  return launch_pdl(quant_merge_kernel<D, NT>, dim3((A.n_borders * cols + 7) / 8), dim3(256), 0, stream, A, cols);
+}
+
+size_t workspace_bytes(const qc_quant_attend_args* a) {
+  return kMostTeams * sizeof(Border) + static_cast<size_t>(kMostTeams) * 2 * 8 * row_tile_of(a) * (a->head_dim + 2) * 4;
 }
 
 }  // namespace
@@ -540,9 +856,7 @@ using namespace qc;
 extern "C" int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes) {
   if (!bytes) return QC_ERR_INVALID_ARG;
   if (const int32_t bad = check_sizes(args)) return bad;
-  const int nt = row_tile_of(args), group = args->n_q_heads / args->n_kv_heads;
-  const int splits = splits_for(args, (args->max_queries * group + 8 * nt - 1) / (8 * nt));
-  *bytes = splits == 1 ? 0 : static_cast<size_t>(splits) * args->n_tokens * args->n_q_heads * (args->head_dim + 2) * 4;
+  *bytes = workspace_bytes(args);
   return QC_OK;
 }
 
@@ -555,32 +869,34 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   if (!args->seq_ids_dev && args->n_seqs > args->max_seqs) return QC_ERR_INVALID_ARG;
   if (!args->starts_dev && args->n_tokens < args->n_seqs) return QC_ERR_INVALID_ARG;
   AttendArgs A{};
-  if (const int32_t bad = check_stream(args->text, args, A.text)) return bad;
+  if (const int32_t bad = check_stream(args->text, args, A.stream[0])) return bad;
   if (args->visual)
-    if (const int32_t bad = check_stream(args->visual, args, A.visual)) return bad;
-  size_t need = 0;
-  if (const int32_t bad = qc_quant_workspace_bytes(args, &need)) return bad;
-  if (need > args->workspace_bytes || (need && !args->workspace_dev)) return QC_ERR_INVALID_ARG;
+    if (const int32_t bad = check_stream(args->visual, args, A.stream[1])) return bad;
+  if (args->workspace_bytes < workspace_bytes(args) || !args->workspace_dev) return QC_ERR_INVALID_ARG;
   if (args->n_tokens == 0) return QC_OK;
   A.has_visual = args->visual != nullptr;
   A.ids = args->seq_ids_dev, A.starts = args->starts_dev;
-  A.out = static_cast<uint16_t*>(args->out_dev), A.lse = args->lse_out_dev, A.part = static_cast<float*>(args->workspace_dev);
+  A.out = static_cast<uint16_t*>(args->out_dev), A.lse = args->lse_out_dev;
+  A.borders = static_cast<Border*>(args->workspace_dev), A.part = reinterpret_cast<float*>(A.borders + kMostTeams);
   A.status = args->status_dev;
   A.hq = args->n_q_heads, A.hkv = args->n_kv_heads, A.group = A.hq / A.hkv, A.page = args->page_size;
   A.page_shift = A.page == 16 ? 4 : A.page == 32 ? 5 : 6;
   A.n_seqs = args->n_seqs, A.max_seqs = args->max_seqs, A.n_tokens = args->n_tokens, A.max_queries = args->starts_dev ? args->max_queries : 1;
   A.causal = args->causal != 0;
+  A.inv_group = 1.f / A.group;
   const int nt = row_tile_of(args);
-  A.row_tiles = (args->max_queries * A.group + 8 * nt - 1) / (8 * nt);
-  A.n_splits = splits_for(args, A.row_tiles);
-  A.page_bytes = quant_page_bytes(A.hkv, args->head_dim, A.page);
+  const int cols = A.max_queries * A.group < 8 * nt ? A.max_queries * A.group : 8 * nt;
+  A.page_bytes = quant_page_bytes(A.hkv, args->head_dim, A.page), A.code_bytes = static_cast<int64_t>(A.hkv) * A.page * (args->head_dim / 2);
+  A.page_units = static_cast<uint32_t>(A.page_bytes / 64), A.head_units = static_cast<uint32_t>(A.page * (args->head_dim / 2) / 64);
+  if (static_cast<int64_t>(args->text->n_pages) * A.page_units > UINT32_MAX || (args->visual && static_cast<int64_t>(args->visual->n_pages) * A.page_units > UINT32_MAX))
+    return QC_ERR_UNSUPPORTED;
   const float scale = args->softmax_scale > 0.f ? args->softmax_scale : 1.0f / sqrtf(static_cast<float>(args->head_dim));
   A.scale_log2 = scale * 1.4426950408889634f;
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (args->head_dim == 128) e = nt == 1 ? launch<128, 1>(A, stream) : launch<128, 2>(A, stream);
-  else e = nt == 1 ? launch<64, 1>(A, stream) : launch<64, 2>(A, stream);
+  if (args->head_dim == 128) e = nt == 1 ? launch<128, 1>(A, device, cols, stream) : launch<128, 2>(A, device, cols, stream);
+  else e = nt == 1 ? launch<64, 1>(A, device, cols, stream) : launch<64, 2>(A, device, cols, stream);
   return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }

@@ -48,9 +48,11 @@ def fill(table, ids, lens, page, pools, k, v, device=DEV):
 def bound(queries, keys, values, scale, out, weights):
     """How far an output row may be from the one in 64 bits, element by element, and its lse; `weights`: the softmax's.
 
-    A score is s * sum q (c - 8) + mid * sum q.  Its products are exact and summed in fp32: every one of the D + 8 steps
-    is off by 2^-23 of the sum's largest magnitude at most (an adder that cuts off), as are the four roundings around it;
-    |score| is bounded with absolute values.  The exponential adds 2^-22 of itself and the rounding of its argument.  The
+    A score is s * sum q c + lo * sum q.  A query element is exact in fp16 with the row's largest in 2^14 .. 2^15
+    (half of them divided by 16 before), or off by half of the least step, 2^-25 times 16, where it is below 2^-9: by 2^-34
+    of the row's largest at most; 2^-17 where it is below 2^-9 of it is allowed for.  The products are exact and summed in fp32: every
+    one of the D + 8 steps is off by 2^-23 of the sum's largest magnitude at most (an adder that cuts off), as are the
+    four roundings around it; |score| is bounded with absolute values.  The exponential adds 2^-22 of itself and the rounding of its argument.  The
     weights p s are rounded to fp16 (2^-11) before the product with c - 8; the sums over L keys, in fp32, are off by
     2^-23 per step of what they add up; the output is rounded to bf16 (2^-8).
     """
@@ -58,8 +60,10 @@ def bound(queries, keys, values, scale, out, weights):
     e = 0.0
     for q, k in zip(queries, keys):
         if len(k["step"]):
-            part = np.abs(k["codes"] - 8) @ np.abs(q) * k["step"] + np.abs(k["lo"] + 8 * k["step"]) * np.abs(q).sum()
-            e = max(e, float(part.max()) * scale * (q.size + 12) * 2.0 ** -23)
+            part = k["codes"] @ np.abs(q) * k["step"] + np.abs(k["lo"]) * np.abs(q).sum()
+            small = np.abs(q) < 2.0 ** -9 * np.abs(q).max()
+            tiny = k["codes"] @ small.astype(float) * k["step"] * 2.0 ** -17 * np.abs(q).max()
+            e = max(e, scale * float((part * (q.size + 12) * 2.0 ** -23 + tiny).max()))
     size = np.concatenate([np.abs(v["lo"] + 8 * v["step"])[:, None] + v["step"][:, None] * np.abs(v["codes"] - 8) for v in values]) if n else np.zeros((1, out.size))
     mass = weights @ size if n else np.zeros(out.size)
     rel = 2 * e + 2.0 ** -21 + (n + 64) * 2.0 ** -23

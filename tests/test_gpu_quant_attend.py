@@ -255,7 +255,9 @@ def test_long_sequences_against_torch_in_64_bits(head_dim, heads, group, n, page
         want_lse = torch.logsumexp(logit, 0)
         w = torch.exp(logit - want_lse)
         want = w @ (vl[:, j, None] + vs[:, j, None] * vc[:, j])
-        e = ((((kc[:, j] - 8).abs() @ x.abs()) * ks[:, j] + (kl[:, j] + 8 * ks[:, j]).abs() * x.abs().sum()).max() * head_dim ** -0.5 * (head_dim + 12) * 2.0 ** -23).item()
+        small = (x.abs() < 2.0 ** -9 * x.abs().max()).double()
+        part = ((kc[:, j] @ x.abs()) * ks[:, j] + kl[:, j].abs() * x.abs().sum()) * (head_dim + 12) * 2.0 ** -23
+        e = ((part + (kc[:, j] @ small) * ks[:, j] * 2.0 ** -17 * x.abs().max()).max() * head_dim ** -0.5).item()
         mass = w @ ((vl[:, j] + 8 * vs[:, j]).abs()[:, None] + vs[:, j, None] * (vc[:, j] - 8).abs())
         rel = 2 * e + 2.0 ** -21 + (n + 64) * 2.0 ** -23
         assert ((out[0, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * rel) * mass).all()
