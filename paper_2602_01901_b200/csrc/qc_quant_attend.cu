@@ -26,7 +26,8 @@ namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
 constexpr int kAttWarps = 8;
-constexpr int kUnitCost = 3;         // what a unit costs besides its tiles, in tiles
+constexpr int kUnitCost = 2;         // what a unit costs each warp besides its tiles, in tiles
+constexpr uint32_t kLongUnit = 64;   // tiles of the average unit from which on teams have eight warps
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
 constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
 
@@ -56,7 +57,7 @@ struct AttendArgs {
   int32_t n_borders;
   float inv_group;
   uint32_t page_units, head_units;   // bytes of a page, and of a head's codes in it, / 64
-  int64_t page_bytes, code_bytes;
+  uint32_t code_units;               // bytes of a page's codes, / 64
   float scale_log2;
 };
 
@@ -99,7 +100,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t a) {
 template <int D, int NT>
 struct Rows {
   float acc[NT][D / 16][4];  // times 2^-24 (even elements) and 2^-20 (odd ones)
-  float ref[NT][2];          // what a column's scores (before the scale) are relative to; 0 before the first key that it sees
+  float ref[NT][2];          // what a column's scores are relative to; 0 before the first key that it sees
   float l[NT][2], z[NT][2];  // this lane's part of sum p and sum p mid
   uint32_t step;             // bits of the power of two that the weights were divided by
   uint32_t seen;             // columns that have seen a key, a bit per (nt, x)
@@ -110,7 +111,7 @@ template <int D, int NT>
 struct Query {
   uint32_t b[NT][D / 16][2];   // operands of the score products: lower codes' elements, and a 16th of the upper ones'
   float sum[NT][2];            // sum of the elements times 2^-24, for the columns 2 t and 2 t + 1
-  float scale[NT][2];          // softmax scale * log2 e * the powers of two that were taken out
+  float scale;                 // softmax scale * log2 e * the powers of two that were taken out
 };
 
 // Row r of a unit is query r / group of the sequence, head r % group of the KV head.
@@ -120,47 +121,57 @@ template <int D, int NT>
 __device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A, const StreamArgs& S, int64_t token0, int head0, int row0,
                                            int n_rows, int lane) {
   const int g = lane >> 2, t = lane & 3;
+  uint4 raw[NT][D / 32];
+  uint32_t top = 0;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = row0 + nt * 8 + g, query = query_of(A, r);
     const bool on = r < n_rows;
     const uint16_t* q = S.q + (token0 + query) * S.q_stride + static_cast<int64_t>(head0 + r - query * A.group) * D + t * (D / 4);
-    uint4 raw[D / 32];
-    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      raw[i] = on ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
-      top = max_bf16x2(top, max_bf16x2(max_bf16x2(raw[i].x & 0x7fff7fffu, raw[i].y & 0x7fff7fffu), max_bf16x2(raw[i].z & 0x7fff7fffu, raw[i].w & 0x7fff7fffu)));
+      const uint4 x = raw[nt][i] = on ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
+      top = max_bf16x2(top, max_bf16x2(max_bf16x2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max_bf16x2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
     }
-    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int top_exp = static_cast<int>(max(top & 0xffffu, top >> 16) >> 7);   // of the row's largest element
-    // 2^e with that element times 2^-e in [2^14, 2^15); a zero or subnormal one counts as 2^-90, the largest as 2^100
-    const int e = min(max(top_exp - 127, -90), 100) - 14;
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -104 <= e <= 86
+  }
+  // (of numbers that are not negative, the larger one has the larger bits)
+  const int top_exp = static_cast<int>(__reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16)) >> 7);
+  // 2^e with the unit's largest element times 2^-e in [2^14, 2^15); below 2^-90 it counts as that, from 2^101 on it has no scores
+  const int e = min(max(top_exp - 127, -90), 100) - 14;
+  const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -104 <= e <= 86
+  Q.scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + 24 + e) << 23);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
     float sum = 0.f;
+    bool large = false;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       float f[8];
-      bf16x8_to_f32(raw[i], f);
+      bf16x8_to_f32(raw[nt][i], f);
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] *= down;
-      sum += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+      const float s = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+      sum += s;
       Q.b[nt][2 * i][0] = pack_f16x2(f[0], f[4]);
       Q.b[nt][2 * i][1] = pack_f16x2(f[1] * 0.0625f, f[5] * 0.0625f);
       Q.b[nt][2 * i + 1][0] = pack_f16x2(f[2], f[6]);
       Q.b[nt][2 * i + 1][1] = pack_f16x2(f[3] * 0.0625f, f[7] * 0.0625f);
     }
+    if (top_exp > 127 + 100) {      // rows with such an element have no scores, the unit's other rows have theirs
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        float f[8];
+        bf16x8_to_f32(raw[nt][i], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) large |= !(fabsf(f[j]) < 2.535301200456459e30f);   // 2^101
+      }
+      if (large) sum = NAN;
+    }
+    sum *= 5.9604644775390625e-8f;      // 2^-24
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-    sum *= 5.9604644775390625e-8f;      // 2^-24
-    if (top_exp > 127 + 100) sum = NAN;      // (a row with an element of 2^101 or more, or an infinite one, has no scores)
-    const float scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + 24 + e) << 23);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      Q.sum[nt][x] = __shfl_sync(0xffffffffu, sum, t * 8 + 4 * x);
-      Q.scale[nt][x] = __shfl_sync(0xffffffffu, scale, t * 8 + 4 * x);
-    }
+    Q.sum[nt][0] = __shfl_sync(0xffffffffu, sum, t * 8);
+    Q.sum[nt][1] = __shfl_sync(0xffffffffu, sum, t * 8 + 4);
   }
 }
 
@@ -177,48 +188,50 @@ struct Ring {
   static constexpr int kBytes = 3 * kCodes + 2 * kParams;
 };
 
-// Where the tile after the one that is worked on comes from.
-struct Fetch {
-  uint32_t at[kTile / 16];   // its blocks' codes in the pool, in units of 64 bytes
-  uint32_t on;               // blocks that are there, a bit each
-  int32_t id;                // lane 4 b + i: page id of block b (of the tile whose ids were asked for last)
-  uint32_t id_on;
+// A run: adjacent tiles of one stream, kBatch of which a lane's worth of page ids covers.
+constexpr int kBatch = 32 / (kTile / 16);
+
+// Where the blocks of a batch of tiles are, one per lane, in units of 64 bytes: a block's parameters are one unit.
+struct Batch {
+  uint32_t codes, params;
+  bool there;
 };
 
-// Asks for the page ids of a tile: lane 4 b + i has block b's (lanes from 16 on the same again).
-__device__ __forceinline__ void fetch_ids(Fetch& F, const AttendArgs& A, const StreamArgs& S, const int32_t* table, int key0, int len, int lane) {
-  const int key = key0 + ((lane >> 2) & 3) * 16;
-  F.id_on = key < len;
-  F.id = F.id_on ? __ldg(table + (key >> A.page_shift)) : 0;
+__device__ __forceinline__ int32_t ask_ids(const AttendArgs& A, const int32_t* table, int tile, int len, int lane) {
+  const int key = tile * kTile + lane * 16;
+  return key < len ? __ldg(table + (key >> A.page_shift)) : -1;
 }
 
-// Requests the codes of a tile of K and the parameters of K and V.
 template <int D>
-__device__ __forceinline__ void fetch_keys(Fetch& F, const AttendArgs& A, const StreamArgs& S, int kvh, int key0, uint32_t codes, uint32_t params, int lane) {
-  const bool bad = F.id_on && static_cast<uint32_t>(F.id) >= static_cast<uint32_t>(S.n_pages);   // a page that is none is not followed
-  if (bad && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_BAD_PAGE));
-  const uint32_t there = __ballot_sync(0xffffffffu, F.id_on && !bad);
-  F.on = (there & 1u) | (there >> 3 & 2u) | (there >> 6 & 4u) | (there >> 9 & 8u);
-  const int32_t id = F.id_on && !bad ? F.id : 0;      // what is not there is fetched from page 0 and never looked at
-  const int mask = A.page - 1;
+__device__ __forceinline__ Batch batch_of(const AttendArgs& A, const StreamArgs& S, int32_t id, int kvh, int tile, int len, int lane) {
+  const int key = tile * kTile + lane * 16, block = (key & (A.page - 1)) >> 4;
+  Batch b;
+  b.there = static_cast<uint32_t>(id) < static_cast<uint32_t>(S.n_pages);
+  if (!b.there && key < len && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_BAD_PAGE));   // a page that is none is not followed
+  const uint32_t page = (b.there ? static_cast<uint32_t>(id) : 0u) * A.page_units;   // what is not there is fetched from page 0 and never looked at
+  b.codes = page + kvh * A.head_units + block * (D / 8);
+  b.params = page + A.code_units + ((kvh * A.page) >> 4) + block;
+  return b;
+}
+
+// Requests the codes of a tile of K and the parameters of K and V; `at` (0, 4, ..): the tile's blocks in the batch.
+template <int D>
+__device__ __forceinline__ void fetch_keys(const StreamArgs& S, const Batch& batch, int at, uint32_t codes, uint32_t params, int lane) {
 #pragma unroll
   for (int b = 0; b < kTile / 16; ++b) {
-    const uint32_t page = static_cast<uint32_t>(__shfl_sync(0xffffffffu, id, 4 * b));
-    F.at[b] = page * A.page_units + kvh * A.head_units + ((key0 + 16 * b) & mask) / 16 * (D / 8);
-    const uint8_t* src = S.k_pool + static_cast<uint64_t>(F.at[b]) * 64 + lane * 16;
+    const uint8_t* src = S.k_pool + static_cast<uint64_t>(__shfl_sync(0xffffffffu, batch.codes, at + b)) * 64 + lane * 16;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) cp_async_16(codes + b * (8 * D) + i * 512 + lane * 16, src + i * 512);
   }
-  const int in_page = (key0 + ((lane >> 2) & 3) * 16) & mask;
-  cp_async_16(params + lane * 16, (lane < 16 ? S.k_pool : S.v_pool) + static_cast<uint64_t>(static_cast<uint32_t>(id)) * A.page_bytes + A.code_bytes +
-                                      static_cast<uint32_t>((kvh * A.page + in_page) * 4 + (lane & 3) * 16));
+  const uint32_t p = __shfl_sync(0xffffffffu, batch.params, at + (lane >> 2 & 3));
+  cp_async_16(params + lane * 16, (lane < 16 ? S.k_pool : S.v_pool) + static_cast<uint64_t>(p) * 64 + (lane & 3) * 16);
 }
 
 template <int D>
-__device__ __forceinline__ void fetch_values(const Fetch& F, const StreamArgs& S, uint32_t codes, int lane) {
+__device__ __forceinline__ void fetch_values(const StreamArgs& S, const Batch& batch, int at, uint32_t codes, int lane) {
 #pragma unroll
   for (int b = 0; b < kTile / 16; ++b) {
-    const uint8_t* src = S.v_pool + static_cast<uint64_t>(F.at[b]) * 64 + lane * 16;
+    const uint8_t* src = S.v_pool + static_cast<uint64_t>(__shfl_sync(0xffffffffu, batch.codes, at + b)) * 64 + lane * 16;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) cp_async_16(codes + b * (8 * D) + i * 512 + lane * 16, src + i * 512);
   }
@@ -264,12 +277,12 @@ __device__ __forceinline__ float step_of(uint32_t params) {
 }
 
 // What the parameters of a tile's rows say, each worked out by one lane: lane l has the rows 4 l .. 4 l + 3 of 128, K's and then
-// V's.  (s, lo) for K, (s, lo + 8 s) for V; those of V rows that are not there may be whatever was there before
+// V's.  (s, lo) times the scale for K, (s, lo + 8 s) for V; those of V rows that are not there may be whatever was there before
 // and count as 0.
 struct RowValues {
   float2 v[4];
 };
-__device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, uint32_t on, int left, bool masked, int lane) {
+__device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, float scale, uint32_t on, int left, bool masked, int lane) {
   const uint4 raw = lds128(params + lane * 16);
   const uint32_t p[4] = {raw.x, raw.y, raw.z, raw.w};
   const bool is_v = lane >= 16;
@@ -278,10 +291,11 @@ __device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, uint32_t
   for (int i = 0; i < 4; ++i) {
     float s = step_of(p[i]);
     const float lo = __uint_as_float(p[i] << 16);
-    float m = is_v ? fmaf(8.f, s, lo) : lo;
+    const float f = is_v ? 1.f : scale;
+    float m = is_v ? fmaf(8.f, s, lo) : lo * f;
     if (masked && is_v && (!(on >> (lane >> 2 & 3) & 1u) || (lane & 15) * 4 + i >= left)) s = m = 0.f;
     top = fmaxf(top, s);
-    r.v[i] = make_float2(s, m);
+    r.v[i] = make_float2(s * f, m);
   }
   return is_v ? top : 0.f;
 }
@@ -350,7 +364,7 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
         h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 16));
         const bool known = R.seen & bit, any = h > -INFINITY;
         const float delta = (known ? h > 0.f : any) ? h : 0.f;
-        const float corr = known ? exp2f(-delta * Q.scale[nt][x]) : 1.f;      // (nothing so far: nothing to put on another reference)
+        const float corr = known ? exp2f(-delta) : 1.f;      // (nothing so far: nothing to put on another reference)
         R.ref[nt][x] += delta;
         if (any) R.seen |= bit;
         all &= (R.seen & bit) != 0;
@@ -374,7 +388,7 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
       float p[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        p[x] = ex2_approx(c[b][nt][x] * Q.scale[nt][x & 1]);
+        p[x] = ex2_approx(c[b][nt][x]);
         R.l[nt][x & 1] += p[x];
       }
       if (!masked) {
@@ -433,11 +447,15 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
 // ---- the batch's work as one row -------------------------------------------------------------------------
 //
 // Sequence after sequence, unit after unit (KV head, then rows of queries), tile after tile (the visual stream's, then the
-// text's).  A unit costs its tiles and kUnitCost more.  The row is cut into equal ranges, one per team of 1, 2, 4 or 8 warps, so that
-// the teams end together whatever the lengths are; a team takes a unit's tiles in turn, warp by warp.  A unit inside one
-// range is finished there; of one that reaches over a border each team leaves its sums, and the launch that follows puts
-// them together, in the order of the teams.  Where units are short next to that launch, or next to a range, a team
-// takes those that begin in its range whole, and nothing is left to put together.
+// text's).  The row is cut into ranges of equal cost, one per team of 1, 2, 4 or 8 warps, so that the teams end together
+// whatever the lengths are; the warps of a team share out a unit's tiles.  A unit costs its tiles and kUnitCost more for
+// every warp of the team.  A unit inside one range is finished there; of one that reaches over a border each team leaves
+// its sums, and the launch that follows puts them together, in the order of the teams.  Where units are short next to
+// that launch, or next to a range, a team takes those that begin in its range whole, and nothing is left to put together.
+//
+// Teams of one warp are the even ones: with teams of eight, a range of many short units costs more than one of a long unit
+// (16 sequences of 1 to 5 000 tokens, 32 heads: XX us with eight, YY with one).  Eight where units are long (fewer sums to leave
+// behind), and as many as there are warps for where the whole batch is small.
 
 struct Place {       // one sequence
   int64_t token0;    // its first query
@@ -526,59 +544,65 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
   constexpr int kRow = D + 4;            // of a column's sums in shared memory
   static_assert(8 * NT * kRow * 4 <= R_::kBytes, "a warp's sums take its ring's place");
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint32_t scan[kAttWarps];
+  __shared__ uint2 scan[kAttWarps];
   __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
-  __shared__ uint32_t longest_, units_;
-  uint32_t* before = reinterpret_cast<uint32_t*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] what the sequences before cost
+  __shared__ uint32_t longest_;
+  uint2* before = reinterpret_cast<uint2*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] tiles and units of the sequences before
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   pdl_launch_dependents();
-  if (threadIdx.x == 0) before[0] = longest_ = units_ = 0;
+  if (threadIdx.x == 0) before[0] = make_uint2(0, 0), longest_ = 0;
   __syncthreads();
   uint64_t total = 0;
+  uint32_t units_all = 0;
   for (int i0 = 0; i0 < A.n_seqs; i0 += kAttWarps * 32) {
     const int i = i0 + threadIdx.x;
     uint64_t mine = 0;
+    uint32_t units = 0;
     if (i < A.n_seqs) {
       const Place u = place_of(A, i, blockIdx.x == 0);
-      const uint32_t units = A.hkv * ((u.n_rows + 8 * NT - 1) / (8 * NT));
-      mine = static_cast<uint64_t>(u.tiles + kUnitCost) * units;
-      if (units) atomicMax(&longest_, static_cast<uint32_t>(u.tiles)), atomicAdd(&units_, units);
+      units = A.hkv * ((u.n_rows + 8 * NT - 1) / (8 * NT));
+      mine = static_cast<uint64_t>(u.tiles) * units;
+      if (units) atomicMax(&longest_, static_cast<uint32_t>(u.tiles));
     }
     const bool big = mine > (1u << 22);
-    uint32_t x = big ? 0u : static_cast<uint32_t>(mine);
+    uint32_t x = big ? 0u : static_cast<uint32_t>(mine), n = units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
+      const uint32_t y = __shfl_up_sync(0xffffffffu, x, o), k = __shfl_up_sync(0xffffffffu, n, o);
+      if (lane >= o) x += y, n += k;
     }
-    if (lane == 31) scan[warp] = x;
+    if (lane == 31) scan[warp] = make_uint2(x, n);
     const bool any_big = __syncthreads_or(big);
-    uint32_t base = 0, sum = 0;
+    uint2 base = make_uint2(0, 0), sum = make_uint2(0, 0);
 #pragma unroll
     for (int w = 0; w < kAttWarps; ++w) {
-      if (w < warp) base += scan[w];
-      sum += scan[w];
+      if (w < warp) base.x += scan[w].x, base.y += scan[w].y;
+      sum.x += scan[w].x, sum.y += scan[w].y;
     }
-    if (i < A.n_seqs) before[i + 1] = static_cast<uint32_t>(total) + base + x;
-    total += sum;
-    if (any_big || total > (1u << 30)) {      // a batch of more than 2^36 rows
+    if (i < A.n_seqs) before[i + 1] = make_uint2(static_cast<uint32_t>(total) + base.x + x, units_all + base.y + n);
+    total += sum.x;
+    units_all += sum.y;
+    if (any_big || total > (1u << 29)) {      // a batch of more than 2^35 rows
       if (blockIdx.x == 0 && threadIdx.x == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
       total = 0;
       break;
     }
     __syncthreads();
   }
-  const uint32_t cost = static_cast<uint32_t>(total), units = units_, longest = longest_;
-  // warps of a team: no more than the average unit has tiles, unless there are warps for more
-  const uint32_t n_warps = gridDim.x * kAttWarps, tiles_all = cost - units * kUnitCost;
+  const uint32_t tiles_all = static_cast<uint32_t>(total), units = total ? units_all : 0, longest = longest_;
+  const uint32_t n_warps = gridDim.x * kAttWarps;
   uint32_t team_warps = 1;
-  while (team_warps < kAttWarps && (units * team_warps * 2 <= tiles_all || units * team_warps * 2 <= n_warps)) team_warps *= 2;
+  if (tiles_all >= units * kLongUnit) team_warps = kAttWarps;
+  else
+    while (team_warps < kAttWarps && units * team_warps * 2 <= n_warps) team_warps *= 2;
   const uint32_t n_teams = n_warps / team_warps;
   const int threads = team_warps * 32, in_block = warp / team_warps, member = warp % team_warps, team0 = in_block * team_warps;
   const uint32_t team = blockIdx.x * (kAttWarps / team_warps) + in_block;
+  const uint32_t more = kUnitCost * team_warps, cost = tiles_all + units * more;
+  const auto before_cost = [&](int s) { return before[s].x + before[s].y * more; };
   uint32_t per = (cost + n_teams - 1) / n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per / 8);
-  if (!whole_units) per = max(per, team_warps + kUnitCost);
+  if (!whole_units) per = max(per, team_warps + more);
   if (member == 0 && lane == 0) {
     const Border none{};
     A.borders[team] = none;
@@ -595,7 +619,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
     int lo = 0, hi = A.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (before[mid] <= at) lo = mid;
+      if (before_cost(mid) <= at) lo = mid;
       else hi = mid - 1;
     }
     seq = lo;
@@ -603,19 +627,20 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
   int done = 0;      // units so far
   while (at < end) {
-    while (before[seq + 1] <= at) ++seq;
+    while (before_cost(seq + 1) <= at) ++seq;
     const Place u = place_of(A, seq, false);
-    const int row_tiles = (u.n_rows + 8 * NT - 1) / (8 * NT), unit_cost = u.tiles + kUnitCost;
-    int unit = (at - before[seq]) / unit_cost, first = 0, last = u.tiles;
-    uint32_t unit_at = before[seq] + unit * unit_cost;
+    const int row_tiles = (u.n_rows + 8 * NT - 1) / (8 * NT), unit_cost = u.tiles + more;
+    const uint32_t seq_at = before_cost(seq);
+    int unit = (at - seq_at) / unit_cost, first = 0, last = u.tiles;
+    uint32_t unit_at = seq_at + unit * unit_cost;
     if (whole_units) {
       if (unit_at < at) {      // it begins before the range: the next one
         at = unit_at + unit_cost;
         continue;
       }
     } else {
-      first = max(0, static_cast<int>(at - unit_at) - kUnitCost);
-      last = min(u.tiles, static_cast<int>(end - unit_at) - kUnitCost);
+      first = max(0, static_cast<int>(at - unit_at) - static_cast<int>(more));
+      last = min(u.tiles, static_cast<int>(end - unit_at) - static_cast<int>(more));
     }
     at = unit_at + unit_cost;
     if (first >= last) continue;
@@ -633,83 +658,72 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
     R.seen = 0;
     R.all_seen = false;
 
-    Query<D, NT> Q;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) Q.scale[nt][0] = Q.scale[nt][1] = 0.f;
-    int stream = -1;           // of the queries at hand
-    Fetch F;
-    // a tile's stream, and its first key
-    const auto stream_of = [&](int tile) { return tile < u.tiles_v ? 1 : 0; };
-    const auto key_of = [&](int tile) { return (tile < u.tiles_v ? tile : tile - u.tiles_v) * kTile; };
-    const auto ids = [&](int tile) {
-      if (tile >= last) return;
-      const StreamArgs& S = A.stream[stream_of(tile)];
-      fetch_ids(F, A, S, S.pages + static_cast<size_t>(u.row) * S.max_pages, key_of(tile), tile < u.tiles_v ? u.len[1] : u.len[0], lane);
-    };
-    const auto keys = [&](int tile, int slot, int par) {
-      if (tile < last) fetch_keys<D>(F, A, A.stream[stream_of(tile)], kvh, key_of(tile), ring + slot * R_::kCodes, ring + 3 * R_::kCodes + par * R_::kParams, lane);
+    // this warp's tiles of the unit, adjacent ones: a run in each stream
+    const int mine0 = first + (last - first) * member / static_cast<int>(team_warps), mine1 = first + (last - first) * (member + 1) / static_cast<int>(team_warps);
+#pragma unroll 1
+    for (int now = 1; now >= 0; --now) {
+      const int shift = now ? 0 : u.tiles_v;      // the stream's first tile in the unit
+      const int run = max(mine0, shift) - shift, stop = (now ? min(mine1, u.tiles_v) : mine1) - shift;
+      if (run >= stop) continue;
+      const StreamArgs& S = A.stream[now];
+      const int len = now ? u.len[1] : u.len[0], back = now || !A.causal ? 0 : u.queries - 1;
+      const int32_t* table = S.pages + static_cast<size_t>(u.row) * S.max_pages;
+      Batch batch = batch_of<D>(A, S, ask_ids(A, table, run, len, lane), kvh, run, len, lane);
+      int at_tile = run;       // the batch's first tile
+      const uint32_t params = ring + 3 * R_::kCodes;
+      fetch_keys<D>(S, batch, 0, ring, params, lane);
       cp_async_commit_group();
-    };
-    const auto values = [&](int tile, int slot) {
-      if (tile < last) fetch_values<D>(F, A.stream[stream_of(tile)], ring + slot * R_::kCodes, lane);
+      fetch_values<D>(S, batch, 0, ring + R_::kCodes, lane);
       cp_async_commit_group();
-    };
-    int tile = first + member, slot = 0, par = 0;
-    const int stride = team_warps;
-    ids(tile);
-    keys(tile, 0, 0);
-    uint32_t on = F.on;
-    values(tile, 1);
-    ids(tile + stride);
-    for (; tile < last; tile += stride) {
-      const int now = stream_of(tile), after = tile + stride;
-      const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
-      const uint32_t on_now = on;
-      keys(after, slot2, par ^ 1);      // the place of the V before
-      on = F.on;
-      if (stream != now) {
-        // (scores are in the units of the stream's queries, and so is what they are relative to)
-        float was[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) was[nt][0] = Q.scale[nt][0], was[nt][1] = Q.scale[nt][1];
-        load_query<D, NT>(Q, A, A.stream[now], u.token0, kvh * A.group, row0, u.n_rows, lane);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-            if (stream >= 0 && R.ref[nt][x] != 0.f) R.ref[nt][x] *= was[nt][x] / Q.scale[nt][x];
-        stream = now;
+      int32_t ids = ask_ids(A, table, run + kBatch, len, lane);      // of the next batch
+      uint32_t there = __ballot_sync(0xffffffffu, batch.there);
+      Query<D, NT> Q;
+      load_query<D, NT>(Q, A, S, u.token0, kvh * A.group, row0, u.n_rows, lane);
+      int slot = 0, par = 0;
+      for (int tile = run; tile < stop; ++tile) {
+        const uint32_t on = there >> ((tile - at_tile) * 4) & 15u;
+        const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
+        const bool more_tiles = tile + 1 < stop;
+        if (tile + 1 - at_tile == kBatch) {
+          at_tile += kBatch;
+          batch = batch_of<D>(A, S, ids, kvh, at_tile, len, lane);
+          there = __ballot_sync(0xffffffffu, batch.there);
+          ids = ask_ids(A, table, at_tile + kBatch, len, lane);
+        }
+        const int at_next = (tile + 1 - at_tile) * 4;
+        if (more_tiles) fetch_keys<D>(S, batch, at_next, ring + slot2 * R_::kCodes, params + (par ^ 1) * R_::kParams, lane);      // the place of the V before
+        cp_async_commit_group();
+        const int left = len - tile * kTile;
+        const bool masked = left - back < kTile || on != 15u;
+        const uint32_t scratch = ring + slot * R_::kCodes;      // K's place, once its codes are read
+        float c[kTile / 16][NT][4];
+        uint32_t w[kTile / 16][NT][2];
+        cp_async_wait_group<2>();
+        __syncwarp();
+        score_tile<D, NT>(c, Q, scratch, lane);
+        __syncwarp();
+        float top;
+        {
+          RowValues rows;
+          top = rows_of(rows, params + par * R_::kParams, Q.scale, on, left, masked, lane);
+          sts_f4(scratch + lane * 32, rows.v[0], rows.v[1]);
+          sts_f4(scratch + lane * 32 + 16, rows.v[2], rows.v[3]);
+        }
+        __syncwarp();
+        weigh_tile<D, NT>(R, c, w, Q, scratch, top, on, A, left, row0, back, masked, lane);
+        __syncwarp();
+        if (more_tiles) fetch_values<D>(S, batch, at_next, scratch, lane);
+        cp_async_commit_group();
+        cp_async_wait_group<2>();
+        __syncwarp();
+        add_values<D, NT>(R, w, ring + slot1 * R_::kCodes, lane);
+        __syncwarp();
+        slot = slot2;
+        par ^= 1;
       }
-      const int left = (now ? u.len[1] : u.len[0]) - key_of(tile), back = now || !A.causal ? 0 : u.queries - 1;
-      const bool masked = left - back < kTile || on_now != 15u;
-      const uint32_t scratch = ring + slot * R_::kCodes;      // K's place, once its codes are read
-      float c[kTile / 16][NT][4];
-      uint32_t w[kTile / 16][NT][2];
-      cp_async_wait_group<2>();
+      cp_async_wait_all();
       __syncwarp();
-      score_tile<D, NT>(c, Q, scratch, lane);
-      __syncwarp();
-      float top;
-      {
-        RowValues rows;
-        top = rows_of(rows, ring + 3 * R_::kCodes + par * R_::kParams, on_now, left, masked, lane);
-        sts_f4(scratch + lane * 32, rows.v[0], rows.v[1]);
-        sts_f4(scratch + lane * 32 + 16, rows.v[2], rows.v[3]);
-      }
-      __syncwarp();
-      weigh_tile<D, NT>(R, c, w, Q, scratch, top, on_now, A, left, row0, back, masked, lane);
-      __syncwarp();
-      values(after, slot);
-      ids(after + stride);
-      cp_async_wait_group<2>();
-      __syncwarp();
-      add_values<D, NT>(R, w, ring + slot1 * R_::kCodes, lane);
-      __syncwarp();
-      slot = slot2;
-      par ^= 1;
     }
-    cp_async_wait_all();
-    __syncwarp();
     // the team's sums meet in shared memory
     const float unit_step = __uint_as_float(R.step) * (1.f / 32768.f);
     constexpr float kEven = 16777216.f, kOdd = 1048576.f;
@@ -722,7 +736,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o), z += __shfl_xor_sync(0xffffffffu, z, o);
         const int col = nt * 8 + 2 * t + x;
-        if (g == 0) sm_m[warp][col] = R.seen >> (2 * nt + x) & 1u ? R.ref[nt][x] * Q.scale[nt][x] : -INFINITY, sm_l[warp][col] = l;
+        if (g == 0) sm_m[warp][col] = R.seen >> (2 * nt + x) & 1u ? R.ref[nt][x] : -INFINITY, sm_l[warp][col] = l;
         if (row0 + col < u.n_rows) {
           float* dst = mine + col * kRow + g * (D / 8);
 #pragma unroll
@@ -735,10 +749,10 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
     const int n_here = min(8 * NT, u.n_rows - row0);
     const bool whole = first == 0 && last == u.tiles;
     float* piece = piece_at<D, NT>(A, team, done == 0 ? 0 : 1);
-    for (int col = member; col < n_here; col += stride) {
+    for (int col = member; col < n_here; col += static_cast<int>(team_warps)) {
       float m = -INFINITY, l = 0.f, o[D / 32] = {};
-      for (int w = team0; w < team0 + stride; ++w) m = fmaxf(m, sm_m[w][col]);
-      for (int w = team0; w < team0 + stride; ++w) {
+      for (int w = team0; w < team0 + static_cast<int>(team_warps); ++w) m = fmaxf(m, sm_m[w][col]);
+      for (int w = team0; w < team0 + static_cast<int>(team_warps); ++w) {
         if (sm_l[w][col] == 0.f) continue;
         const float f = weight_of(sm_m[w][col], m);
         l = fmaf(sm_l[w][col], f, l);
@@ -801,7 +815,7 @@ int32_t check_stream(const qc_quant_stream* s, const qc_quant_attend_args* a, St
   if (!s->q_dev || !s->k_pool_dev || !s->v_pool_dev || !s->pages_dev || !s->lens_dev) return QC_ERR_INVALID_ARG;
   if (off(s->q_dev, 16) || off(s->k_pool_dev, 16) || off(s->v_pool_dev, 16) || off(s->pages_dev, 4) || off(s->lens_dev, 4)) return QC_ERR_INVALID_ARG;
   if (s->q_stride < 0 || s->q_stride % 8 || s->max_pages < 1 || s->n_pages < 1) return QC_ERR_INVALID_ARG;
-  if (static_cast<int64_t>(s->max_pages) * a->page_size > INT32_MAX - kTile || static_cast<int64_t>(s->n_pages) * a->page_size > INT32_MAX) return QC_ERR_UNSUPPORTED;
+  if (static_cast<int64_t>(s->max_pages) * a->page_size > INT32_MAX - 4096 || static_cast<int64_t>(s->n_pages) * a->page_size > INT32_MAX) return QC_ERR_UNSUPPORTED;
   d.q = static_cast<const uint16_t*>(s->q_dev), d.q_stride = s->q_stride;
   d.k_pool = static_cast<const uint8_t*>(s->k_pool_dev), d.v_pool = static_cast<const uint8_t*>(s->v_pool_dev);
   d.pages = s->pages_dev, d.lens = s->lens_dev, d.max_pages = s->max_pages, d.n_pages = s->n_pages;
@@ -825,7 +839,7 @@ constexpr int kMostTeams = 2560;   // of one warp each; the workspace is sized f
 
 template <int D, int NT>
 cudaError_t launch(AttendArgs& A, int device, int cols, cudaStream_t stream) {
-  const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 4;
+  const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
   static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
   cudaError_t e;
   if (device >= 64 || configured[device] < smem) {
@@ -886,8 +900,8 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   A.inv_group = 1.f / A.group;
   const int nt = row_tile_of(args);
   const int cols = A.max_queries * A.group < 8 * nt ? A.max_queries * A.group : 8 * nt;
-  A.page_bytes = quant_page_bytes(A.hkv, args->head_dim, A.page), A.code_bytes = static_cast<int64_t>(A.hkv) * A.page * (args->head_dim / 2);
-  A.page_units = static_cast<uint32_t>(A.page_bytes / 64), A.head_units = static_cast<uint32_t>(A.page * (args->head_dim / 2) / 64);
+  A.head_units = static_cast<uint32_t>(A.page * (args->head_dim / 2) / 64), A.code_units = A.hkv * A.head_units;
+  A.page_units = static_cast<uint32_t>(quant_page_bytes(A.hkv, args->head_dim, A.page) / 64);
   if (static_cast<int64_t>(args->text->n_pages) * A.page_units > UINT32_MAX || (args->visual && static_cast<int64_t>(args->visual->n_pages) * A.page_units > UINT32_MAX))
     return QC_ERR_UNSUPPORTED;
   const float scale = args->softmax_scale > 0.f ? args->softmax_scale : 1.0f / sqrtf(static_cast<float>(args->head_dim));
