@@ -465,8 +465,8 @@ typedef struct qc_quant_attend_args {
   float softmax_scale;           /* 0 => 1/sqrt(head_dim) */
   const int32_t* seq_ids_dev;    /* [n_seqs] table row of each sequence; null: i */
   const int32_t* starts_dev;     /* [n_seqs + 1] query tokens of each sequence, as qc_table_extend numbers them; null: one each */
-  const qc_quant_stream* text;
-  const qc_quant_stream* visual; /* null: one stream */
+  qc_quant_stream text;
+  qc_quant_stream visual;        /* all null: one stream */
   void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim] */
   float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
   void* workspace_dev;           /* qc_quant_workspace_bytes; need not be cleared; one call at a time */
@@ -477,7 +477,7 @@ typedef struct qc_quant_attend_args {
 int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes);
 
 /* Attention of each sequence's query tokens over its cached rows: one softmax over the visual stream's keys scored by
- * visual->q_dev and the text stream's keys scored by text->q_dev (an ordinary layer, VLA_EQ8: the same queries twice;
+ * visual.q_dev and the text stream's keys scored by text.q_dev (an ordinary layer, VLA_EQ8: the same queries twice;
  * VLA_QC: the Q Cache on the leader's visual K; GLA: the Q Cache on both of the leader's).  V is what the pools hold.
  * A query that sees no key gets 0 and lse minus infinity.  Rows of out that belong to no listed sequence are left as
  * they are, and so are those of a sequence whose row or query numbers are out of range (QC_ERR_INVALID_ARG in the status

@@ -19,13 +19,14 @@
 #include "qc_quant.cuh"
 #include "qc_quant.h"
 
-#include <cuda_fp16.h>
+#include <atomic>
+#include <chrono>
 
 namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kAttWarps = 8;
+constexpr int kAttWarps = 4;
 constexpr int kUnitCost = 2;         // what a unit costs each warp besides its tiles, in tiles
 constexpr uint32_t kLongUnit = 64;   // tiles of the average unit from which on teams have eight warps
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
@@ -41,8 +42,6 @@ struct StreamArgs {
   int32_t max_pages, n_pages;
 };
 
-struct Border;
-
 struct AttendArgs {
   StreamArgs stream[2];   // text, visual
   const int32_t* ids;
@@ -50,11 +49,11 @@ struct AttendArgs {
   uint16_t* out;
   float* lse;
   float* part;          // [teams][2][8 * NT * (D + 2)] pieces of units that reach over a border
-  Border* borders;      // [teams]
+  unsigned long long* flags;   // [teams][2] a piece is there: holds `nonce`
+  unsigned long long nonce;    // another one in every call
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, max_seqs, n_tokens, max_queries, causal, has_visual;
-  int32_t n_borders;
   float inv_group;
   uint32_t page_units, head_units;   // bytes of a page, and of a head's codes in it, / 64
   uint32_t code_units;               // bytes of a page's codes, / 64
@@ -243,29 +242,33 @@ __device__ __forceinline__ void fetch_values(const StreamArgs& S, const Batch& b
 // and its odd one (2, 3), times 2^-24.
 template <int D, int NT>
 __device__ __forceinline__ void score_tile(float (&c)[kTile / 16][NT][4], const Query<D, NT>& Q, uint32_t codes, int lane) {
+  constexpr int kPair = 2;      // blocks side by side: each one's products wait for one another
 #pragma unroll
-  for (int b = 0; b < kTile / 16; ++b) {
-    uint32_t even[D / 32], odd[D / 32];
-    const uint4 k0 = lds128(codes + b * (8 * D) + lane * 16);
-    if constexpr (D == 128) {
-      const uint4 k1 = lds128(codes + b * (8 * D) + 512 + lane * 16);
-      even[0] = k0.x, even[1] = k0.y, even[2] = k0.z, even[3] = k0.w;
-      odd[0] = k1.x, odd[1] = k1.y, odd[2] = k1.z, odd[3] = k1.w;
-    } else {
-      even[0] = k0.x, even[1] = k0.y, odd[0] = k0.z, odd[1] = k0.w;
+  for (int b0 = 0; b0 < kTile / 16; b0 += kPair) {
+    uint32_t x[kPair][D / 16];      // the words of the even token, then of the odd one
+#pragma unroll
+    for (int b = 0; b < kPair; ++b) {
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint4 k = lds128(codes + (b0 + b) * (8 * D) + i * 512 + lane * 16);
+        x[b][4 * i] = k.x, x[b][4 * i + 1] = k.y, x[b][4 * i + 2] = k.z, x[b][4 * i + 3] = k.w;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) c[b0 + b][nt][0] = c[b0 + b][nt][1] = c[b0 + b][nt][2] = c[b0 + b][nt][3] = 0.f;
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) c[b][nt][0] = c[b][nt][1] = c[b][nt][2] = c[b][nt][3] = 0.f;
 #pragma unroll
     for (int w = 0; w < D / 32; ++w)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t xe = h ? even[w] >> 8 : even[w], xo = h ? odd[w] >> 8 : odd[w];
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma_f16_16816(c[b][nt], xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1], c[b][nt][0], c[b][nt][1],
-                        c[b][nt][2], c[b][nt][3]);
-      }
+        for (int b = 0; b < kPair; ++b) {
+          const uint32_t xe = x[b][w] >> (8 * h), xo = x[b][D / 32 + w] >> (8 * h);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float(&s)[4] = c[b0 + b][nt];
+            mma_f16_16816(s, xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1], s[0], s[1], s[2], s[3]);
+          }
+        }
   }
 }
 
@@ -425,21 +428,25 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
       x[b][0] = v.x, x[b][1] = v.y, x[b][2] = v.z, x[b][3] = v.w;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float sum[NT][4];
+    for (int j0 = 0; j0 < 4; j0 += 2) {
+      float sum[2][NT][4];
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        const uint32_t lo = x[b][j], hi = lo >> 8;
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float(&c)[4] = b == 0 ? less[nt] : sum[nt];
-          mma_f16_16816(sum[nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1], c[0], c[1], c[2], c[3]);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t lo = x[b][j0 + j], hi = lo >> 8;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float(&c)[4] = b == 0 ? less[nt] : sum[j][nt];
+            mma_f16_16816(sum[j][nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1], c[0], c[1], c[2], c[3]);
+          }
         }
-      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) R.acc[nt][4 * i + j][k] += sum[nt][k];
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) R.acc[nt][4 * i + j0 + j][k] += sum[j][nt][k];
     }
   }
 }
@@ -450,8 +457,11 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
 // text's).  The row is cut into ranges of equal cost, one per team of 1, 2, 4 or 8 warps, so that the teams end together
 // whatever the lengths are; the warps of a team share out a unit's tiles.  A unit costs its tiles and kUnitCost more for
 // every warp of the team.  A unit inside one range is finished there; of one that reaches over a border each team leaves
-// its sums, and the launch that follows puts them together, in the order of the teams.  Where units are short next to
-// that launch, or next to a range, a team takes those that begin in its range whole, and nothing is left to put together.
+// its sums, a piece, and raises the piece's flag.  Then it looks at the flags of the unit's other pieces: the team that
+// finds all of them up puts the pieces together, in the order of the teams, and takes the flags down.  (Each team raises its
+// own before it looks, so the last one finds all.  Two may, and write the same.  A flag is up when it holds the call's
+// number of 64 bits, so the workspace needs no clearing.)  Where units are short next to that, or next to a range, a
+// team takes those that begin in its range whole, and nothing is left to put together.
 //
 // Teams of one warp are the even ones: with teams of eight, a range of many short units costs more than one of a long unit
 // (16 sequences of 1 to 5 000 tokens, 32 heads: XX us with eight, YY with one).  Eight where units are long (fewer sums to leave
@@ -495,6 +505,21 @@ __device__ __forceinline__ Place place_of(const AttendArgs& A, int seq, bool rep
 // no numbers.
 __device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : exp2f(ms - m); }
 
+// Adds a piece (reference and sum, elements) to a column's pieces so far.
+template <int D>
+__device__ __forceinline__ void add_piece(float& m, float& l, float (&o)[D / 32], float2 ml, const float (&v)[D / 32], bool first) {
+  if (first || l == 0.f) {
+    m = ml.x, l = ml.y;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = v[i];
+  } else if (ml.y != 0.f) {
+    const float top = fmaxf(m, ml.x), f = weight_of(m, top), w = weight_of(ml.x, top);
+    m = top, l = fmaf(l, f, ml.y * w);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(o[i], f, v[i] * w);
+  }
+}
+
 template <int D>
 __device__ __forceinline__ void write_row(const AttendArgs& A, size_t row, float m, float l, const float (&o)[D / 32], int lane) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -504,6 +529,18 @@ __device__ __forceinline__ void write_row(const AttendArgs& A, size_t row, float
     reinterpret_cast<uint32_t*>(A.out + row * D)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
   }
   if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// the same from memory that another block wrote in this launch
+template <int D>
+__device__ __forceinline__ void load_run_l2(const float* p, float (&o)[D / 32], int lane) {
+  if constexpr (D == 128) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + lane);
+    o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+  } else {
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(p) + lane);
+    o[0] = v.x, o[1] = v.y;
+  }
 }
 
 template <int D>
@@ -517,20 +554,16 @@ __device__ __forceinline__ void load_run(const float* p, float (&o)[D / 32], int
   }
 }
 
-// A unit that reaches over the border behind a team's range: what puts its pieces together has to know.
-struct __align__(16) Border {
-  int64_t token0;
-  int32_t kvh, row0, n_rows;     // n_rows: of the sequence; 0: no unit begins here and reaches over
-  int32_t last;                  // the last team with a piece
-  int32_t place;                 // of the first piece: 0 if it is the team's first unit, else 1 (later teams': 0)
-  int32_t pad;
-};
-static_assert(sizeof(Border) == 32, "Border layout");
-
 // A piece: columns of D elements, then (reference, sum) of each column.
 template <int D, int NT>
 __device__ __forceinline__ float* piece_at(const AttendArgs& A, int team, int place) {
   return A.part + (static_cast<size_t>(team) * 2 + place) * (8 * NT * (D + 2));
+}
+
+__device__ __forceinline__ unsigned long long flag_of(const unsigned long long* p) {
+  unsigned long long v;
+  asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return v;
 }
 
 __device__ __forceinline__ void team_barrier(int team, int threads) {
@@ -539,7 +572,7 @@ __device__ __forceinline__ void team_barrier(int team, int threads) {
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+__global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
   using R_ = Ring<D>;
   constexpr int kRow = D + 4;            // of a column's sums in shared memory
   static_assert(8 * NT * kRow * 4 <= R_::kBytes, "a warp's sums take its ring's place");
@@ -547,9 +580,10 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
   __shared__ uint2 scan[kAttWarps];
   __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
   __shared__ uint32_t longest_;
+  __shared__ int sm_all[kAttWarps];
   uint2* before = reinterpret_cast<uint2*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] tiles and units of the sequences before
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  pdl_launch_dependents();
+  pdl_wait();
   if (threadIdx.x == 0) before[0] = make_uint2(0, 0), longest_ = 0;
   __syncthreads();
   uint64_t total = 0;
@@ -603,14 +637,6 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
   uint32_t per = (cost + n_teams - 1) / n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per / 8);
   if (!whole_units) per = max(per, team_warps + more);
-  if (member == 0 && lane == 0) {
-    const Border none{};
-    A.borders[team] = none;
-  }
-  for (uint32_t i = blockIdx.x * kAttWarps + warp + n_teams; lane == 0 && i < n_warps; i += n_warps) {
-    const Border none{};
-    A.borders[i] = none;
-  }
   uint32_t at = min(static_cast<uint64_t>(team) * per, static_cast<uint64_t>(cost));
   const uint32_t end = min(cost, at + per);
   if (at >= end) return;
@@ -625,7 +651,6 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
     seq = lo;
   }
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
-  int done = 0;      // units so far
   while (at < end) {
     while (before_cost(seq + 1) <= at) ++seq;
     const Place u = place_of(A, seq, false);
@@ -748,7 +773,10 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
     team_barrier(in_block, threads);
     const int n_here = min(8 * NT, u.n_rows - row0);
     const bool whole = first == 0 && last == u.tiles;
-    float* piece = piece_at<D, NT>(A, team, done == 0 ? 0 : 1);
+    // pieces: the first team's is its second one if a unit before this one ends in its range, all others are a team's first
+    const uint32_t first_team = whole ? team : (unit_at + more) / per, last_team = whole ? team : (unit_at + unit_cost - 1) / per;
+    const uint32_t first_place = unit_at > first_team * per ? 1 : 0, place = team == first_team ? first_place : 0;
+    float* piece = piece_at<D, NT>(A, team, place);
     for (int col = member; col < n_here; col += static_cast<int>(team_warps)) {
       float m = -INFINITY, l = 0.f, o[D / 32] = {};
       for (int w = team0; w < team0 + static_cast<int>(team_warps); ++w) m = fmaxf(m, sm_m[w][col]);
@@ -770,42 +798,48 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 2 : 1) quant_attend_
         if (lane == 0) reinterpret_cast<float2*>(piece + 8 * NT * D)[col] = make_float2(m, l);
       }
     }
-    if (member == 0 && lane == 0 && first == 0 && last < u.tiles) {      // it goes on behind the range
-      Border b{};
-      b.token0 = u.token0, b.kvh = kvh, b.row0 = row0, b.n_rows = u.n_rows;
-      b.last = (unit_at + unit_cost - 1) / per;
-      b.place = done == 0 ? 0 : 1;
-      A.borders[team] = b;
-    }
-    ++done;
-    if (at < end) team_barrier(in_block, threads);      // the rings' places are free again
-  }
-}
-
-// Puts the pieces of the units that reach over borders together: a warp per border and column.
-template <int D, int NT>
-__global__ void __launch_bounds__(256) quant_merge_kernel(const __grid_constant__ AttendArgs A, int32_t cols) {
-  const int lane = threadIdx.x & 31, at = blockIdx.x * 8 + (threadIdx.x >> 5), team = at / cols, col = at - team * cols;
-  pdl_wait();
-  if (team >= A.n_borders) return;
-  const Border b = A.borders[team];
-  if (col < min(8 * NT, b.n_rows - b.row0)) {
-    float m = -INFINITY, l = 0.f, o[D / 32] = {};
-    for (int i = team; i <= b.last; ++i)
-      m = fmaxf(m, reinterpret_cast<const float2*>(piece_at<D, NT>(A, i, i == team ? b.place : 0) + 8 * NT * D)[col].x);
-    for (int i = team; i <= b.last; ++i) {
-      const float* piece = piece_at<D, NT>(A, i, i == team ? b.place : 0);
-      const float2 ml = reinterpret_cast<const float2*>(piece + 8 * NT * D)[col];
-      if (ml.y == 0.f) continue;
-      const float f = weight_of(ml.x, m);
-      l = fmaf(ml.y, f, l);
-      float v[D / 32];
-      load_run<D>(piece + col * D, v, lane);
+    if (!whole) {
+      team_barrier(in_block, threads);
+      if (member == 0) {
+        if (lane == 0) atomicExch(A.flags + 2 * team + place, A.nonce);
+        __syncwarp();
+        asm volatile("fence.sc.gpu;" ::: "memory");
+        bool all = true;
+        for (uint32_t i = first_team + lane; i <= last_team; i += 32) all &= flag_of(A.flags + 2 * i + (i == first_team ? first_place : 0)) == A.nonce;
+        all = __all_sync(0xffffffffu, all);
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");
+        if (lane == 0) sm_all[in_block] = all;
+      }
+      team_barrier(in_block, threads);
+      if (sm_all[in_block]) {
+        constexpr int kCols = 4;      // columns side by side: each one's pieces come one after the other
+        for (int col0 = member; col0 < n_here; col0 += kCols * static_cast<int>(team_warps)) {
+          float m[kCols], l[kCols] = {}, o[kCols][D / 32];
+#pragma unroll 2
+          for (uint32_t i = first_team; i <= last_team; ++i) {
+            const float* p = piece_at<D, NT>(A, i, i == first_team ? first_place : 0);
+            float2 ml[kCols];
+            float v[kCols][D / 32];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) o[j] = fmaf(v[j], f, o[j]);
+            for (int k = 0; k < kCols; ++k) {
+              const int col = min(col0 + k * static_cast<int>(team_warps), n_here - 1);
+              ml[k] = __ldcg(reinterpret_cast<const float2*>(p + 8 * NT * D) + col);
+              load_run_l2<D>(p + col * D, v[k], lane);
+            }
+#pragma unroll
+            for (int k = 0; k < kCols; ++k) add_piece<D>(m[k], l[k], o[k], ml[k], v[k], i == first_team);
+          }
+#pragma unroll
+          for (int k = 0; k < kCols; ++k) {
+            const int col = col0 + k * static_cast<int>(team_warps), r = row0 + col, query = query_of(A, r);
+            if (col < n_here) write_row<D>(A, static_cast<size_t>(u.token0 + query) * A.hq + kvh * A.group + r - query * A.group, m[k], l[k], o[k], lane);
+          }
+        }
+        if (member == 0)
+          for (uint32_t i = first_team + lane; i <= last_team; i += 32) A.flags[2 * i + (i == first_team ? first_place : 0)] = 0;
+      }
     }
-    const int r = b.row0 + col, query = query_of(A, r);
-    write_row<D>(A, static_cast<size_t>(b.token0 + query) * A.hq + b.kvh * A.group + r - query * A.group, m, l, o, lane);
+    if (at < end) team_barrier(in_block, threads);      // the rings' places are free again
   }
 }
 
@@ -837,8 +871,19 @@ int row_tile_of(const qc_quant_attend_args* a) { return a->max_queries * (a->n_q
 
 constexpr int kMostTeams = 2560;   // of one warp each; the workspace is sized for it
 
+// A number that no other call has, nor memory by chance.
+unsigned long long next_nonce() {
+  static std::atomic<unsigned long long> count{static_cast<unsigned long long>(std::chrono::steady_clock::now().time_since_epoch().count()) * 0x9E3779B97F4A7C15ull ^
+                                               static_cast<unsigned long long>(std::chrono::system_clock::now().time_since_epoch().count())};
+  unsigned long long x = count.fetch_add(0x9E3779B97F4A7C15ull, std::memory_order_relaxed);   // splitmix64
+  x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
+  x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+  x ^= x >> 31;
+  return x ? x : 1;
+}
+
 template <int D, int NT>
-cudaError_t launch(AttendArgs& A, int device, int cols, cudaStream_t stream) {
+cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
   const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
   static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
   cudaError_t e;
@@ -849,17 +894,14 @@ cudaError_t launch(AttendArgs& A, int device, int cols, cudaStream_t stream) {
   }
   int sms = 0;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return e;
-  int blocks = sms * (NT == 1 ? 2 : 1);
+  int blocks = sms * (NT == 1 ? 3 : 2);
   if (blocks > kMostTeams / kAttWarps) blocks = kMostTeams / kAttWarps;
-  A.n_borders = blocks * kAttWarps;
-  quant_attend_kernel<D, NT><<<blocks, kAttWarps * 32, smem, stream>>>(A);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  return launch_pdl(quant_merge_kernel<D, NT>, dim3((A.n_borders * cols + 7) / 8), dim3(256), 0, stream, A, cols);
+  A.nonce = next_nonce();
+  return launch_pdl(quant_attend_kernel<D, NT>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
 }
 
 size_t workspace_bytes(const qc_quant_attend_args* a) {
-  return kMostTeams * sizeof(Border) + static_cast<size_t>(kMostTeams) * 2 * 8 * row_tile_of(a) * (a->head_dim + 2) * 4;
+  return kMostTeams * 2 * sizeof(unsigned long long) + static_cast<size_t>(kMostTeams) * 2 * 8 * row_tile_of(a) * (a->head_dim + 2) * 4;
 }
 
 }  // namespace
@@ -876,22 +918,23 @@ extern "C" int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, si
 
 extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend_args* args) {
   if (const int32_t bad = check_sizes(args)) return bad;
-  if (!args->text || !args->out_dev || off(args->out_dev, 16) || off(args->lse_out_dev, 4) || off(args->status_dev, 4) || off(args->seq_ids_dev, 4) ||
+  if (!args->out_dev || off(args->out_dev, 16) || off(args->lse_out_dev, 4) || off(args->status_dev, 4) || off(args->seq_ids_dev, 4) ||
       off(args->starts_dev, 4) || off(args->workspace_dev, 16))
     return QC_ERR_INVALID_ARG;
   if (!(args->softmax_scale >= 0.f) || !isfinite(args->softmax_scale)) return QC_ERR_INVALID_ARG;
   if (!args->seq_ids_dev && args->n_seqs > args->max_seqs) return QC_ERR_INVALID_ARG;
   if (!args->starts_dev && args->n_tokens < args->n_seqs) return QC_ERR_INVALID_ARG;
   AttendArgs A{};
-  if (const int32_t bad = check_stream(args->text, args, A.stream[0])) return bad;
-  if (args->visual)
-    if (const int32_t bad = check_stream(args->visual, args, A.stream[1])) return bad;
+  if (const int32_t bad = check_stream(&args->text, args, A.stream[0])) return bad;
+  const qc_quant_stream& v = args->visual;
+  A.has_visual = v.q_dev || v.k_pool_dev || v.v_pool_dev || v.pages_dev || v.lens_dev;
+  if (A.has_visual)
+    if (const int32_t bad = check_stream(&v, args, A.stream[1])) return bad;
   if (args->workspace_bytes < workspace_bytes(args) || !args->workspace_dev) return QC_ERR_INVALID_ARG;
   if (args->n_tokens == 0) return QC_OK;
-  A.has_visual = args->visual != nullptr;
   A.ids = args->seq_ids_dev, A.starts = args->starts_dev;
   A.out = static_cast<uint16_t*>(args->out_dev), A.lse = args->lse_out_dev;
-  A.borders = static_cast<Border*>(args->workspace_dev), A.part = reinterpret_cast<float*>(A.borders + kMostTeams);
+  A.flags = static_cast<unsigned long long*>(args->workspace_dev), A.part = reinterpret_cast<float*>(A.flags + 2 * kMostTeams);
   A.status = args->status_dev;
   A.hq = args->n_q_heads, A.hkv = args->n_kv_heads, A.group = A.hq / A.hkv, A.page = args->page_size;
   A.page_shift = A.page == 16 ? 4 : A.page == 32 ? 5 : 6;
@@ -899,10 +942,9 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   A.causal = args->causal != 0;
   A.inv_group = 1.f / A.group;
   const int nt = row_tile_of(args);
-  const int cols = A.max_queries * A.group < 8 * nt ? A.max_queries * A.group : 8 * nt;
   A.head_units = static_cast<uint32_t>(A.page * (args->head_dim / 2) / 64), A.code_units = A.hkv * A.head_units;
   A.page_units = static_cast<uint32_t>(quant_page_bytes(A.hkv, args->head_dim, A.page) / 64);
-  if (static_cast<int64_t>(args->text->n_pages) * A.page_units > UINT32_MAX || (args->visual && static_cast<int64_t>(args->visual->n_pages) * A.page_units > UINT32_MAX))
+  if (static_cast<int64_t>(args->text.n_pages) * A.page_units > UINT32_MAX || static_cast<int64_t>(A.has_visual ? v.n_pages : 0) * A.page_units > UINT32_MAX)
     return QC_ERR_UNSUPPORTED;
   const float scale = args->softmax_scale > 0.f ? args->softmax_scale : 1.0f / sqrtf(static_cast<float>(args->head_dim));
   A.scale_log2 = scale * 1.4426950408889634f;
@@ -910,7 +952,7 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (args->head_dim == 128) e = nt == 1 ? launch<128, 1>(A, device, cols, stream) : launch<128, 2>(A, device, cols, stream);
-  else e = nt == 1 ? launch<64, 1>(A, device, cols, stream) : launch<64, 2>(A, device, cols, stream);
+  if (args->head_dim == 128) e = nt == 1 ? launch<128, 1>(A, device, stream) : launch<128, 2>(A, device, stream);
+  else e = nt == 1 ? launch<64, 1>(A, device, stream) : launch<64, 2>(A, device, stream);
   return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }

@@ -150,17 +150,18 @@ def attend_args(stream=None, visual=None, **change):
     t = qc.qc_quant_stream(**{**dict(q_dev=64, q_stride=512, k_pool_dev=64, v_pool_dev=64, pages_dev=64, lens_dev=64, max_pages=4, n_pages=9), **(stream or {})})
     v = qc.qc_quant_stream(**{**dict(q_dev=64, q_stride=512, k_pool_dev=64, v_pool_dev=64, pages_dev=64, lens_dev=64, max_pages=4, n_pages=9), **visual}) if visual is not None else None
     a = qc.qc_quant_attend_args(n_q_heads=4, n_kv_heads=2, head_dim=128, page_size=16, n_seqs=2, max_seqs=3, n_tokens=2, max_queries=1, causal=1,
-                                text=C.pointer(t), visual=C.pointer(v) if v is not None else None, out_dev=64, workspace_dev=256, workspace_bytes=1 << 40)
+                                text=t, out_dev=64, workspace_dev=256, workspace_bytes=1 << 40)
+    if v is not None:
+        a.visual = v
     for name, value in change.items():
         setattr(a, name, value)
-    a.kept = (t, v)
     return a
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(head_dim=80), 2), (dict(page_size=48), 2), (dict(n_q_heads=5), 1), (dict(n_q_heads=0), 1), (dict(n_kv_heads=0), 1), (dict(n_seqs=0), 1), (dict(max_seqs=0), 1),
     (dict(n_seqs=4), 1), (dict(n_tokens=-1), 1), (dict(n_tokens=1), 1), (dict(max_queries=0), 1), (dict(max_queries=qc.QC_QUANT_MAX_QUERIES + 1), 2),
-    (dict(n_seqs=qc.QC_TABLE_MAX_BATCH + 1, seq_ids_dev=64), 2), (dict(n_q_heads=2 * qc.QC_QUANT_MAX_HEADS), 2), (dict(text=None), 1), (dict(out_dev=0), 1), (dict(out_dev=72), 1),
+    (dict(n_seqs=qc.QC_TABLE_MAX_BATCH + 1, seq_ids_dev=64), 2), (dict(n_q_heads=2 * qc.QC_QUANT_MAX_HEADS), 2), (dict(text=qc.qc_quant_stream()), 1), (dict(out_dev=0), 1), (dict(out_dev=72), 1),
     (dict(lse_out_dev=66), 1), (dict(status_dev=65), 1), (dict(seq_ids_dev=66), 1), (dict(starts_dev=66), 1), (dict(softmax_scale=-1.0), 1),
     (dict(softmax_scale=math.nan), 1), (dict(softmax_scale=math.inf), 1), (dict(workspace_dev=72), 1),
     (dict(stream=dict(q_dev=0)), 1), (dict(stream=dict(q_dev=72)), 1), (dict(stream=dict(q_stride=-8)), 1), (dict(stream=dict(q_stride=12)), 1), (dict(stream=dict(k_pool_dev=0)), 1),
@@ -179,6 +180,17 @@ def test_attention_refuses_a_workspace_that_is_too_small():
     for size, at in ((need - 1, 256), (need, 0)):
         a.workspace_bytes, a.workspace_dev = size, at
         assert status_of(lambda: qc.qc_quant_attend(0, 0, a)) == qc.QC_ERR_INVALID_ARG
+
+
+def test_packed_structures_have_the_header_s_layout():
+    for packed, made in ((quant._TABLE, qc.qc_table), (quant._SHAPE, qc.qc_quant_shape), (quant._ATTEND, qc.qc_quant_attend_args)):
+        assert packed.size == C.sizeof(made)
+    args = attend_args(visual=dict(q_dev=128, n_pages=77), status_dev=640, softmax_scale=0.25)
+    fields = [getattr(args, name) for name, _ in args._fields_]
+    flat = []
+    for f in fields:
+        flat += [getattr(f, name) or 0 for name, _ in f._fields_] if isinstance(f, C.Structure) else [f or 0]
+    assert quant._ATTEND.pack(*flat) == bytes(args)
 
 
 def test_null_pointers_are_refused(lib):
