@@ -140,14 +140,14 @@ def load() -> C.CDLL:
         "qc_set_option": [vp, C.c_char_p, i64],
         "qc_get_profile": [vp, C.POINTER(qc_profile)],
         "qc_attend_static": [i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, C.c_float],
-        "qc_table_reset": [i32, vp, vp],
-        "qc_table_extend": [i32, vp, vp, i32, vp, vp, i32, vp, vp],
-        "qc_table_trim": [i32, vp, vp, i32, vp, vp],
+        "qc_table_reset": [i32, vp, C.POINTER(qc_table)],
+        "qc_table_extend": [i32, vp, C.POINTER(qc_table), i32, vp, vp, i32, vp, vp],
+        "qc_table_trim": [i32, vp, C.POINTER(qc_table), i32, vp, vp],
         "qc_quant_pool_bytes": [C.POINTER(qc_quant_shape), C.POINTER(C.c_size_t)],
-        "qc_quant_append": [i32, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp],
-        "qc_quant_read": [i32, vp, vp, i32, vp, vp, vp, vp, vp],
+        "qc_quant_append": [i32, vp, C.POINTER(qc_quant_shape), i32, vp, vp, i64, vp, i64, vp, vp],
+        "qc_quant_read": [i32, vp, C.POINTER(qc_quant_shape), i32, vp, vp, vp, vp, vp],
         "qc_quant_workspace_bytes": [C.POINTER(qc_quant_attend_args), C.POINTER(C.c_size_t)],
-        "qc_quant_attend": [i32, vp, vp],
+        "qc_quant_attend": [i32, vp, C.POINTER(qc_quant_attend_args)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -325,7 +325,6 @@ def qc_attend_static(device: int, cuda_stream: int, q_ptr: int, k_ptr: int, v_pt
 
 # ---- a cache in 4 bits (pointers are device addresses, 0 or None where the header allows null) --------------
 
-# Their structures travel as plain addresses; `quant` hands over packed bytes of the same layout.
 QC_TABLE_MAX_BATCH = 4096
 QC_TABLE_MAX_SEQS = 65536
 QC_QUANT_MAX_HEADS = 1024
@@ -333,19 +332,19 @@ QC_QUANT_MAX_QUERIES = 16
 
 
 def qc_table_reset(device: int, cuda_stream: int, table: qc_table) -> None:
-    _check(load().qc_table_reset(device, cuda_stream, C.byref(table)), "qc_table_reset")
+    _check(load().qc_table_reset(device, cuda_stream, table), "qc_table_reset")
 
 
 def qc_table_extend(device: int, cuda_stream: int, table: qc_table, n_seqs: int, seq_ids_ptr: int, n_new_ptr: int,
                     max_slots: int, starts_ptr: int, slots_ptr: int) -> None:
     _refuse_objects(seq_ids_ptr, n_new_ptr, starts_ptr, slots_ptr)
-    _check(load().qc_table_extend(device, cuda_stream, C.byref(table), n_seqs, seq_ids_ptr, n_new_ptr, max_slots, starts_ptr, slots_ptr),
+    _check(load().qc_table_extend(device, cuda_stream, table, n_seqs, seq_ids_ptr, n_new_ptr, max_slots, starts_ptr, slots_ptr),
            "qc_table_extend")
 
 
 def qc_table_trim(device: int, cuda_stream: int, table: qc_table, n_seqs: int, seq_ids_ptr: int, n_keep_ptr: int) -> None:
     _refuse_objects(seq_ids_ptr, n_keep_ptr)
-    _check(load().qc_table_trim(device, cuda_stream, C.byref(table), n_seqs, seq_ids_ptr, n_keep_ptr), "qc_table_trim")
+    _check(load().qc_table_trim(device, cuda_stream, table, n_seqs, seq_ids_ptr, n_keep_ptr), "qc_table_trim")
 
 
 def qc_quant_pool_bytes(shape: qc_quant_shape) -> int:
@@ -357,14 +356,14 @@ def qc_quant_pool_bytes(shape: qc_quant_shape) -> int:
 def qc_quant_append(device: int, cuda_stream: int, shape: qc_quant_shape, n_tokens: int, slots_ptr: int, k_ptr: int, k_stride: int,
                     v_ptr: int, v_stride: int, k_pool_ptr: int, v_pool_ptr: int) -> None:
     _refuse_objects(slots_ptr, k_ptr, v_ptr, k_pool_ptr, v_pool_ptr)
-    _check(load().qc_quant_append(device, cuda_stream, C.byref(shape), n_tokens, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, k_pool_ptr,
+    _check(load().qc_quant_append(device, cuda_stream, shape, n_tokens, slots_ptr, k_ptr, k_stride, v_ptr, v_stride, k_pool_ptr,
                                   v_pool_ptr), "qc_quant_append")
 
 
 def qc_quant_read(device: int, cuda_stream: int, shape: qc_quant_shape, n_tokens: int, slots_ptr: int, k_pool_ptr: int,
                   v_pool_ptr: int, k_out_ptr: int, v_out_ptr: int) -> None:
     _refuse_objects(slots_ptr, k_pool_ptr, v_pool_ptr, k_out_ptr, v_out_ptr)
-    _check(load().qc_quant_read(device, cuda_stream, C.byref(shape), n_tokens, slots_ptr, k_pool_ptr, v_pool_ptr, k_out_ptr, v_out_ptr),
+    _check(load().qc_quant_read(device, cuda_stream, shape, n_tokens, slots_ptr, k_pool_ptr, v_pool_ptr, k_out_ptr, v_out_ptr),
            "qc_quant_read")
 
 
@@ -375,4 +374,4 @@ def qc_quant_workspace_bytes(args: qc_quant_attend_args) -> int:
 
 
 def qc_quant_attend(device: int, cuda_stream: int, args: qc_quant_attend_args) -> None:
-    _check(load().qc_quant_attend(device, cuda_stream, C.byref(args)), "qc_quant_attend")
+    _check(load().qc_quant_attend(device, cuda_stream, args), "qc_quant_attend")

@@ -83,6 +83,12 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
+// C += A B
+__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 constexpr uint32_t kLower = 0x000f000fu, kUpper = 0x00f000f0u;   // codes as two fp16 numbers: c * 2^-24, and c * 2^-20
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
@@ -266,7 +272,7 @@ __device__ __forceinline__ void score_tile(float (&c)[kTile / 16][NT][4], const 
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float(&s)[4] = c[b0 + b][nt];
-            mma_f16_16816(s, xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1], s[0], s[1], s[2], s[3]);
+            mma_f16_16816(s, xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1]);
           }
         }
   }
@@ -417,7 +423,7 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
     less[nt][0] = less[nt][1] = less[nt][2] = less[nt][3] = 0.f;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)      // rows of 8 * 2^-24 and of 128 * 2^-24, negative
-      mma_f16_16816(less[nt], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, w[b][nt][0], w[b][nt][1], less[nt][0], less[nt][1], less[nt][2], less[nt][3]);
+      mma_f16_16816(less[nt], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, w[b][nt][0], w[b][nt][1]);
   }
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
@@ -437,8 +443,8 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
           const uint32_t lo = x[b][j0 + j], hi = lo >> 8;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const float(&c)[4] = b == 0 ? less[nt] : sum[j][nt];
-            mma_f16_16816(sum[j][nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1], c[0], c[1], c[2], c[3]);
+            if (b == 0) mma_f16_16816(sum[j][nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1], less[nt][0], less[nt][1], less[nt][2], less[nt][3]);
+            else mma_f16_16816(sum[j][nt], lo & kLower, lo & kUpper, hi & kLower, hi & kUpper, w[b][nt][0], w[b][nt][1]);
           }
         }
 #pragma unroll
@@ -558,6 +564,36 @@ __device__ __forceinline__ void load_run(const float* p, float (&o)[D / 32], int
 template <int D, int NT>
 __device__ __forceinline__ float* piece_at(const AttendArgs& A, int team, int place) {
   return A.part + (static_cast<size_t>(team) * 2 + place) * (8 * NT * (D + 2));
+}
+
+// Puts the pieces of a unit together and writes its rows: columns member, member + warps, ...  Not inlined, so that the
+// loop over the tiles keeps its registers.
+template <int D, int NT>
+__device__ __noinline__ void merge_pieces(const AttendArgs& A, uint32_t first_team, uint32_t last_team, uint32_t first_place, int member, int warps, int n_here,
+                                          int row0, int64_t token0, int kvh, int lane) {
+          constexpr int kCols = 4;      // columns side by side: each one's pieces come one after the other
+          for (int col0 = member; col0 < n_here; col0 += kCols * warps) {
+            float m[kCols], l[kCols] = {}, o[kCols][D / 32];
+  #pragma unroll 2
+            for (uint32_t i = first_team; i <= last_team; ++i) {
+              const float* p = piece_at<D, NT>(A, i, i == first_team ? first_place : 0);
+              float2 ml[kCols];
+              float v[kCols][D / 32];
+  #pragma unroll
+              for (int k = 0; k < kCols; ++k) {
+                const int col = min(col0 + k * warps, n_here - 1);
+                ml[k] = __ldcg(reinterpret_cast<const float2*>(p + 8 * NT * D) + col);
+                load_run_l2<D>(p + col * D, v[k], lane);
+              }
+  #pragma unroll
+              for (int k = 0; k < kCols; ++k) add_piece<D>(m[k], l[k], o[k], ml[k], v[k], i == first_team);
+            }
+  #pragma unroll
+            for (int k = 0; k < kCols; ++k) {
+              const int col = col0 + k * warps, r = row0 + col, query = query_of(A, r);
+              if (col < n_here) write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, m[k], l[k], o[k], lane);
+            }
+          }
 }
 
 __device__ __forceinline__ unsigned long long flag_of(const unsigned long long* p) {
@@ -812,29 +848,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
       }
       team_barrier(in_block, threads);
       if (sm_all[in_block]) {
-        constexpr int kCols = 4;      // columns side by side: each one's pieces come one after the other
-        for (int col0 = member; col0 < n_here; col0 += kCols * static_cast<int>(team_warps)) {
-          float m[kCols], l[kCols] = {}, o[kCols][D / 32];
-#pragma unroll 2
-          for (uint32_t i = first_team; i <= last_team; ++i) {
-            const float* p = piece_at<D, NT>(A, i, i == first_team ? first_place : 0);
-            float2 ml[kCols];
-            float v[kCols][D / 32];
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) {
-              const int col = min(col0 + k * static_cast<int>(team_warps), n_here - 1);
-              ml[k] = __ldcg(reinterpret_cast<const float2*>(p + 8 * NT * D) + col);
-              load_run_l2<D>(p + col * D, v[k], lane);
-            }
-#pragma unroll
-            for (int k = 0; k < kCols; ++k) add_piece<D>(m[k], l[k], o[k], ml[k], v[k], i == first_team);
-          }
-#pragma unroll
-          for (int k = 0; k < kCols; ++k) {
-            const int col = col0 + k * static_cast<int>(team_warps), r = row0 + col, query = query_of(A, r);
-            if (col < n_here) write_row<D>(A, static_cast<size_t>(u.token0 + query) * A.hq + kvh * A.group + r - query * A.group, m[k], l[k], o[k], lane);
-          }
-        }
+        merge_pieces<D, NT>(A, first_team, last_team, first_place, member, static_cast<int>(team_warps), n_here, row0, u.token0, kvh, lane);
         if (member == 0)
           for (uint32_t i = first_team + lane; i <= last_team; i += 32) A.flags[2 * i + (i == first_team ? first_place : 0)] = 0;
       }

@@ -182,17 +182,6 @@ def test_attention_refuses_a_workspace_that_is_too_small():
         assert status_of(lambda: qc.qc_quant_attend(0, 0, a)) == qc.QC_ERR_INVALID_ARG
 
 
-def test_packed_structures_have_the_header_s_layout():
-    for packed, made in ((quant._TABLE, qc.qc_table), (quant._SHAPE, qc.qc_quant_shape), (quant._ATTEND, qc.qc_quant_attend_args)):
-        assert packed.size == C.sizeof(made)
-    args = attend_args(visual=dict(q_dev=128, n_pages=77), status_dev=640, softmax_scale=0.25)
-    fields = [getattr(args, name) for name, _ in args._fields_]
-    flat = []
-    for f in fields:
-        flat += [getattr(f, name) or 0 for name, _ in f._fields_] if isinstance(f, C.Structure) else [f or 0]
-    assert quant._ATTEND.pack(*flat) == bytes(args)
-
-
 def test_null_pointers_are_refused(lib):
     n = C.c_size_t()
     assert lib.qc_table_reset(0, None, None) == lib.qc_table_trim(0, None, None, 1, None, None) == qc.QC_ERR_INVALID_ARG
