@@ -21,13 +21,6 @@ __host__ __device__ __forceinline__ int64_t quant_page_bytes(int n_kv_heads, int
   return static_cast<int64_t>(n_kv_heads) * page * (d / 2 + 4);
 }
 
-// Byte of a K block where element e (even) of token i begins.
-template <int D>
-__device__ __forceinline__ int k_code_offset(int i, int e) {
-  if constexpr (D == 128) return (i & 1) * 512 + ((i >> 1) * 4 + e / 32) * 16 + e % 32 / 2;
-  else return ((i >> 1) * 4 + e / 16) * 16 + (i & 1) * 8 + e % 16 / 2;
-}
-
 // The step 1 / r of a row: 0 where r is 0 (all its elements are lo).
 __device__ __forceinline__ float quant_step(uint32_t params) {
   const float r = __uint_as_float(params & 0xffff0000u);

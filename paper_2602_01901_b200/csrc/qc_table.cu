@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(1024) table_kernel(const TableArgs T) {
   if (threadIdx.x == 0) error = 0;
   if (T.ids)
     for (int i = threadIdx.x; i < (T.max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
+  pdl_wait();
   __syncthreads();
   const int32_t n_free = T.state[0];
 
@@ -259,8 +260,7 @@ extern "C" int32_t qc_table_extend(int32_t device, void* cuda_stream, const qc_t
   const size_t smem = static_cast<size_t>(n_seqs) * 12 + (seq_ids_dev ? (a.max_seqs + 31) / 32 * 4 : 0);
   if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
   const int32_t work = max_slots <= kSlotsInBlock && max_slots > n_seqs ? max_slots : n_seqs;
-  table_kernel<false><<<1, threads_for(work), smem, stream>>>(a);
-  if (cudaGetLastError() != cudaSuccess) return QC_ERR_CUDA;
+  if (launch_pdl(table_kernel<false>, dim3(1), dim3(threads_for(work)), smem, stream, a) != cudaSuccess) return QC_ERR_CUDA;
   if (max_slots > kSlotsInBlock) {
     const int blocks = max_slots / 256 + 1 < 1184 ? max_slots / 256 + 1 : 1184;
     if (launch_pdl(slots_kernel, dim3(blocks), dim3(256), 0, stream, a) != cudaSuccess) return QC_ERR_CUDA;
@@ -278,6 +278,5 @@ extern "C" int32_t qc_table_trim(int32_t device, void* cuda_stream, const qc_tab
   a.n_seqs = n_seqs, a.ids = seq_ids_dev, a.count = n_keep_dev;
   const size_t smem = static_cast<size_t>(n_seqs) * 8 + (seq_ids_dev ? (a.max_seqs + 31) / 32 * 4 : 0);
   if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
-  table_kernel<true><<<1, threads_for(n_seqs), smem, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  return launch_pdl(table_kernel<true>, dim3(1), dim3(threads_for(n_seqs)), smem, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }
