@@ -1,16 +1,18 @@
 // Page tables of one stream that live on the device: lengths, page ids, the free pages as a stack.
 // A step's bookkeeping (how many pages every sequence takes or gives back, which ones, and the slot
-// of every new token) is prefix sums over the batch, done by one thread block that holds the whole
-// batch's numbers in shared memory, so a step can be captured into a graph and replayed while its
-// sequences grow.
+// of every new token) is prefix sums over the batch, held in shared memory, so a step can be captured
+// into a graph and replayed while its sequences grow.
 //
 //   have_i = ceil(len_i / P), want_i = ceil((len_i + new_i) / P), first_i = sum_{j<i} (want_j - have_j)
 //   page (have_i + c) of sequence i = free[n_free - 1 - first_i - c]
 //   start_i = sum_{j<i} new_j;  token i of the call: slot = page * P + position % P
 //
 // Trimming is the inverse: what it gives back is taken again in the same order.  Nothing is changed
-// when the call cannot be carried out as a whole.  What bounds it is the launch and three dependent
-// trips to the L2 (ids, lengths, free pages); the bytes (some KB) do not count.
+// when the call cannot be carried out as a whole.  What bounds a step of single tokens is the launch and
+// three dependent trips to the L2 (ids, lengths, free pages); the bytes (some KB) do not count.  Where
+// many pages or slots may be written, a cluster of eight blocks shares them out: each makes the sums for itself,
+// and none writes before all have read (64 sequences of 500 to 9 000 tokens released and taken in: XX us with
+// one block and a launch of its own for the slots, YY so).
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -21,7 +23,9 @@ namespace {
 
 constexpr int kTableMaxBatch = QC_TABLE_MAX_BATCH;
 constexpr int kTableMaxSeqs = QC_TABLE_MAX_SEQS;
-constexpr int kSlotsInBlock = 8192;   // more slots than that are written by a launch of their own
+constexpr int kCluster = 8;
+constexpr int kManySlots = 4096;      // from so many slots (or entries of the rows released) on a cluster
+constexpr int kRun = 8;               // rounds of 32 adjacent slots that a warp writes before it looks for its place again
 
 struct TableArgs {
   int32_t* pages;
@@ -32,58 +36,70 @@ struct TableArgs {
   const int32_t* count;    // new tokens, or tokens to keep; null: 1 each, or none
   int32_t* starts;
   int32_t* slots;
-  int32_t n_seqs, max_seqs, max_pages, page, n_pages, max_slots;
+  int32_t n_seqs, max_seqs, max_pages, page_shift, n_pages, max_slots;
 };
 
-// Sums of a thread block's values: *before is what the threads before this one have, the result is the total.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* before, int64_t* warp_sums) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-  int64_t x = v;
+struct Sums {
+  int64_t pages, tokens;
+};
+
+// Sums of a thread block's values, of which the first n_warps warps have any: before is what the threads before this one
+// have, the result is the total.
+__device__ __forceinline__ Sums block_scan(Sums v, Sums& before, Sums* warp_sums, int n_warps) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Sums x = v;
+  if (warp < n_warps) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t p = __shfl_up_sync(0xffffffffu, x.pages, o), k = __shfl_up_sync(0xffffffffu, x.tokens, o);
+      if (lane >= o) x.pages += p, x.tokens += k;
+    }
   }
   __syncthreads();   // warp_sums may still be read from the sum before
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
-  int64_t base = 0, total = 0;
+  Sums base{0, 0}, total{0, 0};
   for (int w = 0; w < n_warps; ++w) {
-    if (w < warp) base += warp_sums[w];
-    total += warp_sums[w];
+    if (w < warp) base.pages += warp_sums[w].pages, base.tokens += warp_sums[w].tokens;
+    total.pages += warp_sums[w].pages, total.tokens += warp_sums[w].tokens;
   }
-  *before = base + x - v;
+  before = Sums{base.pages + x.pages - v.pages, base.tokens + x.tokens - v.tokens};
   return total;
 }
 
-// the last index whose entry is <= i, of n entries in ascending order (entry 0 is 0)
-__device__ __forceinline__ int last_not_above(const int32_t* a, int n, int32_t i) {
+// One sequence of the call.
+struct __align__(16) Seq {
+  int32_t id, len;     // row of the table, tokens before the call
+  int32_t first;       // pages that the sequences before it take or give back
+  int32_t start;       // tokens of the sequences before it; TRIM: tokens that stay
+};
+
+// the last of n sequences whose `first` (FIRST) or `start` is <= i; both ascend from 0
+template <bool FIRST>
+__device__ __forceinline__ int last_not_above(const Seq* s, int n, int32_t i) {
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (a[mid] <= i) lo = mid;
+    if ((FIRST ? s[mid].first : s[mid].start) <= i) lo = mid;
     else hi = mid - 1;
   }
   return lo;
 }
 
-__device__ __forceinline__ int32_t slot_of(const TableArgs& T, int seq, int32_t len, int32_t end, int32_t i) {
-  const int32_t id = T.ids ? T.ids[seq] : seq;
-  const int32_t pos = len - (end - i);
-  return T.pages[static_cast<size_t>(id) * T.max_pages + pos / T.page] * T.page + pos % T.page;
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// One block.  TRIM: give back what lies behind the tokens to keep; else take pages for the new tokens.
+// One block, or a cluster of them.  TRIM: give back what lies behind the tokens to keep; else take pages for the new tokens.
 template <bool TRIM>
 __global__ void __launch_bounds__(1024) table_kernel(const TableArgs T) {
-  extern __shared__ int32_t shared[];
-  int32_t* first = shared;                       // [n_seqs] pages that the sequences before take or give back
-  int32_t* keep = first + T.n_seqs;              // [n_seqs] pages that stay, or are there before
-  int32_t* start = keep + T.n_seqs;              // [n_seqs] tokens of the sequences before (not TRIM)
-  uint32_t* seen = reinterpret_cast<uint32_t*>(start + (TRIM ? 0 : T.n_seqs));   // [max_seqs / 32] ids met (where ids are given)
-  __shared__ int64_t warp_sums[32];
+  extern __shared__ __align__(16) uint8_t shared[];
+  Seq* seqs = reinterpret_cast<Seq*>(shared);                          // [n_seqs]
+  uint32_t* seen = reinterpret_cast<uint32_t*>(seqs + T.n_seqs);       // [max_seqs / 32] ids met (where ids are given)
+  __shared__ Sums warp_sums[32];
   __shared__ int32_t error;
-  const int n_seqs = T.n_seqs, page = T.page;
+  const int n_seqs = T.n_seqs, shift = T.page_shift, up = (1 << shift) - 1;
+  const int thread = blockIdx.x * blockDim.x + threadIdx.x, n_threads = gridDim.x * blockDim.x;
   if (threadIdx.x == 0) error = 0;
   if (T.ids)
     for (int i = threadIdx.x; i < (T.max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
@@ -91,105 +107,102 @@ __global__ void __launch_bounds__(1024) table_kernel(const TableArgs T) {
   __syncthreads();
   const int32_t n_free = T.state[0];
 
-  int64_t pages_total = 0, tokens_total = 0;
+  Sums all{0, 0};
   for (int i0 = 0; i0 < n_seqs; i0 += blockDim.x) {
     const int i = i0 + threadIdx.x;
-    int64_t moved = 0, tokens = 0;
+    Sums mine{0, 0};
+    Seq s{};
     if (i < n_seqs) {
-      const int32_t id = T.ids ? T.ids[i] : i, count = T.count ? T.count[i] : (TRIM ? 0 : 1);
+      const int32_t count = T.count ? T.count[i] : (TRIM ? 0 : 1);
+      s.id = T.ids ? T.ids[i] : i;
       int bad = 0;
-      if (id < 0 || id >= T.max_seqs || count < 0) bad = QC_ERR_INVALID_ARG;
-      else if (T.ids && (atomicOr(&seen[id >> 5], 1u << (id & 31)) >> (id & 31)) & 1u) bad = QC_ERR_STATE;
+      if (s.id < 0 || s.id >= T.max_seqs || count < 0) bad = QC_ERR_INVALID_ARG;
+      else if (T.ids && (atomicOr(&seen[s.id >> 5], 1u << (s.id & 31)) >> (s.id & 31)) & 1u) bad = QC_ERR_STATE;
       else {
-        const int64_t old = T.lens[id], room = static_cast<int64_t>(T.max_pages) * page;
+        s.len = T.lens[s.id];
+        const int64_t room = static_cast<int64_t>(T.max_pages) << shift, old = s.len;
         if (old < 0 || old > room) bad = QC_ERR_STATE;
         else if (!TRIM && old + count > room) bad = QC_ERR_OOM_PAGES;
         else {
           const int64_t now = TRIM ? min(old, static_cast<int64_t>(count)) : old + count;
-          const int64_t a = (old + page - 1) / page, b = (now + page - 1) / page;
-          moved = TRIM ? a - b : b - a;
-          keep[i] = static_cast<int32_t>(TRIM ? b : a);
-          tokens = TRIM ? 0 : count;
+          const int64_t a = (old + up) >> shift, b = (now + up) >> shift;
+          mine.pages = TRIM ? a - b : b - a;
+          mine.tokens = TRIM ? 0 : count;
+          s.start = static_cast<int32_t>(now);      // (TRIM)
         }
       }
       if (bad) atomicMax(&error, bad);
     }
-    int64_t before;
-    const int64_t sum = block_scan(moved, &before, warp_sums);
-    if (i < n_seqs) first[i] = static_cast<int32_t>(min(pages_total + before, static_cast<int64_t>(INT32_MAX)));
-    pages_total += sum;
-    if (!TRIM) {
-      const int64_t more = block_scan(tokens, &before, warp_sums);
-      if (i < n_seqs) start[i] = static_cast<int32_t>(min(tokens_total + before, static_cast<int64_t>(INT32_MAX)));
-      tokens_total += more;
-    }
+    Sums before;
+    const Sums sum = block_scan(mine, before, warp_sums, (min(n_seqs - i0, static_cast<int>(blockDim.x)) + 31) >> 5);
+    s.first = static_cast<int32_t>(min(all.pages + before.pages, static_cast<int64_t>(INT32_MAX)));
+    if (!TRIM) s.start = static_cast<int32_t>(min(all.tokens + before.tokens, static_cast<int64_t>(INT32_MAX)));
+    if (i < n_seqs) seqs[i] = s;
+    all.pages += sum.pages, all.tokens += sum.tokens;
   }
   __syncthreads();
   int bad = error;
   if (!bad) {
     if (n_free < 0 || n_free > T.n_pages) bad = QC_ERR_STATE;
-    else if (TRIM && n_free + pages_total > T.n_pages) bad = QC_ERR_STATE;   // more pages than there are
-    else if (!TRIM && pages_total > n_free) bad = QC_ERR_OOM_PAGES;
-    else if (!TRIM && tokens_total > T.max_slots) bad = QC_ERR_INVALID_ARG;
+    else if (TRIM && n_free + all.pages > T.n_pages) bad = QC_ERR_STATE;   // more pages than there are
+    else if (!TRIM && all.pages > n_free) bad = QC_ERR_OOM_PAGES;
+    else if (!TRIM && all.tokens > T.max_slots) bad = QC_ERR_INVALID_ARG;
   }
-  if (bad) {
-    if (threadIdx.x == 0) atomicMax(&T.state[1], bad);
+  if (bad) {      // (every block finds the same)
+    if (thread == 0) atomicMax(&T.state[1], bad);
     if (!TRIM) {
-      for (int i = threadIdx.x; i <= n_seqs; i += blockDim.x) T.starts[i] = 0;
-      if (T.max_slots <= kSlotsInBlock)
-        for (int i = threadIdx.x; i < T.max_slots; i += blockDim.x) T.slots[i] = -1;
+      for (int i = thread; i <= n_seqs; i += n_threads) T.starts[i] = 0;
+      for (int i = thread; i < T.max_slots; i += n_threads) T.slots[i] = -1;
     }
     return;
   }
+  if (gridDim.x > 1) cluster_barrier();      // all have read
+  const int32_t n_moved = static_cast<int32_t>(all.pages), n_tokens = static_cast<int32_t>(all.tokens);
   // pages, in one row over all sequences
-  for (int k = threadIdx.x; k < static_cast<int>(pages_total); k += blockDim.x) {
-    const int i = last_not_above(first, n_seqs, k);
-    const int32_t id = T.ids ? T.ids[i] : i;
-    int32_t* entry = T.pages + static_cast<size_t>(id) * T.max_pages + keep[i] + (k - first[i]);
+  for (int k = thread; k < n_moved; k += n_threads) {
+    const Seq s = seqs[last_not_above<true>(seqs, n_seqs, k)];
+    const int32_t stay = ((TRIM ? s.start : s.len) + up) >> shift;
+    int32_t* entry = T.pages + static_cast<size_t>(s.id) * T.max_pages + stay + (k - s.first);
     if (TRIM) {
-      T.free[n_free + static_cast<int>(pages_total) - 1 - k] = *entry;
+      T.free[n_free + n_moved - 1 - k] = *entry;
       *entry = -1;
     } else {
       *entry = T.free[n_free - 1 - k];
     }
   }
-  for (int i = threadIdx.x; i < n_seqs; i += blockDim.x) {
-    const int32_t id = T.ids ? T.ids[i] : i;
+  for (int i = thread; i < n_seqs; i += n_threads) {
+    const Seq s = seqs[i];
     if (TRIM) {
-      const int32_t count = T.count ? T.count[i] : 0;
-      if (count < T.lens[id]) T.lens[id] = count;
+      if (s.start != s.len) T.lens[s.id] = s.start;
     } else {
-      T.lens[id] += T.count ? T.count[i] : 1;
-      T.starts[i] = start[i];
+      T.lens[s.id] = s.len + (T.count ? T.count[i] : 1);
+      T.starts[i] = s.start;
     }
   }
-  if (threadIdx.x == 0) {
-    T.state[0] = n_free + static_cast<int32_t>(TRIM ? pages_total : -pages_total);
-    if (!TRIM) T.starts[n_seqs] = static_cast<int32_t>(tokens_total);
+  if (thread == 0) {
+    T.state[0] = n_free + (TRIM ? n_moved : -n_moved);
+    if (!TRIM) T.starts[n_seqs] = n_tokens;
   }
-  if (TRIM || T.max_slots > kSlotsInBlock) return;
-  __syncthreads();   // this block wrote the pages and lengths that the slots are made from
-  for (int i = threadIdx.x; i < T.max_slots; i += blockDim.x) {
-    int32_t slot = -1;
-    if (i < tokens_total) {
-      const int seq = last_not_above(start, n_seqs, i);
-      slot = slot_of(T, seq, T.lens[T.ids ? T.ids[seq] : seq], seq + 1 < n_seqs ? start[seq + 1] : static_cast<int32_t>(tokens_total), i);
-    }
-    T.slots[i] = slot;
+  if (TRIM) return;
+  // slots: a page that was there is in the table, one that is new among the free ones (which stay as they are)
+  const auto slot_of = [&](int i, const Seq& s) {
+    const int32_t pos = s.len + (i - s.start), page = pos >> shift, have = (s.len + up) >> shift;
+    const int32_t id = page < have ? T.pages[static_cast<size_t>(s.id) * T.max_pages + page] : T.free[n_free - 1 - s.first - (page - have)];
+    return (id << shift) + (pos & up);
+  };
+  if (gridDim.x == 1) {
+    for (int i = thread; i < T.max_slots; i += n_threads) T.slots[i] = i < n_tokens ? slot_of(i, seqs[last_not_above<false>(seqs, n_seqs, i)]) : -1;
+    return;
   }
-}
-
-// The slots of a long call, from what table_kernel has left (no tokens where it refused).
-__global__ void __launch_bounds__(256) slots_kernel(const TableArgs T) {
-  pdl_wait();
-  const int32_t total = T.starts[T.n_seqs];
-  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < T.max_slots; i += gridDim.x * blockDim.x) {
-    int32_t slot = -1;
-    if (i < total) {
-      const int seq = last_not_above(T.starts, T.n_seqs, i);
-      slot = slot_of(T, seq, T.lens[T.ids ? T.ids[seq] : seq], T.starts[seq + 1], i);
+  const int lane = threadIdx.x & 31;
+  for (int run = thread >> 5; run * (32 * kRun) < T.max_slots; run += n_threads >> 5) {
+    int i = run * (32 * kRun) + lane, seq = i < n_tokens ? last_not_above<false>(seqs, n_seqs, i) : 0;
+#pragma unroll
+    for (int k = 0; k < kRun; ++k, i += 32) {
+      if (i < n_tokens)
+        while (seq + 1 < n_seqs && seqs[seq + 1].start <= i) ++seq;
+      if (i < T.max_slots) T.slots[i] = i < n_tokens ? slot_of(i, seqs[seq]) : -1;
     }
-    T.slots[i] = slot;
   }
 }
 
@@ -216,7 +229,8 @@ int32_t check_table(const qc_table* t, TableArgs& a) {
     if (reinterpret_cast<uintptr_t>(p) & 3) return QC_ERR_INVALID_ARG;
   a = TableArgs{};
   a.pages = t->pages_dev, a.lens = t->lens_dev, a.free = t->free_dev, a.state = t->state_dev;
-  a.max_seqs = t->max_seqs, a.max_pages = t->max_pages, a.page = t->page_size, a.n_pages = t->n_pages;
+  a.max_seqs = t->max_seqs, a.max_pages = t->max_pages, a.n_pages = t->n_pages;
+  a.page_shift = t->page_size == 16 ? 4 : t->page_size == 32 ? 5 : 6;
   return QC_OK;
 }
 
@@ -227,7 +241,26 @@ int32_t check_batch(const TableArgs& a, int32_t n_seqs, const int32_t* ids, cons
   return QC_OK;
 }
 
-int threads_for(int32_t n) { return n <= 256 ? 256 : n <= 512 ? 512 : 1024; }
+// One block of as many threads as there is work for, or a cluster; behind the launch before it, whose end it waits for.
+template <bool TRIM>
+int32_t launch_table(const TableArgs& a, bool many, void* cuda_stream) {
+  const size_t smem = static_cast<size_t>(a.n_seqs) * sizeof(Seq) + (a.ids ? (a.max_seqs + 31) / 32 * 4 : 0);
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
+  const int32_t work = a.max_slots > a.n_seqs ? a.max_slots : a.n_seqs;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(many ? kCluster : 1);
+  cfg.blockDim = dim3(many || work > 512 ? 1024 : work > 256 ? 512 : 256);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = static_cast<cudaStream_t>(cuda_stream);
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = many ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, table_kernel<TRIM>, a) == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+}
 
 }  // namespace
 }  // namespace qc
@@ -256,16 +289,7 @@ extern "C" int32_t qc_table_extend(int32_t device, void* cuda_stream, const qc_t
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   a.n_seqs = n_seqs, a.ids = seq_ids_dev, a.count = n_new_dev, a.starts = starts_dev, a.slots = slots_dev, a.max_slots = max_slots;
-  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const size_t smem = static_cast<size_t>(n_seqs) * 12 + (seq_ids_dev ? (a.max_seqs + 31) / 32 * 4 : 0);
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
-  const int32_t work = max_slots <= kSlotsInBlock && max_slots > n_seqs ? max_slots : n_seqs;
-  if (launch_pdl(table_kernel<false>, dim3(1), dim3(threads_for(work)), smem, stream, a) != cudaSuccess) return QC_ERR_CUDA;
-  if (max_slots > kSlotsInBlock) {
-    const int blocks = max_slots / 256 + 1 < 1184 ? max_slots / 256 + 1 : 1184;
-    if (launch_pdl(slots_kernel, dim3(blocks), dim3(256), 0, stream, a) != cudaSuccess) return QC_ERR_CUDA;
-  }
-  return QC_OK;
+  return launch_table<false>(a, max_slots >= kManySlots, cuda_stream);
 }
 
 extern "C" int32_t qc_table_trim(int32_t device, void* cuda_stream, const qc_table* table, int32_t n_seqs, const int32_t* seq_ids_dev,
@@ -276,7 +300,6 @@ extern "C" int32_t qc_table_trim(int32_t device, void* cuda_stream, const qc_tab
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   a.n_seqs = n_seqs, a.ids = seq_ids_dev, a.count = n_keep_dev;
-  const size_t smem = static_cast<size_t>(n_seqs) * 8 + (seq_ids_dev ? (a.max_seqs + 31) / 32 * 4 : 0);
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
-  return launch_pdl(table_kernel<true>, dim3(1), dim3(threads_for(n_seqs)), smem, static_cast<cudaStream_t>(cuda_stream), a) == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  // a release may give back every page of its rows; drafts that are turned down give back a few
+  return launch_table<true>(a, !n_keep_dev && static_cast<int64_t>(n_seqs) * a.max_pages >= kManySlots, cuda_stream);
 }
