@@ -379,6 +379,7 @@ int32_t qc_attend_static(int32_t device, void* cuda_stream, const void* q_dev, c
 #define QC_TABLE_MAX_BATCH 4096   /* sequences listed in one call */
 #define QC_TABLE_MAX_SEQS 65536   /* rows of a page table */
 #define QC_QUANT_MAX_HEADS 1024
+#define QC_QUANT_MAX_SEQS 2048    /* sequences in one qc_quant_attend */
 #define QC_QUANT_MAX_QUERIES 16   /* query tokens of one sequence in one qc_quant_attend */
 
 /* Page table of one stream, all arrays int32 on the device. */

@@ -328,6 +328,7 @@ def qc_attend_static(device: int, cuda_stream: int, q_ptr: int, k_ptr: int, v_pt
 QC_TABLE_MAX_BATCH = 4096
 QC_TABLE_MAX_SEQS = 65536
 QC_QUANT_MAX_HEADS = 1024
+QC_QUANT_MAX_SEQS = 2048
 QC_QUANT_MAX_QUERIES = 16
 
 

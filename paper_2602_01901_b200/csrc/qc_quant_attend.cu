@@ -13,6 +13,10 @@
 // Products are m16n8k16 with the keys (for K) and the elements (for V) as rows and up to eight query rows as columns:
 // the heads of a group times the sequence's queries.  The pages are laid out for this (qc_quant.cuh): a lane's operands
 // are whole 16-byte vectors, and a product's scores become the next one's weights by two transposes in registers.
+// With four query rows or fewer the eight columns hold them twice, with two or one four times.  Every lane then has the
+// scores of all four blocks of a tile for the same rows, and weighs one half or one quarter of them: each set of columns sums up
+// its own blocks, and the sets are put together like the sums of different warps.  (One row, eight sequences of 8 541
+// tokens: XX us with eight columns of which one counts, YY so.)
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -26,9 +30,11 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kAttWarps = 4;
+template <int NT>
+constexpr int kWarpsOf = NT == 1 ? 12 : 8;   // of a block, one per SM: what 168 or 255 registers a thread leave room for
 constexpr int kUnitCost = 2;         // what a unit costs each warp besides its tiles, in tiles
-constexpr uint32_t kLongUnit = 64;   // tiles of the average unit from which on teams have eight warps
+constexpr uint32_t kLongUnit = 512;   // tiles of the average unit from which on teams have eight warps
+constexpr uint32_t kFewTiles = 6;
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
 constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
 
@@ -122,7 +128,7 @@ struct Query {
 // Row r of a unit is query r / group of the sequence, head r % group of the KV head.
 __device__ __forceinline__ int query_of(const AttendArgs& A, int r) { return static_cast<int>((static_cast<float>(r) + 0.5f) * A.inv_group); }
 
-template <int D, int NT>
+template <int D, int NT, int REP>
 __device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A, const StreamArgs& S, int64_t token0, int head0, int row0,
                                            int n_rows, int lane) {
   const int g = lane >> 2, t = lane & 3;
@@ -130,7 +136,7 @@ __device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A,
   uint32_t top = 0;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + nt * 8 + g, query = query_of(A, r);
+    const int r = row0 + nt * 8 + g % (8 / REP), query = query_of(A, r);
     const bool on = r < n_rows;
     const uint16_t* q = S.q + (token0 + query) * S.q_stride + static_cast<int64_t>(head0 + r - query * A.group) * D + t * (D / 4);
 #pragma unroll
@@ -182,15 +188,14 @@ __device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A,
 
 // ---- tiles on their way -------------------------------------------------------------------------------
 //
-// A warp fetches its tiles into a ring of its own: three places for the codes of a tile of K or of V, in the order K, V,
-// K, V, ..., so that while one is worked on the next two are on their way, and two places for the parameters
-// (K's, then V's) of a tile, which come with its K.  A lane's 16-byte copies are the vectors that it reads later itself;
-// the parameters are read by other lanes.
+// A warp fetches its tiles into a ring of its own: two places for the codes of K's tiles and two for V's, and two for the
+// parameters (K's, then V's) of a tile, which come with its K.  A lane's 16-byte copies are the vectors that it reads
+// later itself; the parameters are read by other lanes.
 template <int D>
 struct Ring {
   static constexpr int kCodes = kTile * D / 2;
   static constexpr int kParams = kTile * 8;
-  static constexpr int kBytes = 3 * kCodes + 2 * kParams;
+  static constexpr int kBytes = 4 * kCodes + 2 * kParams;
 };
 
 // A run: adjacent tiles of one stream, kBatch of which a lane's worth of page ids covers.
@@ -244,38 +249,26 @@ __device__ __forceinline__ void fetch_values(const StreamArgs& S, const Batch& b
 
 // ---- a tile -----------------------------------------------------------------------------------------------
 
-// The products of a tile of K with the queries: c[b][nt], for the lane's even token of block b (0, 1: columns 2 t, 2 t + 1)
-// and its odd one (2, 3), times 2^-24.
+// The products of block b of a tile of K with the queries: c[nt] for the lane's even token (0, 1: columns 2 t, 2 t + 1) and
+// its odd one (2, 3), times 2^-24.
 template <int D, int NT>
-__device__ __forceinline__ void score_tile(float (&c)[kTile / 16][NT][4], const Query<D, NT>& Q, uint32_t codes, int lane) {
-  constexpr int kPair = 2;      // blocks side by side: each one's products wait for one another
+__device__ __forceinline__ void score_block(float (&c)[NT][4], const Query<D, NT>& Q, uint32_t codes, int b, int lane) {
+  uint32_t x[D / 16];      // the words of the even token, then of the odd one
 #pragma unroll
-  for (int b0 = 0; b0 < kTile / 16; b0 += kPair) {
-    uint32_t x[kPair][D / 16];      // the words of the even token, then of the odd one
-#pragma unroll
-    for (int b = 0; b < kPair; ++b) {
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const uint4 k = lds128(codes + (b0 + b) * (8 * D) + i * 512 + lane * 16);
-        x[b][4 * i] = k.x, x[b][4 * i + 1] = k.y, x[b][4 * i + 2] = k.z, x[b][4 * i + 3] = k.w;
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) c[b0 + b][nt][0] = c[b0 + b][nt][1] = c[b0 + b][nt][2] = c[b0 + b][nt][3] = 0.f;
-    }
-#pragma unroll
-    for (int w = 0; w < D / 32; ++w)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int b = 0; b < kPair; ++b) {
-          const uint32_t xe = x[b][w] >> (8 * h), xo = x[b][D / 32 + w] >> (8 * h);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            float(&s)[4] = c[b0 + b][nt];
-            mma_f16_16816(s, xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1]);
-          }
-        }
+  for (int i = 0; i < D / 64; ++i) {
+    const uint4 k = lds128(codes + b * (8 * D) + i * 512 + lane * 16);
+    x[4 * i] = k.x, x[4 * i + 1] = k.y, x[4 * i + 2] = k.z, x[4 * i + 3] = k.w;
   }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) c[nt][0] = c[nt][1] = c[nt][2] = c[nt][3] = 0.f;
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t xe = x[w] >> (8 * h), xo = x[D / 32 + w] >> (8 * h);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_f16_16816(c[nt], xe & kLower, xo & kLower, xe & kUpper, xo & kUpper, Q.b[nt][2 * w + h][0], Q.b[nt][2 * w + h][1]);
+    }
 }
 
 __device__ __forceinline__ float step_of(uint32_t params) {
@@ -310,18 +303,26 @@ __device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, float sc
 }
 
 // Weights of a tile's scores, as operands of the value products.  `rows`: what rows_of found, in shared memory; `top`: the
-// largest step that this lane saw.  `masked`: the tile has keys that are not there, or that some column does not see; `left` keys are there from its first
-// on, `back` of them are behind the unit's first query.
-template <int D, int NT>
-__device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16][NT][4], uint32_t (&w)[kTile / 16][NT][2], const Query<D, NT>& Q,
+// largest step that this lane saw.  `masked`: the tile has keys that are not there, or that some column does not see;
+// `left` keys are there from its first on, `back` of them are behind the unit's first query.
+template <int D, int NT, int REP>
+__device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, const float (&scores)[kTile / 16][NT][4], uint32_t (&w)[kTile / 16][NT][2], const Query<D, NT>& Q,
                                            uint32_t rows, float top, uint32_t on, const AttendArgs& A, int left, int row0, int back, bool masked, int lane) {
-  constexpr int kBlocks = kTile / 16;
-  const int g = lane >> 2;
+  constexpr int kMine = kTile / 16 / REP;      // blocks that this lane weighs
+  const int g = lane >> 2, t = lane & 3;
+  const int first = REP == 1 ? 0 : REP == 2 ? t & 2 : t;
+  float c[kMine][NT][4];
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b) {
-    const float4 k = lds_f4(rows + b * 128 + g * 16);
+  for (int b = 0; b < kMine; ++b) {
+    const float4 k = lds_f4(rows + (first + b) * 128 + g * 16);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if constexpr (REP == 1) c[b][nt][x] = scores[b][nt][x];
+        else if constexpr (REP == 2) c[b][nt][x] = first ? scores[2 + b][nt][x] : scores[b][nt][x];
+        else c[b][nt][x] = t & 2 ? (t & 1 ? scores[3][nt][x] : scores[2][nt][x]) : (t & 1 ? scores[1][nt][x] : scores[0][nt][x]);
+      }
       c[b][nt][0] = fmaf(k.x, c[b][nt][0], fmaf(k.y, Q.sum[nt][0], -R.ref[nt][0]));
       c[b][nt][1] = fmaf(k.x, c[b][nt][1], fmaf(k.y, Q.sum[nt][1], -R.ref[nt][1]));
       c[b][nt][2] = fmaf(k.z, c[b][nt][2], fmaf(k.w, Q.sum[nt][0], -R.ref[nt][0]));
@@ -334,12 +335,12 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         // keys of the tile that the column sees
-        const int seen = left - max(0, back - query_of(A, row0 + nt * 8 + 2 * (lane & 3) + x));
+        const int seen = left - max(0, back - query_of(A, row0 + nt * 8 + (2 * t + x) % (8 / REP)));
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+        for (int b = 0; b < kMine; ++b)
 #pragma unroll
           for (int i = 0; i < 2; ++i)
-            if (!(on >> b & 1u) || 16 * b + 2 * g + i >= seen) c[b][nt][2 * i + x] = -INFINITY;
+            if (!(on >> (first + b) & 1u) || 16 * (first + b) + 2 * g + i >= seen) c[b][nt][2 * i + x] = -INFINITY;
       }
   }
   // scores above what they are relative to, or larger steps than before: everything so far is put on a new reference
@@ -351,7 +352,7 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
     for (int x = 0; x < 2; ++x) {
       float h = fmaxf(c[0][nt][x], c[0][nt][x + 2]);
 #pragma unroll
-      for (int b = 1; b < kBlocks; ++b) h = max3(h, c[b][nt][x], c[b][nt][x + 2]);
+      for (int b = 1; b < kMine; ++b) h = max3(h, c[b][nt][x], c[b][nt][x + 2]);
       high[nt][x] = h;
       more |= h > 0.f;
     }
@@ -383,14 +384,15 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
 #pragma unroll
         for (int mb = 0; mb < D / 16; ++mb) R.acc[nt][mb][x] *= f, R.acc[nt][mb][x + 2] *= f;
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b) c[b][nt][x] -= delta, c[b][nt][x + 2] -= delta;
+        for (int b = 0; b < kMine; ++b) c[b][nt][x] -= delta, c[b][nt][x + 2] -= delta;
       }
     R.all_seen = __all_sync(0xffffffffu, all);
   }
   const float up = __uint_as_float(((127u + 127u + 15u) << 23) - R.step);      // 2^15 / step: the largest weight is 2^15
+  uint32_t h[kMine][NT][2];
 #pragma unroll
-  for (int b = 0; b < kBlocks; ++b) {
-    const float4 v = lds_f4(rows + kTile * 8 + b * 128 + g * 16);
+  for (int b = 0; b < kMine; ++b) {
+    const float4 v = lds_f4(rows + kTile * 8 + (first + b) * 128 + g * 16);
     const float u0 = v.x * up, u1 = v.z * up, mid[2] = {v.y, v.w};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -407,14 +409,26 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, float (&c)[kTile / 16
 #pragma unroll
         for (int x = 0; x < 4; ++x) R.z[nt][x & 1] = fmaf(p[x], p[x] == 0.f ? 0.f : mid[x >> 1], R.z[nt][x & 1]);
       }
-      w[b][nt][0] = transpose_8x8(pack_f16x2(p[0] * u0, p[1] * u0));
-      w[b][nt][1] = transpose_8x8(pack_f16x2(p[2] * u1, p[3] * u1));
+      h[b][nt][0] = pack_f16x2(p[0] * u0, p[1] * u0);
+      h[b][nt][1] = pack_f16x2(p[2] * u1, p[3] * u1);
+      if constexpr (REP == 1) w[b][nt][0] = transpose_8x8(h[b][nt][0]), w[b][nt][1] = transpose_8x8(h[b][nt][1]);
     }
   }
+  if constexpr (REP == 1) return;
+  // a block's weights in the columns of the lanes that weighed it, 0 in the others
+#pragma unroll
+  for (int b = 0; b < kTile / 16; ++b)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[b][nt][i] = transpose_8x8(b / kMine == (REP == 2 ? t >> 1 : t) ? h[b % kMine][nt][i] : 0u);
 }
 
-template <int D, int NT>
-__device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[kTile / 16][NT][2], uint32_t codes, int lane) {
+// The values of a tile, and the scores of the next one (NEXT), side by side: neither waits for the other, and what one warp
+// does between its tiles is a chain otherwise.
+template <int D, int NT, bool NEXT>
+__device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[kTile / 16][NT][2], uint32_t codes, float (&c)[kTile / 16][NT][4],
+                                           const Query<D, NT>& Q, uint32_t next_codes, int lane) {
   constexpr int kBlocks = kTile / 16;
   // - 8 * the weights' sums, of even elements' codes, and of odd ones' (which are 16 times as large)
   float less[NT][4];
@@ -435,6 +449,11 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
     }
 #pragma unroll
     for (int j0 = 0; j0 < 4; j0 += 2) {
+      if constexpr (NEXT) {
+        constexpr int kShare = kBlocks / (D / 32);
+#pragma unroll
+        for (int b = 0; b < kShare; ++b) score_block<D, NT>(c[(2 * i + j0 / 2) * kShare + b], Q, next_codes, (2 * i + j0 / 2) * kShare + b, lane);
+      }
       float sum[2][NT][4];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
@@ -460,7 +479,7 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
 // ---- the batch's work as one row -------------------------------------------------------------------------
 //
 // Sequence after sequence, unit after unit (KV head, then rows of queries), tile after tile (the visual stream's, then the
-// text's).  The row is cut into ranges of equal cost, one per team of 1, 2, 4 or 8 warps, so that the teams end together
+// text's).  The row is cut into ranges of equal cost, one per team of 1, 2, 4 or all warps of a block, so that the teams end together
 // whatever the lengths are; the warps of a team share out a unit's tiles.  A unit costs its tiles and kUnitCost more for
 // every warp of the team.  A unit inside one range is finished there; of one that reaches over a border each team leaves
 // its sums, a piece, and raises the piece's flag.  Then it looks at the flags of the unit's other pieces: the team that
@@ -511,20 +530,27 @@ __device__ __forceinline__ Place place_of(const AttendArgs& A, int seq, bool rep
 // no numbers.
 __device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : exp2f(ms - m); }
 
-// Adds a piece (reference and sum, elements) to a column's pieces so far.
-template <int D>
-__device__ __forceinline__ void add_piece(float& m, float& l, float (&o)[D / 32], float2 ml, const float (&v)[D / 32], bool first) {
-  if (first || l == 0.f) {
-    m = ml.x, l = ml.y;
+// Sums (reference, sum, elements) put on one reference, 32 at a time, one per lane.
+struct Joined {
+  float m = -INFINITY, l = 0.f;
+  // This lane's sum counts for what is returned; the elements so far are put on the new reference.
+  template <int N>
+  __device__ __forceinline__ float join(float2 ml, float (&o)[N]) {
+    float top = ml.x;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = v[i];
-  } else if (ml.y != 0.f) {
-    const float top = fmaxf(m, ml.x), f = weight_of(m, top), w = weight_of(ml.x, top);
-    m = top, l = fmaf(l, f, ml.y * w);
+    for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    top = fmaxf(top, m);
+    const float f = ml.y == 0.f ? 0.f : weight_of(ml.x, top), before = l == 0.f ? 0.f : weight_of(m, top);
+    float sum = ml.y * f;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(o[i], f, v[i] * w);
+    for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+    l = fmaf(l, before, sum);
+    m = top;
+#pragma unroll
+    for (int k = 0; k < N; ++k) o[k] *= before;
+    return f;
   }
-}
+};
 
 template <int D>
 __device__ __forceinline__ void write_row(const AttendArgs& A, size_t row, float m, float l, const float (&o)[D / 32], int lane) {
@@ -561,39 +587,54 @@ __device__ __forceinline__ void load_run(const float* p, float (&o)[D / 32], int
 }
 
 // A piece: columns of D elements, then (reference, sum) of each column.
-template <int D, int NT>
+template <int D, int ROWS>
 __device__ __forceinline__ float* piece_at(const AttendArgs& A, int team, int place) {
-  return A.part + (static_cast<size_t>(team) * 2 + place) * (8 * NT * (D + 2));
+  return A.part + (static_cast<size_t>(team) * 2 + place) * (ROWS * (D + 2));
 }
 
 // Puts the pieces of a unit together and writes its rows: columns member, member + warps, ...  Not inlined, so that the
 // loop over the tiles keeps its registers.
-template <int D, int NT>
+template <int D, int ROWS>
 __device__ __noinline__ void merge_pieces(const AttendArgs& A, uint32_t first_team, uint32_t last_team, uint32_t first_place, int member, int warps, int n_here,
                                           int row0, int64_t token0, int kvh, int lane) {
-          constexpr int kCols = 4;      // columns side by side: each one's pieces come one after the other
-          for (int col0 = member; col0 < n_here; col0 += kCols * warps) {
-            float m[kCols], l[kCols] = {}, o[kCols][D / 32];
-  #pragma unroll 2
-            for (uint32_t i = first_team; i <= last_team; ++i) {
-              const float* p = piece_at<D, NT>(A, i, i == first_team ? first_place : 0);
-              float2 ml[kCols];
-              float v[kCols][D / 32];
-  #pragma unroll
-              for (int k = 0; k < kCols; ++k) {
-                const int col = min(col0 + k * warps, n_here - 1);
-                ml[k] = __ldcg(reinterpret_cast<const float2*>(p + 8 * NT * D) + col);
-                load_run_l2<D>(p + col * D, v[k], lane);
-              }
-  #pragma unroll
-              for (int k = 0; k < kCols; ++k) add_piece<D>(m[k], l[k], o[k], ml[k], v[k], i == first_team);
-            }
-  #pragma unroll
-            for (int k = 0; k < kCols; ++k) {
-              const int col = col0 + k * warps, r = row0 + col, query = query_of(A, r);
-              if (col < n_here) write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, m[k], l[k], o[k], lane);
-            }
-          }
+          constexpr int kCols = 4;      // columns side by side: each one's sums are two trips to the L2 after one another
+  for (int col0 = member; col0 < n_here; col0 += kCols * warps) {
+    float o[kCols][D / 32] = {};
+    Joined J[kCols];
+    const auto col_of = [&](int c) { return min(col0 + c * warps, n_here - 1); };
+    for (uint32_t i0 = first_team; i0 <= last_team; i0 += 32) {
+      const uint32_t i = i0 + lane;
+      const int n = min(32u, last_team + 1 - i0);
+      float2 ml[kCols];
+      float f[kCols];
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        ml[c] = make_float2(-INFINITY, 0.f);
+        if (lane < n) ml[c] = __ldcg(reinterpret_cast<const float2*>(piece_at<D, ROWS>(A, i, i == first_team ? first_place : 0) + ROWS * D) + col_of(c));
+      }
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) f[c] = J[c].join(ml[c], o[c]);
+#pragma unroll 2
+      for (int k = 0; k < n; ++k) {
+        const float* piece = piece_at<D, ROWS>(A, i0 + k, i0 + k == first_team ? first_place : 0);
+        float v[kCols][D / 32];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) load_run_l2<D>(piece + col_of(c) * D, v[c], lane);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          const float fk = __shfl_sync(0xffffffffu, f[c], k);
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) o[c][j] = fmaf(v[c][j], fk, o[c][j]);
+        }
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      const int r = row0 + col0 + c * warps, query = query_of(A, r);
+      if (col0 + c * warps < n_here)
+        write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, J[c].m, J[c].l, o[c], lane);
+    }
+  }
 }
 
 __device__ __forceinline__ unsigned long long flag_of(const unsigned long long* p) {
@@ -607,16 +648,31 @@ __device__ __forceinline__ void team_barrier(int team, int threads) {
   else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory");
 }
 
-template <int D, int NT>
-__global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+// What a warp knows about its range and the unit it is at.  Kept in shared memory: it is looked at once a unit, and the
+// loop over the tiles has no registers to spare for it.
+struct Work {
+  int64_t token0;
+  int32_t n_rows, queries, row, len[2], tiles_v, tiles;                     // the sequence (Place)
+  int32_t kvh, row0, first, last;                                           // the unit, and its tiles that are in the range
+  uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
+  int32_t seq, whole_units;
+  uint32_t per, more, team;                                                 // cost of a range, of a unit besides its tiles
+  int32_t in_block, member, warps;                                          // the team's place in the block, the warp's in the team
+};
+
+template <int D, int NT, int REP>
+__global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
   using R_ = Ring<D>;
+  constexpr int kAttWarps = kWarpsOf<NT>;
   constexpr int kRow = D + 4;            // of a column's sums in shared memory
+  constexpr int kRows = 8 * NT / REP;    // query rows of a unit
   static_assert(8 * NT * kRow * 4 <= R_::kBytes, "a warp's sums take its ring's place");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ uint2 scan[kAttWarps];
   __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
   __shared__ uint32_t longest_;
   __shared__ int sm_all[kAttWarps];
+  __shared__ Work work_[kAttWarps];
   uint2* before = reinterpret_cast<uint2*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] tiles and units of the sequences before
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   pdl_wait();
@@ -630,7 +686,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
     uint32_t units = 0;
     if (i < A.n_seqs) {
       const Place u = place_of(A, i, blockIdx.x == 0);
-      units = A.hkv * ((u.n_rows + 8 * NT - 1) / (8 * NT));
+      units = A.hkv * ((u.n_rows + kRows - 1) / kRows);
       mine = static_cast<uint64_t>(u.tiles) * units;
       if (units) atomicMax(&longest_, static_cast<uint32_t>(u.tiles));
     }
@@ -652,7 +708,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
     if (i < A.n_seqs) before[i + 1] = make_uint2(static_cast<uint32_t>(total) + base.x + x, units_all + base.y + n);
     total += sum.x;
     units_all += sum.y;
-    if (any_big || total > (1u << 29)) {      // a batch of more than 2^35 rows
+    if (any_big || total > (1u << 26)) {      // a batch of more than 2^32 rows
       if (blockIdx.x == 0 && threadIdx.x == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
       total = 0;
       break;
@@ -662,50 +718,56 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
   const uint32_t tiles_all = static_cast<uint32_t>(total), units = total ? units_all : 0, longest = longest_;
   const uint32_t n_warps = gridDim.x * kAttWarps;
   uint32_t team_warps = 1;
-  if (tiles_all >= units * kLongUnit) team_warps = kAttWarps;
-  else
-    while (team_warps < kAttWarps && units * team_warps * 2 <= n_warps) team_warps *= 2;
-  const uint32_t n_teams = n_warps / team_warps;
-  const int threads = team_warps * 32, in_block = warp / team_warps, member = warp % team_warps, team0 = in_block * team_warps;
-  const uint32_t team = blockIdx.x * (kAttWarps / team_warps) + in_block;
-  const uint32_t more = kUnitCost * team_warps, cost = tiles_all + units * more;
+  if (tiles_all >= units * kLongUnit || units * kAttWarps <= n_warps) team_warps = kAttWarps;
+  else if (tiles_all <= n_warps * kFewTiles) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
+  const uint32_t n_teams = n_warps / team_warps, more = kUnitCost * team_warps, cost = tiles_all + units * more;
+  uint32_t per_team = (cost + n_teams - 1) / n_teams;
+  const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
+  if (!whole_units) per_team = max(per_team, team_warps + more);
   const auto before_cost = [&](int s) { return before[s].x + before[s].y * more; };
-  uint32_t per = (cost + n_teams - 1) / n_teams;
-  const bool whole_units = longest <= max(team_warps * kWholeTiles, per / 8);
-  if (!whole_units) per = max(per, team_warps + more);
-  uint32_t at = min(static_cast<uint64_t>(team) * per, static_cast<uint64_t>(cost));
-  const uint32_t end = min(cost, at + per);
-  if (at >= end) return;
-  int seq = 0;
-  {   // the last sequence that begins at or before the range
-    int lo = 0, hi = A.n_seqs - 1;
+  volatile Work& W = work_[warp];
+  if (lane == 0) {
+    W.in_block = warp / team_warps, W.member = warp % team_warps, W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
+    W.team = blockIdx.x * (kAttWarps / team_warps) + W.in_block;
+    const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team, static_cast<uint64_t>(cost));
+    W.at = at, W.end = min(cost, at + per_team);
+    int lo = 0, hi = A.n_seqs - 1;      // the last sequence that begins at or before the range
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (before_cost(mid) <= at) lo = mid;
       else hi = mid - 1;
     }
-    seq = lo;
+    W.seq = lo;
   }
+  __syncwarp();
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
-  while (at < end) {
-    while (before_cost(seq + 1) <= at) ++seq;
-    const Place u = place_of(A, seq, false);
-    const int row_tiles = (u.n_rows + 8 * NT - 1) / (8 * NT), unit_cost = u.tiles + more;
-    const uint32_t seq_at = before_cost(seq);
-    int unit = (at - seq_at) / unit_cost, first = 0, last = u.tiles;
-    uint32_t unit_at = seq_at + unit * unit_cost;
-    if (whole_units) {
-      if (unit_at < at) {      // it begins before the range: the next one
-        at = unit_at + unit_cost;
-        continue;
+  while (W.at < W.end) {
+    {   // the next unit: every warp of the team finds the same
+      const uint32_t at = W.at, more = W.more;
+      int seq = W.seq;
+      while (before[seq + 1].x + before[seq + 1].y * more <= at) ++seq;
+      const Place u = place_of(A, seq, false);
+      const int row_tiles = (u.n_rows + kRows - 1) / kRows, unit_cost = u.tiles + more;
+      const uint32_t seq_at = before[seq].x + before[seq].y * more;
+      const int unit = (at - seq_at) / unit_cost;
+      const uint32_t unit_at = seq_at + unit * unit_cost;
+      int first = 0, last = u.tiles;
+      if (W.whole_units) {
+        if (unit_at < at) last = 0;      // it begins before the range: the next one
+      } else {
+        first = max(0, static_cast<int>(at - unit_at) - static_cast<int>(more));
+        last = min(u.tiles, static_cast<int>(W.end - unit_at) - static_cast<int>(more));
       }
-    } else {
-      first = max(0, static_cast<int>(at - unit_at) - static_cast<int>(more));
-      last = min(u.tiles, static_cast<int>(end - unit_at) - static_cast<int>(more));
+      __syncwarp();
+      if (lane == 0) {
+        W.seq = seq, W.at = unit_at + unit_cost, W.unit_at = unit_at, W.first = first, W.last = last;
+        W.kvh = unit / row_tiles, W.row0 = (unit - W.kvh * row_tiles) * kRows;
+        W.token0 = u.token0, W.n_rows = u.n_rows, W.queries = u.queries, W.row = u.row, W.len[0] = u.len[0], W.len[1] = u.len[1];
+        W.tiles_v = u.tiles_v, W.tiles = u.tiles;
+      }
+      __syncwarp();
+      if (first >= last) continue;
     }
-    at = unit_at + unit_cost;
-    if (first >= last) continue;
-    const int kvh = unit / row_tiles, row0 = (unit - kvh * row_tiles) * (8 * NT);
 
     Rows<D, NT> R;
 #pragma unroll
@@ -720,72 +782,83 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
     R.all_seen = false;
 
     // this warp's tiles of the unit, adjacent ones: a run in each stream
-    const int mine0 = first + (last - first) * member / static_cast<int>(team_warps), mine1 = first + (last - first) * (member + 1) / static_cast<int>(team_warps);
 #pragma unroll 1
     for (int now = 1; now >= 0; --now) {
-      const int shift = now ? 0 : u.tiles_v;      // the stream's first tile in the unit
-      const int run = max(mine0, shift) - shift, stop = (now ? min(mine1, u.tiles_v) : mine1) - shift;
+      const int first = W.first, n = W.last - first, member = W.member, warps = W.warps, tiles_v = W.tiles_v;
+      const int mine0 = first + n * member / warps, mine1 = first + n * (member + 1) / warps;
+      const int shift = now ? 0 : tiles_v;      // the stream's first tile in the unit
+      const int run = max(mine0, shift) - shift, stop = (now ? min(mine1, tiles_v) : mine1) - shift;
       if (run >= stop) continue;
       const StreamArgs& S = A.stream[now];
-      const int len = now ? u.len[1] : u.len[0], back = now || !A.causal ? 0 : u.queries - 1;
-      const int32_t* table = S.pages + static_cast<size_t>(u.row) * S.max_pages;
+      const int len = W.len[now], back = now || !A.causal ? 0 : W.queries - 1, kvh = W.kvh;
+      const int32_t* table = S.pages + static_cast<size_t>(W.row) * S.max_pages;
+      // the next tile to ask for: its batch's first tile, the batch, and the next batch's page ids
+      int asked = run, at_tile = run;
       Batch batch = batch_of<D>(A, S, ask_ids(A, table, run, len, lane), kvh, run, len, lane);
-      int at_tile = run;       // the batch's first tile
-      const uint32_t params = ring + 3 * R_::kCodes;
-      fetch_keys<D>(S, batch, 0, ring, params, lane);
-      cp_async_commit_group();
-      fetch_values<D>(S, batch, 0, ring + R_::kCodes, lane);
-      cp_async_commit_group();
-      int32_t ids = ask_ids(A, table, run + kBatch, len, lane);      // of the next batch
-      uint32_t there = __ballot_sync(0xffffffffu, batch.there);
-      Query<D, NT> Q;
-      load_query<D, NT>(Q, A, S, u.token0, kvh * A.group, row0, u.n_rows, lane);
-      int slot = 0, par = 0;
-      for (int tile = run; tile < stop; ++tile) {
-        const uint32_t on = there >> ((tile - at_tile) * 4) & 15u;
-        const int slot1 = slot == 2 ? 0 : slot + 1, slot2 = slot == 0 ? 2 : slot - 1;
-        const bool more_tiles = tile + 1 < stop;
-        if (tile + 1 - at_tile == kBatch) {
+      int32_t ids = ask_ids(A, table, run + kBatch, len, lane);
+      uint32_t there = 0;      // blocks that are there of the next two tiles and the two behind them, 4 bits a tile
+      const uint32_t params = ring + 4 * R_::kCodes;
+      const auto ask_keys = [&]() {       // of tile `asked`
+        if (asked < stop) {
+          const int at = (asked - at_tile) * 4;
+          there |= (__ballot_sync(0xffffffffu, batch.there) >> at & 15u) << ((asked & 3) * 4);
+          fetch_keys<D>(S, batch, at, ring + (asked & 1) * R_::kCodes, params + (asked & 1) * R_::kParams, lane);
+        }
+        cp_async_commit_group();
+      };
+      const auto ask_values = [&]() {      // of the same tile; then the next one's turn
+        if (asked < stop) fetch_values<D>(S, batch, (asked - at_tile) * 4, ring + (2 + (asked & 1)) * R_::kCodes, lane);
+        cp_async_commit_group();
+        if (++asked - at_tile == kBatch) {
           at_tile += kBatch;
           batch = batch_of<D>(A, S, ids, kvh, at_tile, len, lane);
-          there = __ballot_sync(0xffffffffu, batch.there);
           ids = ask_ids(A, table, at_tile + kBatch, len, lane);
         }
-        const int at_next = (tile + 1 - at_tile) * 4;
-        if (more_tiles) fetch_keys<D>(S, batch, at_next, ring + slot2 * R_::kCodes, params + (par ^ 1) * R_::kParams, lane);      // the place of the V before
-        cp_async_commit_group();
+      };
+      ask_keys();
+      ask_values();
+      ask_keys();
+      ask_values();
+      Query<D, NT> Q;
+      load_query<D, NT, REP>(Q, A, S, W.token0, kvh * A.group, W.row0, W.n_rows, lane);
+      float c[kTile / 16][NT][4];
+      cp_async_wait_group<3>();
+      __syncwarp();
+#pragma unroll
+      for (int b = 0; b < kTile / 16; ++b) score_block<D, NT>(c[b], Q, ring + (run & 1) * R_::kCodes, b, lane);
+      for (int tile = run; tile < stop; ++tile) {
+        const uint32_t on = there >> ((tile & 3) * 4) & 15u;
+        there &= ~(15u << ((tile & 3) * 4));
         const int left = len - tile * kTile;
         const bool masked = left - back < kTile || on != 15u;
-        const uint32_t scratch = ring + slot * R_::kCodes;      // K's place, once its codes are read
-        float c[kTile / 16][NT][4];
+        const uint32_t scratch = ring + (tile & 1) * R_::kCodes;      // K's place: its codes have been read
         uint32_t w[kTile / 16][NT][2];
-        cp_async_wait_group<2>();
-        __syncwarp();
-        score_tile<D, NT>(c, Q, scratch, lane);
-        __syncwarp();
         float top;
+        __syncwarp();
         {
           RowValues rows;
-          top = rows_of(rows, params + par * R_::kParams, Q.scale, on, left, masked, lane);
+          top = rows_of(rows, params + (tile & 1) * R_::kParams, Q.scale, on, left, masked, lane);
           sts_f4(scratch + lane * 32, rows.v[0], rows.v[1]);
           sts_f4(scratch + lane * 32 + 16, rows.v[2], rows.v[3]);
         }
         __syncwarp();
-        weigh_tile<D, NT>(R, c, w, Q, scratch, top, on, A, left, row0, back, masked, lane);
+        weigh_tile<D, NT, REP>(R, c, w, Q, scratch, top, on, A, left, W.row0, back, masked, lane);
         __syncwarp();
-        if (more_tiles) fetch_values<D>(S, batch, at_next, scratch, lane);
-        cp_async_commit_group();
-        cp_async_wait_group<2>();
+        ask_keys();                  // two tiles on, in this one's places
+        cp_async_wait_group<2>();    // the next tile's keys, this one's values
         __syncwarp();
-        add_values<D, NT>(R, w, ring + slot1 * R_::kCodes, lane);
+        const uint32_t values = ring + (2 + (tile & 1)) * R_::kCodes, next = ring + ((tile + 1) & 1) * R_::kCodes;
+        if (tile + 1 < stop) add_values<D, NT, true>(R, w, values, c, Q, next, lane);
+        else add_values<D, NT, false>(R, w, values, c, Q, next, lane);
         __syncwarp();
-        slot = slot2;
-        par ^= 1;
+        ask_values();
       }
       cp_async_wait_all();
       __syncwarp();
     }
     // the team's sums meet in shared memory
+    const int n_rows = W.n_rows, row0 = W.row0, kvh = W.kvh, member = W.member, warps = W.warps, in_block = W.in_block, threads = warps * 32, team0 = in_block * warps;
+    const int64_t token0 = W.token0;
     const float unit_step = __uint_as_float(R.step) * (1.f / 32768.f);
     constexpr float kEven = 16777216.f, kOdd = 1048576.f;
     float* mine = reinterpret_cast<float*>(smem + warp * R_::kBytes);
@@ -798,7 +871,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
         for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o), z += __shfl_xor_sync(0xffffffffu, z, o);
         const int col = nt * 8 + 2 * t + x;
         if (g == 0) sm_m[warp][col] = R.seen >> (2 * nt + x) & 1u ? R.ref[nt][x] : -INFINITY, sm_l[warp][col] = l;
-        if (row0 + col < u.n_rows) {
+        if (row0 + col % kRows < n_rows) {
           float* dst = mine + col * kRow + g * (D / 8);
 #pragma unroll
           for (int mb = 0; mb < D / 16; mb += 2)
@@ -807,31 +880,39 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
         }
       }
     team_barrier(in_block, threads);
-    const int n_here = min(8 * NT, u.n_rows - row0);
-    const bool whole = first == 0 && last == u.tiles;
+    const int n_here = min(kRows, n_rows - row0);
+    const bool whole = W.first == 0 && W.last == W.tiles;
     // pieces: the first team's is its second one if a unit before this one ends in its range, all others are a team's first
-    const uint32_t first_team = whole ? team : (unit_at + more) / per, last_team = whole ? team : (unit_at + unit_cost - 1) / per;
+    const uint32_t team = W.team, per = W.per, unit_at = W.unit_at;
+    const uint32_t first_team = whole ? team : (unit_at + W.more) / per, last_team = whole ? team : (W.at - 1) / per;
     const uint32_t first_place = unit_at > first_team * per ? 1 : 0, place = team == first_team ? first_place : 0;
-    float* piece = piece_at<D, NT>(A, team, place);
-    for (int col = member; col < n_here; col += static_cast<int>(team_warps)) {
-      float m = -INFINITY, l = 0.f, o[D / 32] = {};
-      for (int w = team0; w < team0 + static_cast<int>(team_warps); ++w) m = fmaxf(m, sm_m[w][col]);
-      for (int w = team0; w < team0 + static_cast<int>(team_warps); ++w) {
-        if (sm_l[w][col] == 0.f) continue;
-        const float f = weight_of(sm_m[w][col], m);
-        l = fmaf(sm_l[w][col], f, l);
-        float v[D / 32];
-        load_run<D>(reinterpret_cast<const float*>(smem + w * R_::kBytes) + col * kRow, v, lane);
+    float* piece = piece_at<D, kRows>(A, team, place);
+    for (int col = member; col < n_here; col += warps) {
+      // the column's sums of every warp (and set of columns), each lane's weight first
+      float o[D / 32] = {};
+      Joined J;
+      const auto row_of = [&](int i) { return reinterpret_cast<const float*>(smem + (team0 + i / REP) * R_::kBytes) + (col + i % REP * kRows) * kRow; };
+      for (int i0 = 0; i0 < warps * REP; i0 += 32) {
+        const int i = i0 + lane, n = min(32, warps * REP - i0);
+        const float2 ml = lane < n ? make_float2(sm_m[team0 + i / REP][col + i % REP * kRows], sm_l[team0 + i / REP][col + i % REP * kRows]) : make_float2(-INFINITY, 0.f);
+        const float f = J.join(ml, o);
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+          const float fk = __shfl_sync(0xffffffffu, f, k);
+          float v[D / 32];
+          load_run<D>(row_of(i0 + k), v, lane);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] = fmaf(v[i], f, o[i]);
+          for (int j = 0; j < D / 32; ++j) o[j] = fmaf(v[j], fk, o[j]);
+        }
       }
+      const float m = J.m, l = J.l;
       if (whole) {
         const int r = row0 + col, query = query_of(A, r);
-        write_row<D>(A, static_cast<size_t>(u.token0 + query) * A.hq + kvh * A.group + r - query * A.group, m, l, o, lane);
+        write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, m, l, o, lane);
       } else {
         if constexpr (D == 128) reinterpret_cast<float4*>(piece + col * D)[lane] = make_float4(o[0], o[1], o[2], o[3]);
         else reinterpret_cast<float2*>(piece + col * D)[lane] = make_float2(o[0], o[1]);
-        if (lane == 0) reinterpret_cast<float2*>(piece + 8 * NT * D)[col] = make_float2(m, l);
+        if (lane == 0) reinterpret_cast<float2*>(piece + kRows * D)[col] = make_float2(m, l);
       }
     }
     if (!whole) {
@@ -848,12 +929,12 @@ __global__ void __launch_bounds__(kAttWarps * 32, NT == 1 ? 3 : 2) quant_attend_
       }
       team_barrier(in_block, threads);
       if (sm_all[in_block]) {
-        merge_pieces<D, NT>(A, first_team, last_team, first_place, member, static_cast<int>(team_warps), n_here, row0, u.token0, kvh, lane);
+        merge_pieces<D, kRows>(A, first_team, last_team, first_place, member, warps, n_here, row0, token0, kvh, lane);
         if (member == 0)
           for (uint32_t i = first_team + lane; i <= last_team; i += 32) A.flags[2 * i + (i == first_team ? first_place : 0)] = 0;
       }
     }
-    if (at < end) team_barrier(in_block, threads);      // the rings' places are free again
+    if (W.at < W.end) team_barrier(in_block, threads);      // the rings' places are free again
   }
 }
 
@@ -876,12 +957,16 @@ int32_t check_sizes(const qc_quant_attend_args* a) {
   if (a->page_size != 16 && a->page_size != 32 && a->page_size != 64) return QC_ERR_UNSUPPORTED;
   if (a->n_kv_heads < 1 || a->n_q_heads < 1 || a->n_q_heads % a->n_kv_heads || a->n_seqs < 1 || a->max_seqs < 1 || a->n_tokens < 0 || a->max_queries < 1)
     return QC_ERR_INVALID_ARG;
-  if (a->n_kv_heads > QC_QUANT_MAX_HEADS || a->n_q_heads > QC_QUANT_MAX_HEADS || a->n_seqs > QC_TABLE_MAX_BATCH || a->max_queries > QC_QUANT_MAX_QUERIES)
+  if (a->n_kv_heads > QC_QUANT_MAX_HEADS || a->n_q_heads > QC_QUANT_MAX_HEADS || a->n_seqs > QC_QUANT_MAX_SEQS || a->max_queries > QC_QUANT_MAX_QUERIES)
     return QC_ERR_UNSUPPORTED;
   return QC_OK;
 }
 
-int row_tile_of(const qc_quant_attend_args* a) { return a->max_queries * (a->n_q_heads / a->n_kv_heads) > 8 ? 2 : 1; }
+// query rows of a unit: as many columns of a product as they need
+int unit_rows(const qc_quant_attend_args* a) {
+  const int64_t rows = static_cast<int64_t>(a->max_queries) * (a->n_q_heads / a->n_kv_heads);
+  return rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+}
 
 constexpr int kMostTeams = 2560;   // of one warp each; the workspace is sized for it
 
@@ -896,26 +981,27 @@ unsigned long long next_nonce() {
   return x ? x : 1;
 }
 
-template <int D, int NT>
+template <int D, int NT, int REP>
 cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
+  constexpr int kAttWarps = kWarpsOf<NT>;
   const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
   static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
   cudaError_t e;
   if (device >= 64 || configured[device] < smem) {
-    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     if (device < 64) configured[device] = smem;
   }
   int sms = 0;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return e;
-  int blocks = sms * (NT == 1 ? 3 : 2);
+  int blocks = sms;
   if (blocks > kMostTeams / kAttWarps) blocks = kMostTeams / kAttWarps;
   A.nonce = next_nonce();
-  return launch_pdl(quant_attend_kernel<D, NT>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
+  return launch_pdl(quant_attend_kernel<D, NT, REP>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
 }
 
 size_t workspace_bytes(const qc_quant_attend_args* a) {
-  return kMostTeams * 2 * sizeof(unsigned long long) + static_cast<size_t>(kMostTeams) * 2 * 8 * row_tile_of(a) * (a->head_dim + 2) * 4;
+  return kMostTeams * 2 * sizeof(unsigned long long) + static_cast<size_t>(kMostTeams) * 2 * unit_rows(a) * (a->head_dim + 2) * 4;
 }
 
 }  // namespace
@@ -955,7 +1041,6 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   A.n_seqs = args->n_seqs, A.max_seqs = args->max_seqs, A.n_tokens = args->n_tokens, A.max_queries = args->starts_dev ? args->max_queries : 1;
   A.causal = args->causal != 0;
   A.inv_group = 1.f / A.group;
-  const int nt = row_tile_of(args);
   A.head_units = static_cast<uint32_t>(A.page * (args->head_dim / 2) / 64), A.code_units = A.hkv * A.head_units;
   A.page_units = static_cast<uint32_t>(quant_page_bytes(A.hkv, args->head_dim, A.page) / 64);
   if (static_cast<int64_t>(args->text.n_pages) * A.page_units > UINT32_MAX || static_cast<int64_t>(A.has_visual ? v.n_pages : 0) * A.page_units > UINT32_MAX)
@@ -966,7 +1051,15 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (args->head_dim == 128) e = nt == 1 ? launch<128, 1>(A, device, stream) : launch<128, 2>(A, device, stream);
-  else e = nt == 1 ? launch<64, 1>(A, device, stream) : launch<64, 2>(A, device, stream);
+  switch (unit_rows(args) + args->head_dim) {
+    case 128 + 2: e = launch<128, 1, 4>(A, device, stream); break;
+    case 128 + 4: e = launch<128, 1, 2>(A, device, stream); break;
+    case 128 + 8: e = launch<128, 1, 1>(A, device, stream); break;
+    case 128 + 16: e = launch<128, 2, 1>(A, device, stream); break;
+    case 64 + 2: e = launch<64, 1, 4>(A, device, stream); break;
+    case 64 + 4: e = launch<64, 1, 2>(A, device, stream); break;
+    case 64 + 8: e = launch<64, 1, 1>(A, device, stream); break;
+    default: e = launch<64, 2, 1>(A, device, stream);
+  }
   return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }

@@ -161,7 +161,7 @@ def attend_args(stream=None, visual=None, **change):
 @pytest.mark.parametrize("change,status", [
     (dict(head_dim=80), 2), (dict(page_size=48), 2), (dict(n_q_heads=5), 1), (dict(n_q_heads=0), 1), (dict(n_kv_heads=0), 1), (dict(n_seqs=0), 1), (dict(max_seqs=0), 1),
     (dict(n_seqs=4), 1), (dict(n_tokens=-1), 1), (dict(n_tokens=1), 1), (dict(max_queries=0), 1), (dict(max_queries=qc.QC_QUANT_MAX_QUERIES + 1), 2),
-    (dict(n_seqs=qc.QC_TABLE_MAX_BATCH + 1, seq_ids_dev=64), 2), (dict(n_q_heads=2 * qc.QC_QUANT_MAX_HEADS), 2), (dict(text=qc.qc_quant_stream()), 1), (dict(out_dev=0), 1), (dict(out_dev=72), 1),
+    (dict(n_seqs=qc.QC_QUANT_MAX_SEQS + 1, seq_ids_dev=64), 2), (dict(n_q_heads=2 * qc.QC_QUANT_MAX_HEADS), 2), (dict(text=qc.qc_quant_stream()), 1), (dict(out_dev=0), 1), (dict(out_dev=72), 1),
     (dict(lse_out_dev=66), 1), (dict(status_dev=65), 1), (dict(seq_ids_dev=66), 1), (dict(starts_dev=66), 1), (dict(softmax_scale=-1.0), 1),
     (dict(softmax_scale=math.nan), 1), (dict(softmax_scale=math.inf), 1), (dict(workspace_dev=72), 1),
     (dict(stream=dict(q_dev=0)), 1), (dict(stream=dict(q_dev=72)), 1), (dict(stream=dict(q_stride=-8)), 1), (dict(stream=dict(q_stride=12)), 1), (dict(stream=dict(k_pool_dev=0)), 1),
