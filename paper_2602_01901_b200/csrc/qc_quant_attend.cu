@@ -30,11 +30,11 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-template <int NT>
-constexpr int kWarpsOf = NT == 1 ? 12 : 8;   // of a block, one per SM: what 168 or 255 registers a thread leave room for
 constexpr int kUnitCost = 2;         // what a unit costs each warp besides its tiles, in tiles
 constexpr uint32_t kLongUnit = 512;   // tiles of the average unit from which on teams have eight warps
-constexpr uint32_t kFewTiles = 6;
+constexpr uint32_t kFewTiles = 6;     // per warp: of a batch with fewer, units are shared out among warps
+constexpr int64_t kSmallBatch = 8192; // tiles: up to so many blocks of eight warps (32 sequences of 1 375 tokens, 4 heads of 7: 14.0 us
+                                      // against 17.8; eight of 8 541, 32 heads: 73.9 against 68.5)
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
 constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
 
@@ -374,7 +374,7 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, const float (&scores)
         h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 16));
         const bool known = R.seen & bit, any = h > -INFINITY;
         const float delta = (known ? h > 0.f : any) ? h : 0.f;
-        const float corr = known ? exp2f(-delta) : 1.f;      // (nothing so far: nothing to put on another reference)
+        const float corr = known ? ex2_approx(-delta) : 1.f;      // (nothing so far: nothing to put on another reference)
         R.ref[nt][x] += delta;
         if (any) R.seen |= bit;
         all &= (R.seen & bit) != 0;
@@ -414,14 +414,15 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, const float (&scores)
       if constexpr (REP == 1) w[b][nt][0] = transpose_8x8(h[b][nt][0]), w[b][nt][1] = transpose_8x8(h[b][nt][1]);
     }
   }
-  if constexpr (REP == 1) return;
   // a block's weights in the columns of the lanes that weighed it, 0 in the others
+  if constexpr (REP > 1) {
 #pragma unroll
-  for (int b = 0; b < kTile / 16; ++b)
+    for (int b = 0; b < kTile / 16; ++b)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w[b][nt][i] = transpose_8x8(b / kMine == (REP == 2 ? t >> 1 : t) ? h[b % kMine][nt][i] : 0u);
+        for (int i = 0; i < 2; ++i) w[b][nt][i] = transpose_8x8(b / kMine == (REP == 2 ? t >> 1 : t) ? h[b % kMine][nt][i] : 0u);
+  }
 }
 
 // The values of a tile, and the scores of the next one (NEXT), side by side: neither waits for the other, and what one warp
@@ -528,7 +529,7 @@ __device__ __forceinline__ Place place_of(const AttendArgs& A, int seq, bool rep
 
 // What a part with reference ms and a sum counts for on reference m.  Minus infinity with a sum means that its scores were
 // no numbers.
-__device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : exp2f(ms - m); }
+__device__ __forceinline__ float weight_of(float ms, float m) { return ms == -INFINITY ? NAN : ex2_approx(ms - m); }
 
 // Sums (reference, sum, elements) put on one reference, 32 at a time, one per lane.
 struct Joined {
@@ -554,13 +555,16 @@ struct Joined {
 
 template <int D>
 __device__ __forceinline__ void write_row(const AttendArgs& A, size_t row, float m, float l, const float (&o)[D / 32], int lane) {
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  float inv, log;      // (off by 2^-23 of themselves, and by 2^-22)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(l));
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(log) : "f"(l));
+  if (l == 0.f) inv = 0.f;
   if constexpr (D == 128) {
     reinterpret_cast<uint2*>(A.out + row * D)[lane] = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
   } else {
     reinterpret_cast<uint32_t*>(A.out + row * D)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
   }
-  if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log) * 0.69314718055994531f;
 }
 
 // the same from memory that another block wrote in this launch
@@ -653,17 +657,18 @@ __device__ __forceinline__ void team_barrier(int team, int threads) {
 struct Work {
   int64_t token0;
   int32_t n_rows, queries, row, len[2], tiles_v, tiles;                     // the sequence (Place)
-  int32_t kvh, row0, first, last;                                           // the unit, and its tiles that are in the range
+  int32_t kvh, row0, first, last, mine0, mine1;                             // the unit, its tiles that are in the range, and the warp's of them
   uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
   int32_t seq, whole_units;
   uint32_t per, more, team;                                                 // cost of a range, of a unit besides its tiles
   int32_t in_block, member, warps;                                          // the team's place in the block, the warp's in the team
 };
 
-template <int D, int NT, int REP>
-__global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+// One block per SM: of twelve warps (168 registers a thread), or of eight (255), which are sooner done with a small batch and
+// have too little on their way for a large one.
+template <int D, int NT, int REP, int kAttWarps>
+__global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
   using R_ = Ring<D>;
-  constexpr int kAttWarps = kWarpsOf<NT>;
   constexpr int kRow = D + 4;            // of a column's sums in shared memory
   constexpr int kRows = 8 * NT / REP;    // query rows of a unit
   static_assert(8 * NT * kRow * 4 <= R_::kBytes, "a warp's sums take its ring's place");
@@ -671,6 +676,7 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
   __shared__ uint2 scan[kAttWarps];
   __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
   __shared__ uint32_t longest_;
+  __shared__ uint2 sums_;      // tiles and units of the batch
   __shared__ int sm_all[kAttWarps];
   __shared__ Work work_[kAttWarps];
   uint2* before = reinterpret_cast<uint2*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] tiles and units of the sequences before
@@ -678,57 +684,78 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
   pdl_wait();
   if (threadIdx.x == 0) before[0] = make_uint2(0, 0), longest_ = 0;
   __syncthreads();
-  uint64_t total = 0;
-  uint32_t units_all = 0;
-  for (int i0 = 0; i0 < A.n_seqs; i0 += kAttWarps * 32) {
-    const int i = i0 + threadIdx.x;
+  // what a sequence costs, and the sums up to it over a warp
+  const auto cost_of = [&](int i, uint32_t& x, uint32_t& n) {
     uint64_t mine = 0;
-    uint32_t units = 0;
+    n = 0;
     if (i < A.n_seqs) {
       const Place u = place_of(A, i, blockIdx.x == 0);
-      units = A.hkv * ((u.n_rows + kRows - 1) / kRows);
-      mine = static_cast<uint64_t>(u.tiles) * units;
-      if (units) atomicMax(&longest_, static_cast<uint32_t>(u.tiles));
+      n = A.hkv * ((u.n_rows + kRows - 1) / kRows);
+      mine = static_cast<uint64_t>(u.tiles) * n;
+      if (n) atomicMax(&longest_, static_cast<uint32_t>(u.tiles));
     }
     const bool big = mine > (1u << 22);
-    uint32_t x = big ? 0u : static_cast<uint32_t>(mine), n = units;
+    x = big ? 0u : static_cast<uint32_t>(mine);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, x, o), k = __shfl_up_sync(0xffffffffu, n, o);
       if (lane >= o) x += y, n += k;
     }
-    if (lane == 31) scan[warp] = make_uint2(x, n);
-    const bool any_big = __syncthreads_or(big);
-    uint2 base = make_uint2(0, 0), sum = make_uint2(0, 0);
-#pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) {
-      if (w < warp) base.x += scan[w].x, base.y += scan[w].y;
-      sum.x += scan[w].x, sum.y += scan[w].y;
+    return big;
+  };
+  constexpr uint32_t kMost = 1u << 26;      // tiles of a batch: 2^32 rows
+  if (A.n_seqs <= 64) {      // one warp: a small batch is soon done, and what a block does once it waits for, instructions included
+    if (warp == 0) {
+      uint32_t tiles = 0, units = 0;
+      for (int i0 = 0; i0 < A.n_seqs; i0 += 32) {
+        uint32_t x, n;
+        if (__any_sync(0xffffffffu, cost_of(i0 + lane, x, n))) tiles = kMost + 1;
+        if (i0 + lane < A.n_seqs) before[i0 + lane + 1] = make_uint2(tiles + x, units + n);
+        tiles += __shfl_sync(0xffffffffu, x, 31), units += __shfl_sync(0xffffffffu, n, 31);
+      }
+      if (lane == 0) sums_ = make_uint2(tiles, units);
     }
-    if (i < A.n_seqs) before[i + 1] = make_uint2(static_cast<uint32_t>(total) + base.x + x, units_all + base.y + n);
-    total += sum.x;
-    units_all += sum.y;
-    if (any_big || total > (1u << 26)) {      // a batch of more than 2^32 rows
-      if (blockIdx.x == 0 && threadIdx.x == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
-      total = 0;
-      break;
+  } else {
+    uint2 all = make_uint2(0, 0);
+#pragma unroll 1
+    for (int i0 = 0; i0 < A.n_seqs; i0 += kAttWarps * 32) {
+      const int i = i0 + threadIdx.x;
+      uint32_t x, n;
+      const bool big = cost_of(i, x, n);
+      if (lane == 31) scan[warp] = make_uint2(x, n);
+      if (__syncthreads_or(big)) all.x = kMost + 1;
+      uint2 base = all;
+#pragma unroll 1
+      for (int w = 0; w < kAttWarps; ++w) {
+        if (w < warp) base.x += scan[w].x, base.y += scan[w].y;
+        all.x += scan[w].x, all.y += scan[w].y;
+      }
+      if (i < A.n_seqs) before[i + 1] = make_uint2(base.x + x, base.y + n);
+      all.x = min(all.x, 2 * kMost);
+      __syncthreads();
     }
-    __syncthreads();
+    if (threadIdx.x == 0) sums_ = all;
   }
-  const uint32_t tiles_all = static_cast<uint32_t>(total), units = total ? units_all : 0, longest = longest_;
+  __syncthreads();
+  if (sums_.x > kMost) {
+    if (blockIdx.x == 0 && threadIdx.x == 0 && A.status) atomicMax(A.status, static_cast<int>(QC_ERR_PLAN));
+    return;
+  }
+  const uint32_t tiles_all = sums_.x, units = sums_.y, longest = longest_;
   const uint32_t n_warps = gridDim.x * kAttWarps;
   uint32_t team_warps = 1;
   if (tiles_all >= units * kLongUnit || units * kAttWarps <= n_warps) team_warps = kAttWarps;
   else if (tiles_all <= n_warps * kFewTiles) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
-  const uint32_t n_teams = n_warps / team_warps, more = kUnitCost * team_warps, cost = tiles_all + units * more;
+  const int shift = team_warps == 2 ? 1 : team_warps == 4 ? 2 : 0;      // (of the teams that are not a whole block)
+  const uint32_t n_teams = team_warps == kAttWarps ? gridDim.x : n_warps >> shift, more = kUnitCost * team_warps, cost = tiles_all + units * more;
   uint32_t per_team = (cost + n_teams - 1) / n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
   if (!whole_units) per_team = max(per_team, team_warps + more);
   const auto before_cost = [&](int s) { return before[s].x + before[s].y * more; };
   volatile Work& W = work_[warp];
   if (lane == 0) {
-    W.in_block = warp / team_warps, W.member = warp % team_warps, W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
-    W.team = blockIdx.x * (kAttWarps / team_warps) + W.in_block;
+    W.in_block = team_warps == kAttWarps ? 0 : warp >> shift, W.member = team_warps == kAttWarps ? warp : warp & (team_warps - 1), W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
+    W.team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + W.in_block;
     const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team, static_cast<uint64_t>(cost));
     W.at = at, W.end = min(cost, at + per_team);
     int lo = 0, hi = A.n_seqs - 1;      // the last sequence that begins at or before the range
@@ -749,7 +776,7 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
       const Place u = place_of(A, seq, false);
       const int row_tiles = (u.n_rows + kRows - 1) / kRows, unit_cost = u.tiles + more;
       const uint32_t seq_at = before[seq].x + before[seq].y * more;
-      const int unit = (at - seq_at) / unit_cost;
+      const int unit = static_cast<uint32_t>(at - seq_at) / static_cast<uint32_t>(unit_cost);
       const uint32_t unit_at = seq_at + unit * unit_cost;
       int first = 0, last = u.tiles;
       if (W.whole_units) {
@@ -761,7 +788,9 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
       __syncwarp();
       if (lane == 0) {
         W.seq = seq, W.at = unit_at + unit_cost, W.unit_at = unit_at, W.first = first, W.last = last;
-        W.kvh = unit / row_tiles, W.row0 = (unit - W.kvh * row_tiles) * kRows;
+        const int kvh = row_tiles == 1 ? unit : unit / row_tiles, n = last - first;
+        W.kvh = kvh, W.row0 = (unit - kvh * row_tiles) * kRows;
+        W.mine0 = first + n * W.member / W.warps, W.mine1 = first + n * (W.member + 1) / W.warps;      // (even shares: warps share their units)
         W.token0 = u.token0, W.n_rows = u.n_rows, W.queries = u.queries, W.row = u.row, W.len[0] = u.len[0], W.len[1] = u.len[1];
         W.tiles_v = u.tiles_v, W.tiles = u.tiles;
       }
@@ -784,8 +813,7 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
     // this warp's tiles of the unit, adjacent ones: a run in each stream
 #pragma unroll 1
     for (int now = 1; now >= 0; --now) {
-      const int first = W.first, n = W.last - first, member = W.member, warps = W.warps, tiles_v = W.tiles_v;
-      const int mine0 = first + n * member / warps, mine1 = first + n * (member + 1) / warps;
+      const int mine0 = W.mine0, mine1 = W.mine1, tiles_v = W.tiles_v;
       const int shift = now ? 0 : tiles_v;      // the stream's first tile in the unit
       const int run = max(mine0, shift) - shift, stop = (now ? min(mine1, tiles_v) : mine1) - shift;
       if (run >= stop) continue;
@@ -879,7 +907,6 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
                                                                    fmaf(R.acc[nt][mb + 1][x] * kEven, unit_step, z), fmaf(R.acc[nt][mb + 1][x + 2] * kOdd, unit_step, z));
         }
       }
-    team_barrier(in_block, threads);
     const int n_here = min(kRows, n_rows - row0);
     const bool whole = W.first == 0 && W.last == W.tiles;
     // pieces: the first team's is its second one if a unit before this one ends in its range, all others are a team's first
@@ -887,32 +914,46 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
     const uint32_t first_team = whole ? team : (unit_at + W.more) / per, last_team = whole ? team : (W.at - 1) / per;
     const uint32_t first_place = unit_at > first_team * per ? 1 : 0, place = team == first_team ? first_place : 0;
     float* piece = piece_at<D, kRows>(A, team, place);
-    for (int col = member; col < n_here; col += warps) {
-      // the column's sums of every warp (and set of columns), each lane's weight first
-      float o[D / 32] = {};
-      Joined J;
-      const auto row_of = [&](int i) { return reinterpret_cast<const float*>(smem + (team0 + i / REP) * R_::kBytes) + (col + i % REP * kRows) * kRow; };
-      for (int i0 = 0; i0 < warps * REP; i0 += 32) {
-        const int i = i0 + lane, n = min(32, warps * REP - i0);
-        const float2 ml = lane < n ? make_float2(sm_m[team0 + i / REP][col + i % REP * kRows], sm_l[team0 + i / REP][col + i % REP * kRows]) : make_float2(-INFINITY, 0.f);
+    // four sets of columns of a warp put together first, then the team's warps (the same instructions: they are fetched once)
+    constexpr bool kTwice = REP == 4;
+    constexpr int kSets = kTwice ? 1 : REP;
+#pragma unroll 1
+    for (int round = kTwice ? 0 : 1; round < 2; ++round) {
+      const bool own = kTwice && round == 0;
+      const int w0 = own ? warp : team0, n = own ? REP : warps * kSets;
+      const auto ml_at = [&](int i) { return own ? i * kRows : i / kSets * (8 * NT) + i % kSets * kRows; };
+      const auto row_at = [&](int i) { return own ? i * (kRows * kRow) : i / kSets * static_cast<int>(R_::kBytes / 4) + i % kSets * (kRows * kRow); };
+      if (own) __syncwarp();
+      else team_barrier(in_block, threads);
+#pragma unroll 1
+      for (int col = own ? 0 : member; col < n_here; col += own ? 1 : warps) {
+        const int i = ml_at(min(lane, n - 1));
+        const float2 ml = lane < n ? make_float2((&sm_m[w0][col])[i], (&sm_l[w0][col])[i]) : make_float2(-INFINITY, 0.f);
+        float o[D / 32] = {};
+        Joined J;
         const float f = J.join(ml, o);
-#pragma unroll 4
+        const float* row = reinterpret_cast<const float*>(smem + w0 * R_::kBytes) + col * kRow;
+#pragma unroll 2
         for (int k = 0; k < n; ++k) {
           const float fk = __shfl_sync(0xffffffffu, f, k);
           float v[D / 32];
-          load_run<D>(row_of(i0 + k), v, lane);
+          load_run<D>(row + row_at(k), v, lane);
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) o[j] = fmaf(v[j], fk, o[j]);
         }
-      }
-      const float m = J.m, l = J.l;
-      if (whole) {
-        const int r = row0 + col, query = query_of(A, r);
-        write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, m, l, o, lane);
-      } else {
-        if constexpr (D == 128) reinterpret_cast<float4*>(piece + col * D)[lane] = make_float4(o[0], o[1], o[2], o[3]);
-        else reinterpret_cast<float2*>(piece + col * D)[lane] = make_float2(o[0], o[1]);
-        if (lane == 0) reinterpret_cast<float2*>(piece + kRows * D)[col] = make_float2(m, l);
+        if (!own && whole) {
+          const int r = row0 + col, query = query_of(A, r);
+          write_row<D>(A, static_cast<size_t>(token0 + query) * A.hq + kvh * A.group + r - query * A.group, J.m, J.l, o, lane);
+        } else {
+          float* to = own ? const_cast<float*>(row) : piece + col * D;
+          if constexpr (D == 128) reinterpret_cast<float4*>(to)[lane] = make_float4(o[0], o[1], o[2], o[3]);
+          else reinterpret_cast<float2*>(to)[lane] = make_float2(o[0], o[1]);
+          __syncwarp();
+          if (lane == 0) {
+            if (own) sm_m[warp][col] = J.m, sm_l[warp][col] = J.l;
+            else reinterpret_cast<float2*>(piece + kRows * D)[col] = make_float2(J.m, J.l);
+          }
+        }
       }
     }
     if (!whole) {
@@ -981,14 +1022,13 @@ unsigned long long next_nonce() {
   return x ? x : 1;
 }
 
-template <int D, int NT, int REP>
+template <int D, int NT, int REP, int kAttWarps>
 cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
-  constexpr int kAttWarps = kWarpsOf<NT>;
   const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
   static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
   cudaError_t e;
   if (device >= 64 || configured[device] < smem) {
-    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP, kAttWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     if (device < 64) configured[device] = smem;
   }
@@ -997,7 +1037,12 @@ cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
   int blocks = sms;
   if (blocks > kMostTeams / kAttWarps) blocks = kMostTeams / kAttWarps;
   A.nonce = next_nonce();
-  return launch_pdl(quant_attend_kernel<D, NT, REP>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
+  return launch_pdl(quant_attend_kernel<D, NT, REP, kAttWarps>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
+}
+
+template <int D, int REP>
+cudaError_t launch_rows(AttendArgs& A, int device, bool small, cudaStream_t stream) {
+  return small ? launch<D, 1, REP, 8>(A, device, stream) : launch<D, 1, REP, 12>(A, device, stream);
 }
 
 size_t workspace_bytes(const qc_quant_attend_args* a) {
@@ -1051,15 +1096,13 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  switch (unit_rows(args) + args->head_dim) {
-    case 128 + 2: e = launch<128, 1, 4>(A, device, stream); break;
-    case 128 + 4: e = launch<128, 1, 2>(A, device, stream); break;
-    case 128 + 8: e = launch<128, 1, 1>(A, device, stream); break;
-    case 128 + 16: e = launch<128, 2, 1>(A, device, stream); break;
-    case 64 + 2: e = launch<64, 1, 4>(A, device, stream); break;
-    case 64 + 4: e = launch<64, 1, 2>(A, device, stream); break;
-    case 64 + 8: e = launch<64, 1, 1>(A, device, stream); break;
-    default: e = launch<64, 2, 1>(A, device, stream);
-  }
+  // the most tiles that the tables have room for, over all units
+  const int rows = unit_rows(args);
+  const int64_t pages = static_cast<int64_t>(args->text.max_pages) + (A.has_visual ? v.max_pages : 0);
+  const bool small = ((pages * A.page + kTile - 1) / kTile) * A.n_seqs * A.hkv <= kSmallBatch;
+  if (args->head_dim == 128) e = rows == 2 ? launch_rows<128, 4>(A, device, small, stream) : rows == 4 ? launch_rows<128, 2>(A, device, small, stream)
+                               : rows == 8 ? launch_rows<128, 1>(A, device, small, stream) : launch<128, 2, 1, 8>(A, device, stream);
+  else e = rows == 2 ? launch_rows<64, 4>(A, device, small, stream) : rows == 4 ? launch_rows<64, 2>(A, device, small, stream)
+           : rows == 8 ? launch_rows<64, 1>(A, device, small, stream) : launch<64, 2, 1, 8>(A, device, stream);
   return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }
