@@ -128,23 +128,33 @@ struct Query {
 // Row r of a unit is query r / group of the sequence, head r % group of the KV head.
 __device__ __forceinline__ int query_of(const AttendArgs& A, int r) { return static_cast<int>((static_cast<float>(r) + 0.5f) * A.inv_group); }
 
+template <int D, int NT>
+struct RawQuery {
+  uint4 x[NT][D / 32];
+};
 template <int D, int NT, int REP>
-__device__ __forceinline__ void load_query(Query<D, NT>& Q, const AttendArgs& A, const StreamArgs& S, int64_t token0, int head0, int row0,
-                                           int n_rows, int lane) {
-  const int g = lane >> 2, t = lane & 3;
-  uint4 raw[NT][D / 32];
-  uint32_t top = 0;
+__device__ __forceinline__ void ask_query(RawQuery<D, NT>& raw, const AttendArgs& A, const StreamArgs& S, int64_t token0, int head0, int row0, int n_rows, int lane) {
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int r = row0 + nt * 8 + g % (8 / REP), query = query_of(A, r);
-    const bool on = r < n_rows;
-    const uint16_t* q = S.q + (token0 + query) * S.q_stride + static_cast<int64_t>(head0 + r - query * A.group) * D + t * (D / 4);
+    const int r = row0 + nt * 8 + (lane >> 2) % (8 / REP), query = query_of(A, r);
+    const uint16_t* q = S.q + (token0 + query) * S.q_stride + static_cast<int64_t>(head0 + r - query * A.group) * D + (lane & 3) * (D / 4);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) raw.x[nt][i] = r < n_rows ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
+  }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void make_query(Query<D, NT>& Q, const RawQuery<D, NT>& given, const AttendArgs& A, int lane) {
+  const int t = lane & 3;
+  const uint4(&raw)[NT][D / 32] = given.x;
+  uint32_t top = 0;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      const uint4 x = raw[nt][i] = on ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
+      const uint4 x = raw[nt][i];
       top = max_bf16x2(top, max_bf16x2(max_bf16x2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max_bf16x2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
     }
-  }
   // (of numbers that are not negative, the larger one has the larger bits)
   const int top_exp = static_cast<int>(__reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16)) >> 7);
   // 2^e with the unit's largest element times 2^-e in [2^14, 2^15); below 2^-90 it counts as that, from 2^101 on it has no scores
@@ -660,7 +670,7 @@ struct Work {
   int32_t kvh, row0, first, last, mine0, mine1;                             // the unit, its tiles that are in the range, and the warp's of them
   uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
   int32_t seq, whole_units;
-  uint32_t per, more, team;                                                 // cost of a range, of a unit besides its tiles
+  uint32_t per, longer, more, team;                                         // cost of a range, ranges that cost one more, cost of a unit besides its tiles
   int32_t in_block, member, warps;                                          // the team's place in the block, the warp's in the team
 };
 
@@ -748,16 +758,18 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   else if (tiles_all <= n_warps * kFewTiles) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
   const int shift = team_warps == 2 ? 1 : team_warps == 4 ? 2 : 0;      // (of the teams that are not a whole block)
   const uint32_t n_teams = team_warps == kAttWarps ? gridDim.x : n_warps >> shift, more = kUnitCost * team_warps, cost = tiles_all + units * more;
-  uint32_t per_team = (cost + n_teams - 1) / n_teams;
+  // ranges of per_team or one more
+  uint32_t per_team = cost / n_teams, longer = cost - per_team * n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
-  if (!whole_units) per_team = max(per_team, team_warps + more);
+  if (!whole_units && per_team < team_warps + more) per_team = team_warps + more, longer = 0;
   const auto before_cost = [&](int s) { return before[s].x + before[s].y * more; };
   volatile Work& W = work_[warp];
   if (lane == 0) {
     W.in_block = team_warps == kAttWarps ? 0 : warp >> shift, W.member = team_warps == kAttWarps ? warp : warp & (team_warps - 1), W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
     W.team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + W.in_block;
-    const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team, static_cast<uint64_t>(cost));
-    W.at = at, W.end = min(cost, at + per_team);
+    W.longer = longer;
+    const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team + min(W.team, longer), static_cast<uint64_t>(cost));
+    W.at = at, W.end = min(cost, at + per_team + (W.team < longer ? 1 : 0));
     int lo = 0, hi = A.n_seqs - 1;      // the last sequence that begins at or before the range
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -822,8 +834,11 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
       const int32_t* table = S.pages + static_cast<size_t>(W.row) * S.max_pages;
       // the next tile to ask for: its batch's first tile, the batch, and the next batch's page ids
       int asked = run, at_tile = run;
-      Batch batch = batch_of<D>(A, S, ask_ids(A, table, run, len, lane), kvh, run, len, lane);
-      int32_t ids = ask_ids(A, table, run + kBatch, len, lane);
+      int32_t ids = ask_ids(A, table, run, len, lane);
+      RawQuery<D, NT> raw;
+      ask_query<D, NT, REP>(raw, A, S, W.token0, kvh * A.group, W.row0, W.n_rows, lane);
+      Batch batch = batch_of<D>(A, S, ids, kvh, run, len, lane);
+      ids = ask_ids(A, table, run + kBatch, len, lane);
       uint32_t there = 0;      // blocks that are there of the next two tiles and the two behind them, 4 bits a tile
       const uint32_t params = ring + 4 * R_::kCodes;
       const auto ask_keys = [&]() {       // of tile `asked`
@@ -848,7 +863,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
       ask_keys();
       ask_values();
       Query<D, NT> Q;
-      load_query<D, NT, REP>(Q, A, S, W.token0, kvh * A.group, W.row0, W.n_rows, lane);
+      make_query<D, NT>(Q, raw, A, lane);
       float c[kTile / 16][NT][4];
       cp_async_wait_group<3>();
       __syncwarp();
@@ -910,9 +925,15 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     const int n_here = min(kRows, n_rows - row0);
     const bool whole = W.first == 0 && W.last == W.tiles;
     // pieces: the first team's is its second one if a unit before this one ends in its range, all others are a team's first
-    const uint32_t team = W.team, per = W.per, unit_at = W.unit_at;
-    const uint32_t first_team = whole ? team : (unit_at + W.more) / per, last_team = whole ? team : (W.at - 1) / per;
-    const uint32_t first_place = unit_at > first_team * per ? 1 : 0, place = team == first_team ? first_place : 0;
+    const uint32_t team = W.team, unit_at = W.unit_at;
+    uint32_t first_team = team, last_team = team, first_place = 0;
+    if (!whole) {
+      const uint32_t per = W.per, longer = W.longer, turn = longer * (per + 1);      // where the shorter ranges begin
+      const auto team_at = [&](uint32_t p) { return p < turn ? p / (per + 1) : longer + (p - turn) / per; };
+      first_team = team_at(unit_at + W.more), last_team = team_at(W.at - 1);
+      first_place = unit_at > first_team * per + min(first_team, longer) ? 1 : 0;
+    }
+    const uint32_t place = team == first_team ? first_place : 0;
     float* piece = piece_at<D, kRows>(A, team, place);
     // four sets of columns of a warp put together first, then the team's warps (the same instructions: they are fetched once)
     constexpr bool kTwice = REP == 4;
