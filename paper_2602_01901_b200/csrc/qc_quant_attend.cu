@@ -30,9 +30,12 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kUnitCost = 2;         // what a unit costs each warp besides its tiles, in tiles
+constexpr int kUnitCost = 4;         // what a unit costs each warp besides its tiles, in tiles
 constexpr uint32_t kLongUnit = 512;   // tiles of the average unit from which on teams have eight warps
-constexpr uint32_t kFewTiles = 6;     // per warp: of a batch with fewer, units are shared out among warps
+template <int ROWS>
+constexpr uint32_t kFewTiles = ROWS == 2 ? 3 : 6;   // per warp: of a batch with fewer, units are shared out among warps (more rows
+                                                    // make more of a unit's pieces: drafts on 64-wide heads, 16 rows, 29 us against
+                                                    // 42 with teams of one warp; 16 ragged sequences of one row 31 against 28.5)
 constexpr int64_t kSmallBatch = 8192; // tiles: up to so many blocks of eight warps (32 sequences of 1 375 tokens, 4 heads of 7: 14.0 us
                                       // against 17.8; eight of 8 541, 32 heads: 73.9 against 68.5)
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
@@ -670,7 +673,7 @@ struct Work {
   int32_t kvh, row0, first, last, mine0, mine1;                             // the unit, its tiles that are in the range, and the warp's of them
   uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
   int32_t seq, whole_units;
-  uint32_t per, longer, more, team;                                         // cost of a range, ranges that cost one more, cost of a unit besides its tiles
+  uint32_t per, longer, more, per_tile, team;                                         // cost of a range, ranges that cost one more, cost of a unit besides its tiles, and of a tile
   int32_t in_block, member, warps;                                          // the team's place in the block, the warp's in the team
 };
 
@@ -755,19 +758,22 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   const uint32_t n_warps = gridDim.x * kAttWarps;
   uint32_t team_warps = 1;
   if (tiles_all >= units * kLongUnit || units * kAttWarps <= n_warps) team_warps = kAttWarps;
-  else if (tiles_all <= n_warps * kFewTiles) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
+  else if (tiles_all <= n_warps * kFewTiles<kRows>) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
   const int shift = team_warps == 2 ? 1 : team_warps == 4 ? 2 : 0;      // (of the teams that are not a whole block)
-  const uint32_t n_teams = team_warps == kAttWarps ? gridDim.x : n_warps >> shift, more = kUnitCost * team_warps, cost = tiles_all + units * more;
+  const uint32_t n_teams = team_warps == kAttWarps ? gridDim.x : n_warps >> shift;
+  // a team for every unit, each one short: one each, whatever they cost
+  const bool one_each = units <= n_teams && longest <= team_warps * kWholeTiles;
+  const uint32_t more = one_each ? 1 : kUnitCost * team_warps, per_tile = one_each ? 0 : 1, cost = tiles_all * per_tile + units * more;
   // ranges of per_team or one more
   uint32_t per_team = cost / n_teams, longer = cost - per_team * n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
   if (!whole_units && per_team < team_warps + more) per_team = team_warps + more, longer = 0;
-  const auto before_cost = [&](int s) { return before[s].x + before[s].y * more; };
+  const auto before_cost = [&](int s) { return before[s].x * per_tile + before[s].y * more; };
   volatile Work& W = work_[warp];
   if (lane == 0) {
     W.in_block = team_warps == kAttWarps ? 0 : warp >> shift, W.member = team_warps == kAttWarps ? warp : warp & (team_warps - 1), W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
     W.team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + W.in_block;
-    W.longer = longer;
+    W.longer = longer, W.per_tile = per_tile;
     const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team + min(W.team, longer), static_cast<uint64_t>(cost));
     W.at = at, W.end = min(cost, at + per_team + (W.team < longer ? 1 : 0));
     int lo = 0, hi = A.n_seqs - 1;      // the last sequence that begins at or before the range
@@ -782,12 +788,12 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
   while (W.at < W.end) {
     {   // the next unit: every warp of the team finds the same
-      const uint32_t at = W.at, more = W.more;
+      const uint32_t at = W.at, more = W.more, per_tile = W.per_tile;
       int seq = W.seq;
-      while (before[seq + 1].x + before[seq + 1].y * more <= at) ++seq;
+      while (before[seq + 1].x * per_tile + before[seq + 1].y * more <= at) ++seq;
       const Place u = place_of(A, seq, false);
-      const int row_tiles = (u.n_rows + kRows - 1) / kRows, unit_cost = u.tiles + more;
-      const uint32_t seq_at = before[seq].x + before[seq].y * more;
+      const int row_tiles = (u.n_rows + kRows - 1) / kRows, unit_cost = u.tiles * per_tile + more;
+      const uint32_t seq_at = before[seq].x * per_tile + before[seq].y * more;
       const int unit = static_cast<uint32_t>(at - seq_at) / static_cast<uint32_t>(unit_cost);
       const uint32_t unit_at = seq_at + unit * unit_cost;
       int first = 0, last = u.tiles;
@@ -1024,10 +1030,12 @@ int32_t check_sizes(const qc_quant_attend_args* a) {
   return QC_OK;
 }
 
-// query rows of a unit: as many columns of a product as they need
+// Query rows of a unit: as many columns of a product as they need.  Sixteen only where they are all taken (sequences of 8 000
+// tokens, 4 heads of 8, 64 wide, two queries: 31 us against 37 with units of eight; with one to five queries on 4 heads of 4,
+// 128 wide, 30 against 26).
 int unit_rows(const qc_quant_attend_args* a) {
   const int64_t rows = static_cast<int64_t>(a->max_queries) * (a->n_q_heads / a->n_kv_heads);
-  return rows <= 2 ? 2 : rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+  return rows <= 2 ? 2 : rows <= 4 ? 4 : rows % 16 ? 8 : 16;
 }
 
 constexpr int kMostTeams = 2560;   // of one warp each; the workspace is sized for it
