@@ -665,16 +665,15 @@ __device__ __forceinline__ void team_barrier(int team, int threads) {
   else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory");
 }
 
-// What a warp knows about its range and the unit it is at.  Kept in shared memory: it is looked at once a unit, and the
-// loop over the tiles has no registers to spare for it.
+// What a team knows about its range and the unit it is at, found by its first warp.  Kept in shared memory: it is looked at
+// once a unit, and the loop over the tiles has no registers to spare for it.
 struct Work {
   int64_t token0;
   int32_t n_rows, queries, row, len[2], tiles_v, tiles;                     // the sequence (Place)
-  int32_t kvh, row0, first, last, mine0, mine1;                             // the unit, its tiles that are in the range, and the warp's of them
+  int32_t kvh, row0, first, last;                                           // the unit, and its tiles that are in the range
   uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
-  int32_t seq, whole_units;
+  int32_t seq, whole_units, found, warps;
   uint32_t per, longer, more, per_tile, team;                                         // cost of a range, ranges that cost one more, cost of a unit besides its tiles, and of a tile
-  int32_t in_block, member, warps;                                          // the team's place in the block, the warp's in the team
 };
 
 // One block per SM: of twelve warps (168 registers a thread), or of eight (255), which are sooner done with a small batch and
@@ -692,6 +691,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   __shared__ uint2 sums_;      // tiles and units of the batch
   __shared__ int sm_all[kAttWarps];
   __shared__ Work work_[kAttWarps];
+  __shared__ int2 me_[kAttWarps];      // a warp's team in the block, its place in the team
   uint2* before = reinterpret_cast<uint2*>(smem + kAttWarps * R_::kBytes);   // [n_seqs + 1] tiles and units of the sequences before
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   pdl_wait();
@@ -769,13 +769,14 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
   if (!whole_units && per_team < team_warps + more) per_team = team_warps + more, longer = 0;
   const auto before_cost = [&](int s) { return before[s].x * per_tile + before[s].y * more; };
-  volatile Work& W = work_[warp];
-  if (lane == 0) {
-    W.in_block = team_warps == kAttWarps ? 0 : warp >> shift, W.member = team_warps == kAttWarps ? warp : warp & (team_warps - 1), W.warps = team_warps, W.per = per_team, W.more = more, W.whole_units = whole_units;
-    W.team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + W.in_block;
-    W.longer = longer, W.per_tile = per_tile;
-    const uint32_t at = min(static_cast<uint64_t>(W.team) * per_team + min(W.team, longer), static_cast<uint64_t>(cost));
-    W.at = at, W.end = min(cost, at + per_team + (W.team < longer ? 1 : 0));
+  const int in_block = team_warps == kAttWarps ? 0 : warp >> shift, member = team_warps == kAttWarps ? warp : warp & (team_warps - 1);
+  volatile Work& W = work_[in_block];
+  if (lane == 0) me_[warp] = make_int2(in_block, member);
+  if (member == 0 && lane == 0) {
+    const uint32_t team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + in_block;
+    const uint32_t at = min(static_cast<uint64_t>(team) * per_team + min(team, longer), static_cast<uint64_t>(cost));
+    W.warps = team_warps, W.team = team, W.per = per_team, W.longer = longer, W.more = more, W.per_tile = per_tile, W.whole_units = whole_units;
+    W.at = at, W.end = min(cost, at + per_team + (team < longer ? 1 : 0));
     int lo = 0, hi = A.n_seqs - 1;      // the last sequence that begins at or before the range
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -784,37 +785,40 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     }
     W.seq = lo;
   }
-  __syncwarp();
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
-  while (W.at < W.end) {
-    {   // the next unit: every warp of the team finds the same
-      const uint32_t at = W.at, more = W.more, per_tile = W.per_tile;
-      int seq = W.seq;
-      while (before[seq + 1].x * per_tile + before[seq + 1].y * more <= at) ++seq;
-      const Place u = place_of(A, seq, false);
-      const int row_tiles = (u.n_rows + kRows - 1) / kRows, unit_cost = u.tiles * per_tile + more;
-      const uint32_t seq_at = before[seq].x * per_tile + before[seq].y * more;
-      const int unit = static_cast<uint32_t>(at - seq_at) / static_cast<uint32_t>(unit_cost);
-      const uint32_t unit_at = seq_at + unit * unit_cost;
-      int first = 0, last = u.tiles;
-      if (W.whole_units) {
-        if (unit_at < at) last = 0;      // it begins before the range: the next one
-      } else {
-        first = max(0, static_cast<int>(at - unit_at) - static_cast<int>(more));
-        last = min(u.tiles, static_cast<int>(W.end - unit_at) - static_cast<int>(more));
-      }
+  while (true) {
+    if (me_[warp].y == 0) {   // the team's first warp finds its next unit
       __syncwarp();
-      if (lane == 0) {
-        W.seq = seq, W.at = unit_at + unit_cost, W.unit_at = unit_at, W.first = first, W.last = last;
-        const int kvh = row_tiles == 1 ? unit : unit / row_tiles, n = last - first;
-        W.kvh = kvh, W.row0 = (unit - kvh * row_tiles) * kRows;
-        W.mine0 = first + n * W.member / W.warps, W.mine1 = first + n * (W.member + 1) / W.warps;      // (even shares: warps share their units)
-        W.token0 = u.token0, W.n_rows = u.n_rows, W.queries = u.queries, W.row = u.row, W.len[0] = u.len[0], W.len[1] = u.len[1];
-        W.tiles_v = u.tiles_v, W.tiles = u.tiles;
+      uint32_t at = W.at;
+      const uint32_t end = W.end, more = W.more, per_tile = W.per_tile;
+      int seq = W.seq, first = 0, last = 0;
+      while (at < end && first >= last) {
+        while (before[seq + 1].x * per_tile + before[seq + 1].y * more <= at) ++seq;
+        const Place u = place_of(A, seq, false);
+        const int row_tiles = (u.n_rows + kRows - 1) / kRows, units = A.hkv * row_tiles;
+        const uint32_t unit_cost = u.tiles * per_tile + more, seq_at = before[seq].x * per_tile + before[seq].y * more;
+        const int unit = (at - seq_at) / unit_cost;
+        const uint32_t unit_at = seq_at + unit * unit_cost;
+        last = u.tiles;
+        if (W.whole_units) {
+          if (unit_at < at) last = 0;      // it begins before the range: the next one
+        } else {
+          first = max(0, static_cast<int>(at - unit_at) - static_cast<int>(more));
+          last = min(u.tiles, static_cast<int>(end - unit_at) - static_cast<int>(more));
+        }
+        if (unit >= units) last = 0;       // (lengths that change under the call: wrong sums, and no more than that)
+        at = unit_at + unit_cost;
+        if (first < last && lane == 0) {
+          const int kvh = row_tiles == 1 ? unit : unit / row_tiles;
+          W.unit_at = unit_at, W.first = first, W.last = last, W.kvh = kvh, W.row0 = (unit - kvh * row_tiles) * kRows;
+          W.token0 = u.token0, W.n_rows = u.n_rows, W.queries = u.queries, W.row = u.row, W.len[0] = u.len[0], W.len[1] = u.len[1];
+          W.tiles_v = u.tiles_v, W.tiles = u.tiles;
+        }
       }
-      __syncwarp();
-      if (first >= last) continue;
+      if (lane == 0) W.seq = seq, W.at = at, W.found = first < last;
     }
+    team_barrier(me_[warp].x, W.warps * 32);
+    if (!W.found) break;
 
     Rows<D, NT> R;
 #pragma unroll
@@ -831,7 +835,8 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     // this warp's tiles of the unit, adjacent ones: a run in each stream
 #pragma unroll 1
     for (int now = 1; now >= 0; --now) {
-      const int mine0 = W.mine0, mine1 = W.mine1, tiles_v = W.tiles_v;
+      const int first = W.first, n = W.last - first, warps = W.warps, member = me_[warp].y, tiles_v = W.tiles_v;
+      const int mine0 = first + n * member / warps, mine1 = first + n * (member + 1) / warps;      // (even shares: warps share their units)
       const int shift = now ? 0 : tiles_v;      // the stream's first tile in the unit
       const int run = max(mine0, shift) - shift, stop = (now ? min(mine1, tiles_v) : mine1) - shift;
       if (run >= stop) continue;
@@ -906,7 +911,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
       __syncwarp();
     }
     // the team's sums meet in shared memory
-    const int n_rows = W.n_rows, row0 = W.row0, kvh = W.kvh, member = W.member, warps = W.warps, in_block = W.in_block, threads = warps * 32, team0 = in_block * warps;
+    const int in_block = me_[warp].x, member = me_[warp].y, n_rows = W.n_rows, row0 = W.row0, kvh = W.kvh, warps = W.warps, threads = warps * 32, team0 = in_block * warps;
     const int64_t token0 = W.token0;
     const float unit_step = __uint_as_float(R.step) * (1.f / 32768.f);
     constexpr float kEven = 16777216.f, kOdd = 1048576.f;
@@ -936,7 +941,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     if (!whole) {
       const uint32_t per = W.per, longer = W.longer, turn = longer * (per + 1);      // where the shorter ranges begin
       const auto team_at = [&](uint32_t p) { return p < turn ? p / (per + 1) : longer + (p - turn) / per; };
-      first_team = team_at(unit_at + W.more), last_team = team_at(W.at - 1);
+      first_team = team_at(unit_at + W.more), last_team = team_at(unit_at + W.tiles + W.more - 1);
       first_place = unit_at > first_team * per + min(first_team, longer) ? 1 : 0;
     }
     const uint32_t place = team == first_team ? first_place : 0;
@@ -1002,7 +1007,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
           for (uint32_t i = first_team + lane; i <= last_team; i += 32) A.flags[2 * i + (i == first_team ? first_place : 0)] = 0;
       }
     }
-    if (W.at < W.end) team_barrier(in_block, threads);      // the rings' places are free again
+    team_barrier(in_block, threads);      // the rings' places, and what is known about the unit, are free again
   }
 }
 
@@ -1054,12 +1059,13 @@ unsigned long long next_nonce() {
 template <int D, int NT, int REP, int kAttWarps>
 cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
   const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
-  static int configured[64] = {};     // shared memory that the kernel may take on a device (a benign race: the same call again)
+  constexpr int kMost = kAttWarps * Ring<D>::kBytes + (QC_QUANT_MAX_SEQS + 1) * 8;
+  static std::atomic<bool> configured[64] = {};     // per device: the kernel may take that much
   cudaError_t e;
-  if (device >= 64 || configured[device] < smem) {
-    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP, kAttWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (device >= 64 || !configured[device].load(std::memory_order_relaxed)) {
+    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP, kAttWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
-    if (device < 64) configured[device] = smem;
+    if (device < 64) configured[device].store(true, std::memory_order_relaxed);
   }
   int sms = 0;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return e;

@@ -97,15 +97,16 @@ __global__ void __launch_bounds__(1024) table_kernel(const TableArgs T) {
   Seq* seqs = reinterpret_cast<Seq*>(shared);                          // [n_seqs]
   uint32_t* seen = reinterpret_cast<uint32_t*>(seqs + T.n_seqs);       // [max_seqs / 32] ids met (where ids are given)
   __shared__ Sums warp_sums[32];
-  __shared__ int32_t error;
+  __shared__ int32_t error, free_pages;
   const int n_seqs = T.n_seqs, shift = T.page_shift, up = (1 << shift) - 1;
   const int thread = blockIdx.x * blockDim.x + threadIdx.x, n_threads = gridDim.x * blockDim.x;
   if (threadIdx.x == 0) error = 0;
   if (T.ids)
     for (int i = threadIdx.x; i < (T.max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
   pdl_wait();
+  if (threadIdx.x == 0) free_pages = T.state[0];      // (one read: all threads go the same way whatever happens to it meanwhile)
   __syncthreads();
-  const int32_t n_free = T.state[0];
+  const int32_t n_free = free_pages;
 
   Sums all{0, 0};
   for (int i0 = 0; i0 < n_seqs; i0 += blockDim.x) {
@@ -245,7 +246,9 @@ int32_t check_batch(const TableArgs& a, int32_t n_seqs, const int32_t* ids, cons
 template <bool TRIM>
 int32_t launch_table(const TableArgs& a, bool many, void* cuda_stream) {
   const size_t smem = static_cast<size_t>(a.n_seqs) * sizeof(Seq) + (a.ids ? (a.max_seqs + 31) / 32 * 4 : 0);
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) return QC_ERR_CUDA;
+  // (always the most, so that two calls at once cannot take it from one another)
+  constexpr int kMost = kTableMaxBatch * static_cast<int>(sizeof(Seq)) + kTableMaxSeqs / 8;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return QC_ERR_CUDA;
   const int32_t work = a.max_slots > a.n_seqs ? a.max_slots : a.n_seqs;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(many ? kCluster : 1);
