@@ -98,3 +98,39 @@ def check_attend(out, lse, starts, ids, lens, q, k_held, v_held, group, scale, c
                 tol, tol_lse = bound(queries, keys, values, scale, want, weights)
                 assert np.all(np.abs(out[t, h] - want) <= tol), (where, np.max(np.abs(out[t, h] - want) / tol))
                 assert abs(lse[t, h] - want_lse) <= tol_lse + 2.0 ** -23 * abs(want_lse), (where, lse[t, h], want_lse)
+
+
+def held_torch(x):
+    """``held`` for many rows at once, fp64 on the rows' device."""
+    x = x.double()
+    lo, hi = x.min(-1).values, x.max(-1).values
+    r = (15 / (hi - lo)).float().bfloat16().double()      # (rows of a range, whose two roundings do not meet a tie)
+    return {"lo": lo, "step": 1 / r, "codes": torch.round((x - lo[..., None]) * r[..., None])}
+
+
+def check_attend_torch(out, lse, q, k, v, seen, scale):
+    """Rows of one batch against softmax attention in 64 bits, all at once: out, q [rows, d], k, v: ``held_torch`` of [rows or 1,
+    keys, d] (keys padded), seen [rows]: how many of the keys a row sees.  The bound is that of ``bound``."""
+    x = q.double()
+    there = torch.arange(k["lo"].shape[1], device=x.device) < seen[:, None]
+    parts = lambda a: (a["lo"], a["step"], a["codes"])
+    (kl, ks, kc), (vl, vs, vc) = parts(k), parts(v)
+    dot = lambda c, y: (c * y[:, None, :]).sum(-1)
+    logit = (dot(kc, x) * ks + kl * x.sum(-1, keepdim=True)) * scale
+    logit = torch.where(there, logit, -math.inf)
+    want_lse = torch.logsumexp(logit, -1)
+    some = seen > 0
+    w = torch.where(there, torch.exp(logit - torch.where(some, want_lse, 0.0)[:, None]), 0.0)
+    want = (w[..., None] * (vl[..., None] + vs[..., None] * vc)).sum(1)
+    top = x.abs().max(-1, keepdim=True).values
+    small = (x.abs() < 2.0 ** -9 * top).double()
+    e = ((dot(kc, x.abs()) * ks + kl.abs() * x.abs().sum(-1, keepdim=True)) * (x.shape[1] + 12) * 2.0 ** -23 + dot(kc, small) * ks * 2.0 ** -17 * top) * scale
+    e = torch.where(there, e, 0.0).max(-1).values
+    mass = (w[..., None] * ((vl + 8 * vs).abs()[..., None] + vs[..., None] * (vc - 8).abs())).sum(1)
+    rel = 2 * e + 2.0 ** -21 + (seen + 64) * 2.0 ** -23
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * rel)[:, None] * mass + 1e-37
+    far = (out.double() - want).abs() > tol
+    assert not far.any(), (far.any(-1).nonzero()[:5].tolist(), ((out.double() - want).abs() / tol).max().item())
+    assert (lse[~some] == -math.inf).all()
+    near = (lse.double() - want_lse).abs() <= e + 2.0 ** -20 + (seen + 64) * 2.0 ** -23 + 2.0 ** -23 * want_lse.abs()
+    assert near[some].all(), (lse.double() - want_lse)[some].abs().max().item()

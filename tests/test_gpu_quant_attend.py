@@ -11,7 +11,7 @@ import torch
 from paper_2602_01901_b200 import binding as qc
 from paper_2602_01901_b200 import quant
 
-from quant_util import DEV, check_attend, fill, gen, held, rows
+from quant_util import DEV, check_attend, check_attend_torch, fill, gen, held, held_torch, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -265,6 +265,68 @@ def test_long_sequences_against_torch_in_64_bits(head_dim, heads, group, n, page
         err = ((out[0, h].double() - want).norm() / want.norm()).item()
         assert err <= 2.0 ** -8, err
         assert abs(lse[0, h].item() - want_lse.item()) <= e + 2.0 ** -20 + (n + 64) * 2.0 ** -23
+
+
+@pytest.mark.parametrize("seqs,heads,group,head_dim,page,low,high,most", [
+    (70, 2, 1, 128, 16, 1, 130, 1),          # more sequences than one warp counts, units that are not cut
+    (300, 1, 8, 64, 32, 0, 700, 2),
+    (2048, 1, 1, 128, 16, 0, 90, 1),         # the most sequences
+    (2048, 1, 3, 64, 64, 0, 90, 2),
+    (100, 4, 4, 128, 16, 1, 3000, 1),        # ranges of one warp, cut
+    (60, 2, 1, 64, 16, 900, 5000, 3),
+    (24, 3, 2, 128, 32, 1, 6000, 1),
+    (9, 2, 16, 128, 16, 2000, 9000, 1),      # sixteen rows to a unit
+    (5, 1, 8, 64, 16, 100, 9000, 16),        # the most queries, in units of sixteen rows
+    (7, 1, 5, 128, 64, 100, 9000, 15),       # and in units of eight
+    (2, 2, 1, 128, 64, 40000, 41000, 1),     # few long ones: a unit in the ranges of many teams
+    (1, 1, 16, 64, 16, 60000, 60000, 1),
+    (1, 1, 1, 128, 16, 30001, 30001, 1),
+    (1, 1, 4, 128, 32, 50007, 50007, 2),
+    (130, 8, 1, 128, 16, 512, 512, 1),
+])
+def test_batches_of_many_kinds_against_torch_in_64_bits(seqs, heads, group, head_dim, page, low, high, most):
+    rng, g = random.Random(seqs + high), gen(seqs + high)
+    lens = [rng.randint(low, high) for _ in range(seqs)]
+    counts = [rng.randint(0 if seqs > 9 else 1, most) if most > 1 else 1 for _ in range(seqs)]
+    starts = [0]
+    for c in counts:
+        starts.append(starts[-1] + c)
+    total = sum(lens)
+    table = quant.PageTable.empty(seqs, max(1, -(-high // page)), page, sum(-(-n // page) for n in lens) + 1)
+    pools = [quant.empty_pool(heads, head_dim, page, table.free.numel()) for _ in "kv"]
+    for p in pools:
+        p.fill_(0xFF)
+    ids = i32(torch.randperm(seqs, generator=g).tolist())
+    k, v = (rows(total, heads, head_dim, g).to(DEV) for _ in "kv")
+    _, slots = quant.table_extend(table, i32(lens), seq_ids=ids, max_slots=total)
+    quant.append(pools[0], pools[1], slots, k, v, page)
+    q = torch.randn(max(1, starts[-1]), heads * group, head_dim, generator=g).bfloat16().to(DEV)
+    status = i32([0])
+    stream = quant.Stream(q, pools[0], pools[1], table.pages, table.lens)
+    out, lse = quant.attend(stream, heads, page, seq_ids=ids, starts=i32(starts), max_queries=most, status=status)
+    again, lse_again = quant.attend(stream, heads, page, seq_ids=ids, starts=i32(starts), max_queries=most)
+    assert int(status) == qc.QC_OK
+    used = starts[-1]
+    assert torch.equal(out[:used], again[:used]) and torch.equal(lse[:used], lse_again[:used])
+    first = [0]
+    for n in lens:
+        first.append(first[-1] + n)
+    k_held, v_held = held_torch(k), held_torch(v)
+    seq_of = torch.repeat_interleave(torch.arange(seqs), torch.tensor(counts))
+    picked = list(range(used)) if used * max(lens) * head_dim < 2e7 else sorted(rng.sample(range(used), max(1, min(used, int(2e7 / (max(lens) * head_dim))))))
+    for h in range(heads * group):
+        if heads * group > 8 and h not in (0, 1, heads * group - 1) and rng.random() < 0.5:
+            continue
+        j = h // group
+        for at in range(0, len(picked), max(1, int(2e7 / (max(lens + [1]) * head_dim)))):
+            part = picked[at: at + max(1, int(2e7 / (max(lens + [1]) * head_dim)))]
+            s = [int(seq_of[t]) for t in part]
+            seen = [max(0, lens[i] - (starts[i + 1] - 1 - t)) for t, i in zip(part, s)]
+            width = max(seen + [1])
+            place = torch.tensor([first[i] for i in s])[:, None] + torch.arange(width)
+            place = place.clamp_(max=max(0, total - 1)).to(DEV)
+            cut = lambda a: {name: x[place, j] for name, x in a.items()}
+            check_attend_torch(out[part, h], lse[part, h], q[part, h], cut(k_held), cut(v_held), torch.tensor(seen, device=DEV), head_dim ** -0.5)
 
 
 def test_pages_behind_four_gigabytes():

@@ -78,6 +78,14 @@ def test_attention_by_hand():
     assert O.attention([1.0], [([1.0], np.zeros((0, 1)), np.zeros((0, 1)))], 1.0)[1] == -math.inf
 
 
+def test_many_rows_at_once_are_held_as_one_by_one():
+    from quant_util import gen, held, held_torch, rows
+
+    x = rows(200, 2, 64, gen(5))
+    a, b = held(x), held_torch(x)
+    assert all(np.array_equal(a[name], b[name].numpy()) for name in ("lo", "codes")) and np.allclose(a["step"], b["step"].numpy(), rtol=1e-15)
+
+
 # ---- refusals of the C calls: none of them touches a device -------------------------------------------
 
 OK_TABLE = dict(max_seqs=4, max_pages=3, page_size=16, n_pages=9, pages_dev=64, lens_dev=64, free_dev=64, state_dev=64)
