@@ -5,8 +5,8 @@
 //   sum_j p_j v_j = sum_j (p_j s_j)(c_jd - 8) + sum_j p_j (lo_j + 8 s_j)
 // and the long sums run over codes, which take next to no conversion: masked out of a word they are fp16 numbers already,
 // c * 2^-24 (subnormal ones, whose steps are equal), or 16 times that from the upper half of a byte.  The queries are exact in
-// fp16 once a power of two has brought the row's largest element below 2^15 (bf16 has fewer bits; what is below 2^-24 of the
-// largest loses some).  The weights p_j s_j are rounded to fp16 (2^-11) after a division by a power of two not below the
+// fp16 once a power of two has brought the unit's largest element below 2^15 (bf16 has fewer bits; what is below 2^-21 of the
+// largest loses some, 2^-35 of the largest at most).  The weights p_j s_j are rounded to fp16 (2^-11) after a division by a power of two not below the
 // largest s so far.  Everything else is fp32.  The 8 is taken off tile by tile, as a product with ones: sums of c alone
 // would grow with the keys, and the tensor cores' adder, which cuts off, would leave a part of them behind.
 //
@@ -16,7 +16,12 @@
 // With four query rows or fewer the eight columns hold them twice, with two or one four times.  Every lane then has the
 // scores of all four blocks of a tile for the same rows, and weighs one half or one quarter of them: each set of columns sums up
 // its own blocks, and the sets are put together like the sums of different warps.  (One row, eight sequences of 8 541
-// tokens: XX us with eight columns of which one counts, YY so.)
+// tokens, 32 heads: 67.0 us with eight columns of which one counts, 64.5 so; 16 sequences of 60 to 5 000: 32.6 and 29.7.)
+//
+// What bounds it: the bytes, 68 per row of 128 elements, would take 45 us of those 64.5.  A tile of 64 keys is some 930
+// instructions of a warp, of which 128 are products; masks and shifts run at half the rate of other instructions and the products at an
+// eighth, so that the ALUs and the tensor pipe, not the memory, are busy most of the time.  Small batches are bound by a
+// block's start: the plan, page ids, first tiles, sums and the join follow one another, 9.6 us for one sequence.
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -30,15 +35,14 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kUnitCost = 4;         // what a unit costs each warp besides its tiles, in tiles
-constexpr uint32_t kLongUnit = 512;   // tiles of the average unit from which on teams have eight warps
+constexpr int kUnitCost = 4;         // what a unit costs each warp besides its tiles, in tiles (its first tiles' way, the sums; 1: 33.8 us instead of
+                                     // 29.7 for 16 sequences of 60 to 5 000 tokens, 32 heads; 70.4 instead of 65.0 for three of 90 000)
+// Tiles per warp below which units are shared out among warps.  More rows make more of a unit's pieces: 24 ragged sequences with
+// five queries, 8 heads of 4, 64 wide, take 32.3 us with 3 and 26.2 with 6 or 12, 16 sequences of 4 000 tokens with five
+// queries, 4 heads of 4, 41.2 with 6 and 35.6 with 12, 16 ragged ones of one row 32.5 with 6 and 30.7 with 3.
 template <int ROWS>
-constexpr uint32_t kFewTiles = ROWS == 2 ? 3 : 6;   // per warp: of a batch with fewer, units are shared out among warps (more rows
-                                                    // make more of a unit's pieces: drafts on 64-wide heads, 16 rows, 29 us against
-                                                    // 42 with teams of one warp; 16 ragged sequences of one row 31 against 28.5)
-constexpr int64_t kSmallBatch = 8192; // tiles: up to so many blocks of eight warps (32 sequences of 1 375 tokens, 4 heads of 7: 14.0 us
-                                      // against 17.8; eight of 8 541, 32 heads: 73.9 against 68.5)
-constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut
+constexpr uint32_t kFewTiles = ROWS == 2 ? 3 : 12;
+constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut (one sequence of 707 tokens, 32 heads: 9.6 us, cut 22.8)
 constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
 
 struct StreamArgs {
@@ -502,9 +506,10 @@ __device__ __forceinline__ void add_values(Rows<D, NT>& R, const uint32_t (&w)[k
 // number of 64 bits, so the workspace needs no clearing.)  Where units are short next to that, or next to a range, a
 // team takes those that begin in its range whole, and nothing is left to put together.
 //
-// Teams of one warp are the even ones: with teams of eight, a range of many short units costs more than one of a long unit
-// (16 sequences of 1 to 5 000 tokens, 32 heads: XX us with eight, YY with one).  Eight where units are long (fewer sums to leave
-// behind), and as many as there are warps for where the whole batch is small.
+// Teams of one warp are the even ones: with teams of a whole block, a range of many short units costs more than one of a long
+// unit (16 sequences of 60 to 5 000 tokens, 32 heads: 52.2 us with whole blocks, 29.7 with single warps; 40 sequences of
+// 33 000, 4 heads of 4: 142 and 135).  Whole blocks only where there are fewer units than blocks, two or four warps
+// where the whole batch is small.
 
 struct Place {       // one sequence
   int64_t token0;    // its first query
@@ -614,7 +619,7 @@ __device__ __forceinline__ float* piece_at(const AttendArgs& A, int team, int pl
 template <int D, int ROWS>
 __device__ __noinline__ void merge_pieces(const AttendArgs& A, uint32_t first_team, uint32_t last_team, uint32_t first_place, int member, int warps, int n_here,
                                           int row0, int64_t token0, int kvh, int lane) {
-          constexpr int kCols = 4;      // columns side by side: each one's sums are two trips to the L2 after one another
+  constexpr int kCols = 4;      // columns side by side: each one's sums are two trips to the L2 after one another
   for (int col0 = member; col0 < n_here; col0 += kCols * warps) {
     float o[kCols][D / 32] = {};
     Joined J[kCols];
@@ -673,13 +678,16 @@ struct Work {
   int32_t kvh, row0, first, last;                                           // the unit, and its tiles that are in the range
   uint32_t unit_at, at, end;                                                // where the unit begins, where the next one does, where the range ends
   int32_t seq, whole_units, found, warps;
-  uint32_t per, longer, more, per_tile, team;                                         // cost of a range, ranges that cost one more, cost of a unit besides its tiles, and of a tile
+  uint32_t per, longer, more, per_tile, team;   // cost of a range, ranges that cost one more, cost of a unit besides its tiles, and of a tile
 };
 
-// One block per SM: of twelve warps (168 registers a thread), or of eight (255), which are sooner done with a small batch and
-// have too little on their way for a large one.
-template <int D, int NT, int REP, int kAttWarps>
-__global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+// One block per SM, of twelve warps (168 registers a thread; eight with 255 have too little on their way: 69.9 us instead of 64.5
+// for eight sequences of 8 541 tokens, 32 heads).  With sixteen rows to a unit eight warps, or its sums would not stay in registers.
+template <int NT>
+constexpr int kWarpsOf = NT == 1 ? 12 : 8;
+template <int D, int NT, int REP>
+__global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(const __grid_constant__ AttendArgs A) {
+  constexpr int kAttWarps = kWarpsOf<NT>;
   using R_ = Ring<D>;
   constexpr int kRow = D + 4;            // of a column's sums in shared memory
   constexpr int kRows = 8 * NT / REP;    // query rows of a unit
@@ -757,23 +765,26 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
   const uint32_t tiles_all = sums_.x, units = sums_.y, longest = longest_;
   const uint32_t n_warps = gridDim.x * kAttWarps;
   uint32_t team_warps = 1;
-  if (tiles_all >= units * kLongUnit || units * kAttWarps <= n_warps) team_warps = kAttWarps;
+  if (units * kAttWarps <= n_warps) team_warps = kAttWarps;
   else if (tiles_all <= n_warps * kFewTiles<kRows>) team_warps = units * 4 <= n_warps ? 4 : units * 2 <= n_warps ? 2 : 1;
   const int shift = team_warps == 2 ? 1 : team_warps == 4 ? 2 : 0;      // (of the teams that are not a whole block)
   const uint32_t n_teams = team_warps == kAttWarps ? gridDim.x : n_warps >> shift;
-  // a team for every unit, each one short: one each, whatever they cost
+  // a team for every unit, each one short: one each, whatever they cost.  Else a unit's cost is at most a range's share of the tiles:
+  // a whole range would have nothing but a cost to cover (one sequence of 32 000 tokens, 8 heads of 8: 27.0 us without that, 23.9 so)
   const bool one_each = units <= n_teams && longest <= team_warps * kWholeTiles;
-  const uint32_t more = one_each ? 1 : kUnitCost * team_warps, per_tile = one_each ? 0 : 1, cost = tiles_all * per_tile + units * more;
+  const uint32_t more = one_each ? 1 : max(1u, min(kUnitCost * team_warps, tiles_all / n_teams)), per_tile = one_each ? 0 : 1, cost = tiles_all * per_tile + units * more;
   // ranges of per_team or one more
   uint32_t per_team = cost / n_teams, longer = cost - per_team * n_teams;
   const bool whole_units = longest <= max(team_warps * kWholeTiles, per_team / 8);
-  if (!whole_units && per_team < team_warps + more) per_team = team_warps + more, longer = 0;
+  if (!whole_units && per_team < team_warps) per_team = team_warps, longer = 0;
   const auto before_cost = [&](int s) { return before[s].x * per_tile + before[s].y * more; };
   const int in_block = team_warps == kAttWarps ? 0 : warp >> shift, member = team_warps == kAttWarps ? warp : warp & (team_warps - 1);
   volatile Work& W = work_[in_block];
   if (lane == 0) me_[warp] = make_int2(in_block, member);
   if (member == 0 && lane == 0) {
-    const uint32_t team = team_warps == kAttWarps ? blockIdx.x : blockIdx.x * (kAttWarps >> shift) + in_block;
+    // where there are more teams than units, those that find nothing to do are spread over the chip (64 sequences of 20 to 100
+    // tokens, 8 heads of 8: 10.5 us against 11.7); else adjacent ranges share an SM (16 ragged sequences: 29.5 against 30.6)
+    const uint32_t team = one_each ? in_block * gridDim.x + blockIdx.x : blockIdx.x * (kAttWarps / team_warps) + in_block;
     const uint32_t at = min(static_cast<uint64_t>(team) * per_team + min(team, longer), static_cast<uint64_t>(cost));
     W.warps = team_warps, W.team = team, W.per = per_team, W.longer = longer, W.more = more, W.per_tile = per_tile, W.whole_units = whole_units;
     W.at = at, W.end = min(cost, at + per_team + (team < longer ? 1 : 0));
@@ -785,6 +796,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     }
     W.seq = lo;
   }
+  __syncthreads();      // every warp knows its team, and the team's size
   const uint32_t ring = smem_u32(smem) + warp * R_::kBytes;
   while (true) {
     if (me_[warp].y == 0) {   // the team's first warp finds its next unit
@@ -940,7 +952,8 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     uint32_t first_team = team, last_team = team, first_place = 0;
     if (!whole) {
       const uint32_t per = W.per, longer = W.longer, turn = longer * (per + 1);      // where the shorter ranges begin
-      const auto team_at = [&](uint32_t p) { return p < turn ? p / (per + 1) : longer + (p - turn) / per; };
+      const uint32_t most = gridDim.x * (kAttWarps / warps) - 1;
+      const auto team_at = [&](uint32_t p) { return min(most, p < turn ? p / (per + 1) : longer + (p - turn) / per); };
       first_team = team_at(unit_at + W.more), last_team = team_at(unit_at + W.tiles + W.more - 1);
       first_place = unit_at > first_team * per + min(first_team, longer) ? 1 : 0;
     }
@@ -991,6 +1004,7 @@ __global__ void __launch_bounds__(kAttWarps * 32, 1) quant_attend_kernel(const _
     if (!whole) {
       team_barrier(in_block, threads);
       if (member == 0) {
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");      // the piece, which other warps wrote a part of, is there before its flag
         if (lane == 0) atomicExch(A.flags + 2 * team + place, A.nonce);
         __syncwarp();
         asm volatile("fence.sc.gpu;" ::: "memory");
@@ -1035,9 +1049,9 @@ int32_t check_sizes(const qc_quant_attend_args* a) {
   return QC_OK;
 }
 
-// Query rows of a unit: as many columns of a product as they need.  Sixteen only where they are all taken (sequences of 8 000
-// tokens, 4 heads of 8, 64 wide, two queries: 31 us against 37 with units of eight; with one to five queries on 4 heads of 4,
-// 128 wide, 30 against 26).
+// Query rows of a unit: as many columns of a product as they need.  Sixteen only where they are all taken (16 sequences of 8 000
+// tokens, 4 heads of 8, 64 wide, two queries: 31.2 us against 37.3 with units of eight; with one to five queries on 4 heads of
+// 4, 128 wide, 30 against 26).
 int unit_rows(const qc_quant_attend_args* a) {
   const int64_t rows = static_cast<int64_t>(a->max_queries) * (a->n_q_heads / a->n_kv_heads);
   return rows <= 2 ? 2 : rows <= 4 ? 4 : rows % 16 ? 8 : 16;
@@ -1056,14 +1070,15 @@ unsigned long long next_nonce() {
   return x ? x : 1;
 }
 
-template <int D, int NT, int REP, int kAttWarps>
+template <int D, int NT, int REP>
 cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
+  constexpr int kAttWarps = kWarpsOf<NT>;
   const int smem = kAttWarps * Ring<D>::kBytes + (A.n_seqs + 1) * 8;
   constexpr int kMost = kAttWarps * Ring<D>::kBytes + (QC_QUANT_MAX_SEQS + 1) * 8;
   static std::atomic<bool> configured[64] = {};     // per device: the kernel may take that much
   cudaError_t e;
   if (device >= 64 || !configured[device].load(std::memory_order_relaxed)) {
-    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP, kAttWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    e = cudaFuncSetAttribute(quant_attend_kernel<D, NT, REP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     if (device < 64) configured[device].store(true, std::memory_order_relaxed);
   }
@@ -1072,12 +1087,13 @@ cudaError_t launch(AttendArgs& A, int device, cudaStream_t stream) {
   int blocks = sms;
   if (blocks > kMostTeams / kAttWarps) blocks = kMostTeams / kAttWarps;
   A.nonce = next_nonce();
-  return launch_pdl(quant_attend_kernel<D, NT, REP, kAttWarps>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
+  return launch_pdl(quant_attend_kernel<D, NT, REP>, dim3(blocks), dim3(kAttWarps * 32), smem, stream, A);
 }
 
-template <int D, int REP>
-cudaError_t launch_rows(AttendArgs& A, int device, bool small, cudaStream_t stream) {
-  return small ? launch<D, 1, REP, 8>(A, device, stream) : launch<D, 1, REP, 12>(A, device, stream);
+template <int D>
+cudaError_t launch_rows(AttendArgs& A, int rows, int device, cudaStream_t stream) {
+  return rows == 2 ? launch<D, 1, 4>(A, device, stream) : rows == 4 ? launch<D, 1, 2>(A, device, stream) : rows == 8 ? launch<D, 1, 1>(A, device, stream)
+                                                                                                                   : launch<D, 2, 1>(A, device, stream);
 }
 
 size_t workspace_bytes(const qc_quant_attend_args* a) {
@@ -1130,14 +1146,7 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  cudaError_t e;
-  // the most tiles that the tables have room for, over all units
   const int rows = unit_rows(args);
-  const int64_t pages = static_cast<int64_t>(args->text.max_pages) + (A.has_visual ? v.max_pages : 0);
-  const bool small = ((pages * A.page + kTile - 1) / kTile) * A.n_seqs * A.hkv <= kSmallBatch;
-  if (args->head_dim == 128) e = rows == 2 ? launch_rows<128, 4>(A, device, small, stream) : rows == 4 ? launch_rows<128, 2>(A, device, small, stream)
-                               : rows == 8 ? launch_rows<128, 1>(A, device, small, stream) : launch<128, 2, 1, 8>(A, device, stream);
-  else e = rows == 2 ? launch_rows<64, 4>(A, device, small, stream) : rows == 4 ? launch_rows<64, 2>(A, device, small, stream)
-           : rows == 8 ? launch_rows<64, 1>(A, device, small, stream) : launch<64, 2, 1, 8>(A, device, stream);
+  const cudaError_t e = args->head_dim == 128 ? launch_rows<128>(A, rows, device, stream) : launch_rows<64>(A, rows, device, stream);
   return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
 }

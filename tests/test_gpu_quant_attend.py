@@ -329,6 +329,29 @@ def test_batches_of_many_kinds_against_torch_in_64_bits(seqs, heads, group, head
             check_attend_torch(out[part, h], lse[part, h], q[part, h], cut(k_held), cut(v_held), torch.tensor(seen, device=DEV), head_dim ** -0.5)
 
 
+@pytest.mark.parametrize("seqs,heads,group,head_dim,tokens", [(1, 1, 1, 128, 30000), (3, 2, 4, 64, 9001), (30, 8, 1, 128, 1900), (40, 4, 16, 64, 700)])
+def test_a_captured_call_gives_the_same_bits_each_time(seqs, heads, group, head_dim, tokens):
+    g, page = gen(tokens), 32
+    per = -(-tokens // page)
+    table = quant.PageTable.empty(seqs, per, page, seqs * per)
+    pools = [torch.empty_like(quant.empty_pool(heads, head_dim, page, seqs * per)) for _ in "kv"]
+    _, slots = quant.table_extend(table, torch.full((seqs,), tokens, dtype=torch.int32, device=DEV), max_slots=seqs * tokens)
+    rows_ = torch.randn(seqs * tokens, heads, head_dim, generator=g).bfloat16().to(DEV)
+    quant.append(pools[0], pools[1], slots, rows_, rows_.flip(0).contiguous(), page)
+    q = torch.randn(seqs, heads * group, head_dim, generator=g).bfloat16().to(DEV)
+    stream = quant.Stream(q, pools[0], pools[1], table.pages, table.lens)
+    want, want_lse = quant.attend(stream, heads, page)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [quant.attend(stream, heads, page) for _ in range(4)]
+    for _ in range(50):
+        for out, lse in outs:
+            out.fill_(7)
+        graph.replay()
+        for out, lse in outs:
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 def test_pages_behind_four_gigabytes():
     heads, head_dim, page = 32, 128, 64
     per = heads * page * (head_dim // 2 + 4)
