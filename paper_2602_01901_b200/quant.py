@@ -4,7 +4,7 @@ The calls of ``include/qc.h`` on torch tensors: every buffer is the caller's, ev
 stream of the tensors' device and returns at once, and nothing is kept between calls, so a step can be captured into a
 ``torch.cuda.graph`` and replayed while its sequences grow.  Arguments that a call can see on the host are checked here
 or by the library (``ValueError``, ``QcError``); numbers on the device (ids, lengths, pages) are checked there and end in
-the table's status word (``PageTable.check``).
+the table's status word (``PageTable.check``).  No gradient flows through any of them.
 
     table = PageTable.empty(max_seqs, max_pages, page_size, n_pages)
     k_pool, v_pool = (empty_pool(n_kv_heads, head_dim, page_size, n_pages) for _ in "kv")      # of each layer
@@ -46,13 +46,17 @@ def _cuda(device) -> torch.device:
 
 class PageTable:
     """Page table of one stream (``qc_table``) over the caller's int32 tensors: ``pages`` [max_seqs, max_pages],
-    ``lens`` [max_seqs], ``free`` [n_pages], ``state`` [4]."""
+    ``lens`` [max_seqs], ``free`` [n_pages], ``state`` [4].  It is these tensors for good: others make another table."""
 
     __slots__ = ("pages", "lens", "free", "state", "page_size", "packed")
 
     def __init__(self, pages: torch.Tensor, lens: torch.Tensor, free: torch.Tensor, state: torch.Tensor, page_size: int):
-        self.packed = _native().table(pages, lens, free, state, page_size)
-        self.pages, self.lens, self.free, self.state, self.page_size = pages, lens, free, state, page_size
+        packed = _native().table(pages, lens, free, state, page_size)
+        for name, value in zip(self.__slots__, (pages, lens, free, state, page_size, packed)):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):      # (the packed structure holds the tensors' addresses)
+        raise AttributeError(f"{name} of a PageTable stays what it is")
 
     @classmethod
     def empty(cls, max_seqs: int, max_pages: int, page_size: int, n_pages: int, device=0) -> "PageTable":
@@ -128,5 +132,5 @@ def attend(text: Stream, n_kv_heads: int, page_size: int, *, visual: Optional[St
     Sequence i is row ``seq_ids[i]`` (None: i) of the tables and has query tokens ``starts[i]`` to ``starts[i + 1] - 1`` (None:
     token i), ``max_queries`` at most.  ``causal``: they are the last tokens of the text stream, and none sees what is behind
     it.  Returns (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); a query that sees nothing gets 0
-    and minus infinity.  ``status``: an int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
+    and minus infinity; tokens of no sequence stay what they were in ``out`` (where it is made here, anything).  ``status``: an int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
     return _native().attend(text, n_kv_heads, page_size, visual, seq_ids, starts, max_queries, causal, scale, out, status)

@@ -65,6 +65,14 @@ def test_tables_follow_the_integer_model_through_a_random_run(page, seqs, most):
     assert int(table.state[0]) == n_pages
 
 
+def test_a_table_stays_with_its_tensors():
+    table = quant.PageTable.empty(2, 3, 16, 5)
+    for name in quant.PageTable.__slots__:
+        with pytest.raises(AttributeError):
+            setattr(table, name, getattr(table, name))
+    table.check()
+
+
 def test_one_token_each_without_lists_and_slots_of_a_long_call():
     table, model = quant.PageTable.empty(7, 3000, 16, 7 * 3000), O.Table(7, 3000, 16, 7 * 3000)
     for _ in range(18):
