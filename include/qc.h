@@ -381,6 +381,7 @@ int32_t qc_attend_static(int32_t device, void* cuda_stream, const void* q_dev, c
 #define QC_QUANT_MAX_HEADS 1024
 #define QC_QUANT_MAX_SEQS 2048    /* sequences in one qc_quant_attend */
 #define QC_QUANT_MAX_QUERIES 16   /* query tokens of one sequence in one qc_quant_attend */
+#define QC_QUANT_MAX_TOKENS (1 << 30)   /* tokens of one qc_quant_append or qc_quant_read, slots of one qc_table_extend */
 
 /* Page table of one stream, all arrays int32 on the device. */
 typedef struct qc_table {
@@ -483,7 +484,11 @@ int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes
  * A query that sees no key gets 0 and lse minus infinity.  Rows of out that belong to no listed sequence are left as
  * they are, and so are those of a sequence whose row or query numbers are out of range (QC_ERR_INVALID_ARG in the status
  * word).  A page id that is not in the pool is not followed: its keys count as absent (QC_ERR_BAD_PAGE).  A length
- * beyond the table's room is cut to it (QC_ERR_PLAN). */
+ * beyond the table's room is cut to it (QC_ERR_PLAN).  A batch that is too much for one call (over 2^32 rows of K, counted
+ * once per KV head and per 2, 4, 8 or 16 query rows, or a sequence with more than 2^28 of them) is not computed at all
+ * (QC_ERR_PLAN): out stays as it was.
+ * Query elements are kept to 2^-35 of the largest element among the up to 16 query rows of a sequence that share a KV head's rows;
+ * a row with an element of 2^101 or more in size, infinite or no number gets NaN. */
 int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend_args* args);
 
 const char* qc_status_string(int32_t status);

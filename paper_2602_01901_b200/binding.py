@@ -330,6 +330,7 @@ QC_TABLE_MAX_SEQS = 65536
 QC_QUANT_MAX_HEADS = 1024
 QC_QUANT_MAX_SEQS = 2048
 QC_QUANT_MAX_QUERIES = 16
+QC_QUANT_MAX_TOKENS = 1 << 30
 
 
 def qc_table_reset(device: int, cuda_stream: int, table: qc_table) -> None:

@@ -11,7 +11,8 @@
 // block of the page.  Its lanes hold what the attention's lanes read (see qc_quant.cuh), K a quarter of two
 // tokens' rows and V an eighth of four tokens', so codes go to and from a page as whole vectors in lane order, and
 // V's words, which hold four tokens, are put together in registers.  (With four tokens a warp and the exchanges that takes,
-// 10 813 tokens of 32 heads took 56 us to store and 57 to read; XX and YY so.)
+// 10 813 tokens of 32 heads took 111 us to store and read back; 76.7 so, of which 61 are their bytes at the copy rate and 7
+// the codes' second trip.  A step of 32 tokens is two launches' time, 3.6 us.)
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -22,7 +23,6 @@ namespace qc {
 namespace {
 
 constexpr int kRowWarps = 8;       // warps of a block, one head each
-constexpr int64_t kFewRows = 4096;
 constexpr float kLeastSpan = 7.8886090522101181e-31f;   // 2^-100
 
 struct RowArgs {
@@ -35,7 +35,7 @@ struct RowArgs {
   uint16_t* k_out;         // read: rows out
   uint16_t* v_out;
   int64_t page_bytes, code_bytes;
-  int32_t n_tokens, hkv, page_shift, n_pages, window, group_mask;
+  int32_t n_tokens, hkv, page_shift, n_pages, window;
   bool has_k;              // blocks of z = 0 take K (and those of z = 1 V), else all take V
   bool wide;               // read: rows out begin at multiples of 32 bytes
 };
@@ -71,7 +71,7 @@ __device__ __forceinline__ void for_groups(const RowArgs& T, int lane, Fn fn) {
   };
   const int32_t slot = slot_at(tok);
   const int32_t left = __shfl_up_sync(0xffffffffu, slot, 1);
-  const bool begins = slot >= 0 && (lane == 0 || (slot & T.group_mask) == 0 || left != slot - 1);
+  const bool begins = slot >= 0 && (lane == 0 || (slot & 15) == 0 || left != slot - 1);
   const bool follows = slot >= 0 && !begins;
   uint32_t todo = __ballot_sync(0xffffffffu, begins);
   const uint32_t followers = __ballot_sync(0xffffffffu, follows);
@@ -159,7 +159,8 @@ __device__ __forceinline__ void places_of(const RowArgs& T, int32_t block, int h
 }
 
 // Grid: (windows of T.window tokens, groups of kRowWarps heads, K and V: tensors in blocks of their own, or one warp would hold
-// both's rows in registers and too few would be on their way).
+// both's rows in registers and too few would be on their way).  Four blocks an SM here and six in the read: 76.7 us for those
+// 10 813 tokens, 80.8 with the registers that the compiler takes by itself.
 template <int D>
 __global__ void __launch_bounds__(kRowWarps * 32, 4) quant_append_kernel(const __grid_constant__ RowArgs T) {
   constexpr int kK = D / 4, kV = D / 8;      // elements of a row per lane
@@ -312,12 +313,9 @@ void place(RowArgs& a, const qc_quant_shape* s, int32_t n_tokens) {
   a.n_tokens = n_tokens, a.hkv = s->n_kv_heads, a.n_pages = s->n_pages;
   a.page_shift = s->page_size == 16 ? 4 : s->page_size == 32 ? 5 : 6;
   a.page_bytes = quant_page_bytes(a.hkv, s->head_dim, s->page_size), a.code_bytes = static_cast<int64_t>(a.hkv) * s->page_size * (s->head_dim / 2);
-  // a batch's single tokens lie in blocks of their own: one token per warp, so that none waits for another.  Groups of four
-  // tokens as long as those of 16 would leave most of the chip idle.
-  const int64_t rows = static_cast<int64_t>(n_tokens) * a.hkv;
+  // a batch's single tokens lie in blocks of their own: one token per warp, so that none waits for another (32 tokens: 3.6 us
+  // against 8.0)
   a.window = n_tokens <= 512 ? 1 : 16;
-  a.group_mask = rows <= kFewRows ? 3 : 15;
-  if (a.group_mask == 3 && a.window == 16) a.window = 4;
 }
 
 dim3 grid_of(const RowArgs& a, bool both) { return dim3((a.n_tokens + a.window - 1) / a.window, (a.hkv + kRowWarps - 1) / kRowWarps, both ? 2 : 1); }
@@ -341,6 +339,7 @@ extern "C" int32_t qc_quant_append(int32_t device, void* cuda_stream, const qc_q
                                    void* v_pool_dev) {
   if (const int32_t bad = check_shape(shape)) return bad;
   if (n_tokens < 0 || (!k_dev) != (!k_pool_dev) || (!v_dev) != (!v_pool_dev) || (!k_dev && !v_dev)) return QC_ERR_INVALID_ARG;
+  if (n_tokens > QC_QUANT_MAX_TOKENS) return QC_ERR_UNSUPPORTED;
   if (n_tokens == 0) return QC_OK;
   if (!slots_dev || (reinterpret_cast<uintptr_t>(slots_dev) & 3)) return QC_ERR_INVALID_ARG;
   if (off16(k_dev) || off16(v_dev) || off16(k_pool_dev) || off16(v_pool_dev)) return QC_ERR_INVALID_ARG;
@@ -364,6 +363,7 @@ extern "C" int32_t qc_quant_read(int32_t device, void* cuda_stream, const qc_qua
                                  const void* k_pool_dev, const void* v_pool_dev, void* k_out_dev, void* v_out_dev) {
   if (const int32_t bad = check_shape(shape)) return bad;
   if (n_tokens < 0 || (!k_out_dev) != (!k_pool_dev) || (!v_out_dev) != (!v_pool_dev) || (!k_out_dev && !v_out_dev)) return QC_ERR_INVALID_ARG;
+  if (n_tokens > QC_QUANT_MAX_TOKENS) return QC_ERR_UNSUPPORTED;
   if (n_tokens == 0) return QC_OK;
   if (!slots_dev || (reinterpret_cast<uintptr_t>(slots_dev) & 3)) return QC_ERR_INVALID_ARG;
   if (off16(k_pool_dev) || off16(v_pool_dev) || off16(k_out_dev) || off16(v_out_dev)) return QC_ERR_INVALID_ARG;

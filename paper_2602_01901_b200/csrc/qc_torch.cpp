@@ -1,8 +1,7 @@
 // The calls on a 4-bit cache taken straight from torch tensors (module _qc_torch, used by quant.py).
 //
-// What a call checks and packs is some forty tensor attributes.  From Python through ctypes that took the host 14 us for one
-// attention call (21 us with its allocations and the launch), more than the kernel runs for a small batch; from here it is
-// 1 us.  The calls keep nothing, enqueue on the current stream of the tensors' device, and raise ValueError for
+// What a call checks and packs is some forty tensor attributes.  An attention call, its allocations and its launch took the host
+// 28 us from Python through ctypes, more than the kernel runs for a small batch; from here they take 8.  The calls keep nothing, enqueue on the current stream of the tensors' device, and raise ValueError for
 // arguments that do not fit and QcError for a status of the library.
 
 #define PY_SSIZE_T_CLEAN

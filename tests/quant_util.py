@@ -48,9 +48,9 @@ def fill(table, ids, lens, page, pools, k, v, device=DEV):
 def bound(queries, keys, values, scale, out, weights):
     """How far an output row may be from the one in 64 bits, element by element, and its lse; `weights`: the softmax's.
 
-    A score is s * sum q c + lo * sum q.  A query element is exact in fp16 with the row's largest in 2^14 .. 2^15
-    (half of them divided by 16 before), or off by half of the least step, 2^-25 times 16, where it is below 2^-9: by 2^-34
-    of the row's largest at most; 2^-17 where it is below 2^-9 of it is allowed for.  The products are exact and summed in fp32: every
+    A score is s * sum q c + lo * sum q.  A query element is exact in fp16 with the largest of the rows computed together in
+    2^14 .. 2^15 (half of them divided by 16 before), or off by half of the least step, 2^-25 times 16: by 2^-35 of that largest
+    one at most; 2^-17 of the row's own largest is allowed for elements below 2^-9 of it.  The products are exact and summed in fp32: every
     one of the D + 8 steps is off by 2^-23 of the sum's largest magnitude at most (an adder that cuts off), as are the
     four roundings around it; |score| is bounded with absolute values.  The exponential adds 2^-22 of itself and the rounding of its argument.  The
     weights p s are rounded to fp16 (2^-11) before the product with c - 8; the sums over L keys, in fp32, are off by

@@ -136,6 +136,13 @@ def test_a_shape_that_is_none_is_refused(change, status):
     assert status_of(lambda: qc.qc_quant_read(0, 0, s, 1, 64, 64, 64, 64, 64)) == status
 
 
+def test_more_tokens_than_indexes_reach_are_refused():
+    t, s, n = qc.qc_table(**OK_TABLE), qc.qc_quant_shape(**SHAPE), qc.QC_QUANT_MAX_TOKENS + 1
+    assert status_of(lambda: qc.qc_table_extend(0, 0, t, 1, 0, 0, n, 64, 64)) == qc.QC_ERR_UNSUPPORTED
+    assert status_of(lambda: qc.qc_quant_append(0, 0, s, n, 64, 64, 256, 64, 256, 64, 64)) == qc.QC_ERR_UNSUPPORTED
+    assert status_of(lambda: qc.qc_quant_read(0, 0, s, n, 64, 64, 64, 64, 64)) == qc.QC_ERR_UNSUPPORTED
+
+
 def test_pool_bytes_and_row_arguments():
     s = qc.qc_quant_shape(**SHAPE)
     assert qc.qc_quant_pool_bytes(s) == 5 * 2 * 16 * 68
