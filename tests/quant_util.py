@@ -50,24 +50,33 @@ def bound(queries, keys, values, scale, out, weights):
 
     A score is s * sum q c + lo * sum q.  A query element is exact in fp16 with the largest of the rows computed together in
     2^14 .. 2^15 (half of them divided by 16 before), or off by half of the least step, 2^-25 times 16: by 2^-35 of that largest
-    one at most; 2^-17 of the row's own largest is allowed for elements below 2^-9 of it.  The products are exact and summed in fp32: every
-    one of the D + 8 steps is off by 2^-23 of the sum's largest magnitude at most (an adder that cuts off), as are the
-    four roundings around it; |score| is bounded with absolute values.  The exponential adds 2^-22 of itself and the rounding of its argument.  The
-    weights p s are rounded to fp16 (2^-11) before the product with c - 8; the sums over L keys, in fp32, are off by
-    2^-23 per step of what they add up; the output is rounded to bf16 (2^-8).
+    one at most.  The products are exact and summed in fp32: every one of the D + 8 steps is off by 2^-23 of the sum's largest
+    magnitude at most (an adder that cuts off), as are the four roundings around it; |score| is bounded with absolute values.
+    The exponential adds 2^-22 of itself and the rounding of its argument.  The weights p s are rounded to fp16 (2^-11) before
+    the product with c - 8; the sums over L keys, in fp32, are off by 2^-23 per step of what they add up; s in lo + 8 s is off by
+    2^-23 of itself, 2^-20 p s; the output is rounded to bf16 (2^-8).
+
+    The adder lines up 16 addends and the sum so far by the operands' exponents, a subnormal code's being that of 2^-14: each
+    addend is cut off at 2^-15 of the largest query element (scores) or weight p s (values) among the 16, times one code.  An
+    addend whose factor is not below 2^-7 of the largest query element (8 bits) or 2^-4 of the largest weight (11 bits) has nothing
+    there; another loses no more than it is, 15 times the factor.  The codes' addends and those that take off the 8 are cut
+    off in opposite directions.  The sum so far is cut off D / 16 times for a score and eight times for a tile of 64 values.
     """
     n = sum(len(k["step"]) for k in keys)
     e = 0.0
     for q, k in zip(queries, keys):
         if len(k["step"]):
             part = k["codes"] @ np.abs(q) * k["step"] + np.abs(k["lo"]) * np.abs(q).sum()
-            small = np.abs(q) < 2.0 ** -9 * np.abs(q).max()
-            tiny = k["codes"] @ small.astype(float) * k["step"] * 2.0 ** -17 * np.abs(q).max()
-            e = max(e, scale * float((part * (q.size + 12) * 2.0 ** -23 + tiny).max()))
+            top = np.abs(q).max()
+            small = np.where(np.abs(q) < 2.0 ** -7 * top, np.minimum(2.0 ** -15 * top, 15 * np.abs(q)), 0.0).sum()
+            cut = k["step"] * (small + (q.size / 16 * 2.0 ** -15 * top if small else 0.0))
+            e = max(e, scale * float((part * (q.size + 12) * 2.0 ** -23 + cut).max()))
     size = np.concatenate([np.abs(v["lo"] + 8 * v["step"])[:, None] + v["step"][:, None] * np.abs(v["codes"] - 8) for v in values]) if n else np.zeros((1, out.size))
     mass = weights @ size if n else np.zeros(out.size)
+    ps = weights * np.concatenate([v["step"] for v in values]) if n else np.zeros(1)
+    cut = np.minimum(2.0 ** -15 * ps.max(), 15 * ps).sum() + 2.0 ** -12 * min((n / 64 + 2) * ps.max(), ps.sum())
     rel = 2 * e + 2.0 ** -21 + (n + 64) * 2.0 ** -23
-    return 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + 2 * rel) * mass + 1e-37, e + 2.0 ** -20 + (n + 64) * 2.0 ** -23
+    return 2.0 ** -8 * np.abs(out) + (2.0 ** -11 + 2 * rel) * mass + cut + 2.0 ** -20 * ps.sum() + 1e-37, e + 2.0 ** -20 + (n + 64) * 2.0 ** -23
 
 
 def check_attend(out, lse, starts, ids, lens, q, k_held, v_held, group, scale, causal=True, visual=None):
@@ -123,12 +132,16 @@ def check_attend_torch(out, lse, q, k, v, seen, scale):
     w = torch.where(there, torch.exp(logit - torch.where(some, want_lse, 0.0)[:, None]), 0.0)
     want = (w[..., None] * (vl[..., None] + vs[..., None] * vc)).sum(1)
     top = x.abs().max(-1, keepdim=True).values
-    small = (x.abs() < 2.0 ** -9 * top).double()
-    e = ((dot(kc, x.abs()) * ks + kl.abs() * x.abs().sum(-1, keepdim=True)) * (x.shape[1] + 12) * 2.0 ** -23 + dot(kc, small) * ks * 2.0 ** -17 * top) * scale
+    small = torch.where(x.abs() < 2.0 ** -7 * top, torch.minimum(2.0 ** -15 * top, 15 * x.abs()), 0.0).sum(-1, keepdim=True)
+    cut = ks * (small + torch.where(small > 0, x.shape[1] / 16 * 2.0 ** -15 * top, 0.0))
+    e = ((dot(kc, x.abs()) * ks + kl.abs() * x.abs().sum(-1, keepdim=True)) * (x.shape[1] + 12) * 2.0 ** -23 + cut) * scale
     e = torch.where(there, e, 0.0).max(-1).values
     mass = (w[..., None] * ((vl + 8 * vs).abs()[..., None] + vs[..., None] * (vc - 8).abs())).sum(1)
+    ps = w * vs
+    most = ps.max(-1).values
+    cut = torch.minimum(2.0 ** -15 * most[:, None], 15 * ps).sum(-1) + 2.0 ** -12 * torch.minimum((seen / 64 + 2) * most, ps.sum(-1))
     rel = 2 * e + 2.0 ** -21 + (seen + 64) * 2.0 ** -23
-    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * rel)[:, None] * mass + 1e-37
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2 * rel)[:, None] * mass + (cut + 2.0 ** -20 * ps.sum(-1))[:, None] + 1e-37
     far = (out.double() - want).abs() > tol
     assert not far.any(), (far.any(-1).nonzero()[:5].tolist(), ((out.double() - want).abs() / tol).max().item())
     assert (lse[~some] == -math.inf).all()
