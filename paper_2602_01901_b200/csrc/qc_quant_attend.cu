@@ -25,7 +25,7 @@
 // its own blocks, and the sets are put together like the sums of different warps.  (One row, eight sequences of 8 541
 // tokens, 32 heads: 67.0 us with eight columns of which one counts, 64.5 so; 16 sequences of 60 to 5 000: 32.6 and 29.7.)
 //
-// What bounds it: the bytes, 68 per row of 128 elements, would take 45 us of those 64.5.  A tile of 64 keys is some 930
+// What bounds it: the bytes, 68 per row of 128 elements, would take 45 us of those 64.5.  A tile of 64 keys is some 950
 // instructions of a warp, 68 of them products; masks and shifts run at half the rate of other instructions and the products at an
 // eighth, which together is about as long as the tile's bytes take.  Small batches are bound by a
 // block's start: the plan, page ids, first tiles, sums and the join follow one another, 9.6 us for one sequence.
