@@ -352,6 +352,16 @@ def test_a_captured_call_gives_the_same_bits_each_time(seqs, heads, group, head_
             assert torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
+@pytest.mark.parametrize("seqs,heads", [(1, 2), (40, 1), (100, 1)])      # one sequence too long, a batch too large, one of more sequences than a warp counts
+def test_a_batch_that_is_too_much_for_one_call_is_left_alone(seqs, heads):
+    pages, lens = torch.full((1, 1 << 22), -1, dtype=torch.int32, device=DEV), i32([1 << 28])
+    pool = quant.empty_pool(heads, 64, 64, 1).zero_()
+    q, status = torch.ones(seqs, heads, 64, dtype=torch.bfloat16, device=DEV), i32([0])
+    out = torch.full_like(q, 3)
+    quant.attend(quant.Stream(q, pool, pool, pages, lens), heads, 64, seq_ids=i32([0] * seqs), out=out, status=status)
+    assert int(status) == qc.QC_ERR_PLAN and bool((out == 3).all())
+
+
 def test_pages_behind_four_gigabytes():
     heads, head_dim, page = 32, 128, 64
     per = heads * page * (head_dim // 2 + 4)
