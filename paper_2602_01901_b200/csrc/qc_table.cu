@@ -246,9 +246,10 @@ int32_t check_batch(const TableArgs& a, int32_t n_seqs, const int32_t* ids, cons
 template <bool TRIM>
 int32_t launch_table(const TableArgs& a, bool many, void* cuda_stream) {
   const size_t smem = static_cast<size_t>(a.n_seqs) * sizeof(Seq) + (a.ids ? (a.max_seqs + 31) / 32 * 4 : 0);
-  // (always the most, so that two calls at once cannot take it from one another)
+  // 48 KB are there for a call's lists and the kernel's own variables (528 bytes) together; a longer list asks for more, well before
+  // that.  (Always the most, so that two calls at once cannot take it from one another.)
   constexpr int kMost = kTableMaxBatch * static_cast<int>(sizeof(Seq)) + kTableMaxSeqs / 8;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return QC_ERR_CUDA;
+  if (smem > 32 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return QC_ERR_CUDA;
   const int32_t work = a.max_slots > a.n_seqs ? a.max_slots : a.n_seqs;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(many ? kCluster : 1);
