@@ -487,8 +487,8 @@ int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes
  * beyond the table's room is cut to it (QC_ERR_PLAN).  A batch that is too much for one call (over 2^32 rows of K, counted
  * once per KV head and per 2, 4, 8 or 16 query rows, or a sequence with more than 2^28 of them) is not computed at all
  * (QC_ERR_PLAN): out stays as it was.
- * Query elements are kept to 2^-35 of the largest element among the up to 16 query rows of a sequence that share a KV head's rows;
- * a row with an element of 2^101 or more in size, infinite or no number gets NaN. */
+ * Query elements are kept to 2^-35 of the largest element of their row (token, head; a stream's); a row with an element of 2^101
+ * or more in size, infinite or no number gets NaN, and no other row is different for it. */
 int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend_args* args);
 
 const char* qc_status_string(int32_t status);

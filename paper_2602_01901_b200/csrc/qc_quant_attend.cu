@@ -4,9 +4,10 @@
 //   q . k_j       = s_j sum_d q_d c_jd + lo_j sum_d q_d
 //   sum_j p_j v_j = sum_j (p_j s_j)(c_jd - 8) + sum_j p_j (lo_j + 8 s_j)
 // and the long sums run over codes, which take next to no conversion: masked out of a word they are fp16 numbers already,
-// c * 2^-24 (subnormal ones, whose steps are equal), or 16 times that from the upper half of a byte.  The queries are exact in
-// fp16 once a power of two has brought the unit's largest element below 2^15 (bf16 has fewer bits; what is below 2^-21 of the
-// largest loses some, 2^-35 of the largest at most).  The weights p_j s_j are rounded to fp16 (2^-11) after a division by a power of two not below the
+// c * 2^-24 (subnormal ones, whose steps are equal), or 16 times that from the upper half of a byte.  A query row is exact in
+// fp16 once a power of two of its own has brought its largest element below 2^15 (bf16 has fewer bits; what is below 2^-21 of the
+// largest loses some, 2^-35 of the largest at most), so a row does not depend on those beside it: columns of a product are
+// separate sums.  The weights p_j s_j are rounded to fp16 (2^-11) after a division by a power of two not below the
 // largest s so far.  Everything else is fp32.  The 8 is taken off tile by tile, as a product with ones: sums of c alone
 // would grow with the keys, and the tensor cores' adder, which cuts off, would leave a part of them behind.
 //
@@ -110,9 +111,9 @@ __device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 constexpr uint32_t kLower = 0x000f000fu, kUpper = 0x00f000f0u;   // codes as two fp16 numbers: c * 2^-24, and c * 2^-20
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {      // NaN if one is
   uint32_t d;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t a) {
@@ -136,7 +137,7 @@ template <int D, int NT>
 struct Query {
   uint32_t b[NT][D / 16][2];   // operands of the score products: lower codes' elements, and a 16th of the upper ones'
   float sum[NT][2];            // sum of the elements times 2^-24, for the columns 2 t and 2 t + 1
-  float scale;                 // softmax scale * log2 e * the powers of two that were taken out
+  float scale[NT][2];          // softmax scale * log2 e * the powers of two that were taken out of the column
 };
 
 // Row r of a unit is query r / group of the sequence, head r % group of the KV head.
@@ -161,24 +162,22 @@ template <int D, int NT>
 __device__ __forceinline__ void make_query(Query<D, NT>& Q, const RawQuery<D, NT>& given, const AttendArgs& A, int lane) {
   const int t = lane & 3;
   const uint4(&raw)[NT][D / 32] = given.x;
-  uint32_t top = 0;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int nt = 0; nt < NT; ++nt) {
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       const uint4 x = raw[nt][i];
       top = max_bf16x2(top, max_bf16x2(max_bf16x2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), max_bf16x2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
     }
-  // (of numbers that are not negative, the larger one has the larger bits)
-  const int top_exp = static_cast<int>(__reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16)) >> 7);
-  // 2^e with the unit's largest element times 2^-e in [2^14, 2^15); below 2^-90 it counts as that, from 2^101 on it has no scores
-  const int e = min(max(top_exp - 127, -90), 100) - 14;
-  const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -104 <= e <= 86
-  Q.scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + 24 + e) << 23);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int top_exp = static_cast<int>(max(top & 0xffffu, top >> 16) >> 7);      // (of numbers that are not negative, the larger one has the larger bits)
+    // 2^e with the row's largest element times 2^-e in [2^14, 2^15); below 2^-90 it counts as that, from 2^101 on it has no scores
+    const int e = min(max(top_exp - 127, -90), 100) - 14;
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // -104 <= e <= 86
+    const float scale = A.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 + 24 + e) << 23);
     float sum = 0.f;
-    bool large = false;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       float f[8];
@@ -192,21 +191,14 @@ __device__ __forceinline__ void make_query(Query<D, NT>& Q, const RawQuery<D, NT
       Q.b[nt][2 * i + 1][0] = pack_f16x2(f[2], f[6]);
       Q.b[nt][2 * i + 1][1] = pack_f16x2(f[3] * 0.0625f, f[7] * 0.0625f);
     }
-    if (top_exp > 127 + 100) {      // rows with such an element have no scores, the unit's other rows have theirs
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        float f[8];
-        bf16x8_to_f32(raw[nt][i], f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) large |= !(fabsf(f[j]) < 2.535301200456459e30f);   // 2^101
-      }
-      if (large) sum = NAN;
-    }
+    if (top_exp > 127 + 100) sum = NAN;      // (an infinity or a NaN among them)
     sum *= 5.9604644775390625e-8f;      // 2^-24
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     Q.sum[nt][0] = __shfl_sync(0xffffffffu, sum, t * 8);
     Q.sum[nt][1] = __shfl_sync(0xffffffffu, sum, t * 8 + 4);
+    Q.scale[nt][0] = __shfl_sync(0xffffffffu, scale, t * 8);
+    Q.scale[nt][1] = __shfl_sync(0xffffffffu, scale, t * 8 + 4);
   }
 }
 
@@ -303,12 +295,12 @@ __device__ __forceinline__ float step_of(uint32_t params) {
 }
 
 // What the parameters of a tile's rows say, each worked out by one lane: lane l has the rows 4 l .. 4 l + 3 of 128, K's and then
-// V's.  (s, lo) times the scale for K, (s, lo + 8 s) for V; those of V rows that are not there may be whatever was there before
+// V's.  (s, lo) for K, (s, lo + 8 s) for V; those of V rows that are not there may be whatever was there before
 // and count as 0.
 struct RowValues {
   float2 v[4];
 };
-__device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, float scale, uint32_t on, int left, bool masked, int lane) {
+__device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, uint32_t on, int left, bool masked, int lane) {
   const uint4 raw = lds128(params + lane * 16);
   const uint32_t p[4] = {raw.x, raw.y, raw.z, raw.w};
   const bool is_v = lane >= 16;
@@ -317,11 +309,10 @@ __device__ __forceinline__ float rows_of(RowValues& r, uint32_t params, float sc
   for (int i = 0; i < 4; ++i) {
     float s = step_of(p[i]);
     const float lo = __uint_as_float(p[i] << 16);
-    const float f = is_v ? 1.f : scale;
-    float m = is_v ? fmaf(8.f, s, lo) : lo * f;
+    float m = is_v ? fmaf(8.f, s, lo) : lo;
     if (masked && is_v && (!(on >> (lane >> 2 & 3) & 1u) || (lane & 15) * 4 + i >= left)) s = m = 0.f;
     top = fmaxf(top, s);
-    r.v[i] = make_float2(s * f, m);
+    r.v[i] = make_float2(s, m);
   }
   return is_v ? top : 0.f;
 }
@@ -347,10 +338,15 @@ __device__ __forceinline__ void weigh_tile(Rows<D, NT>& R, const float (&scores)
         else if constexpr (REP == 2) c[b][nt][x] = first ? scores[2 + b][nt][x] : scores[b][nt][x];
         else c[b][nt][x] = t & 2 ? (t & 1 ? scores[3][nt][x] : scores[2][nt][x]) : (t & 1 ? scores[1][nt][x] : scores[0][nt][x]);
       }
-      c[b][nt][0] = fmaf(k.x, c[b][nt][0], fmaf(k.y, Q.sum[nt][0], -R.ref[nt][0]));
-      c[b][nt][1] = fmaf(k.x, c[b][nt][1], fmaf(k.y, Q.sum[nt][1], -R.ref[nt][1]));
-      c[b][nt][2] = fmaf(k.z, c[b][nt][2], fmaf(k.w, Q.sum[nt][0], -R.ref[nt][0]));
-      c[b][nt][3] = fmaf(k.z, c[b][nt][3], fmaf(k.w, Q.sum[nt][1], -R.ref[nt][1]));
+      // (s C + lo sum) stays below 2^127, whatever the row of K: |C| <= 15 * 2^15 * 128 * 2^-24
+      const float2 sum = make_float2(Q.sum[nt][0], Q.sum[nt][1]), scale = make_float2(Q.scale[nt][0], Q.scale[nt][1]),
+                   less = make_float2(-R.ref[nt][0], -R.ref[nt][1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 step = i ? make_float2(k.z, k.z) : make_float2(k.x, k.x), lo = i ? make_float2(k.w, k.w) : make_float2(k.y, k.y);
+        const float2 x = fma2(fma2(step, make_float2(c[b][nt][2 * i], c[b][nt][2 * i + 1]), mul2(lo, sum)), scale, less);
+        c[b][nt][2 * i] = x.x, c[b][nt][2 * i + 1] = x.y;
+      }
     }
   }
   if (masked) {
@@ -910,7 +906,7 @@ __global__ void __launch_bounds__(kWarpsOf<NT> * 32, 1) quant_attend_kernel(cons
         __syncwarp();
         {
           RowValues rows;
-          top = rows_of(rows, params + (tile & 1) * R_::kParams, Q.scale, on, left, masked, lane);
+          top = rows_of(rows, params + (tile & 1) * R_::kParams, on, left, masked, lane);
           sts_f4(scratch + lane * 32, rows.v[0], rows.v[1]);
           sts_f4(scratch + lane * 32 + 16, rows.v[2], rows.v[3]);
         }
