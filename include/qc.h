@@ -484,7 +484,8 @@ int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes
  * A query that sees no key gets 0 and lse minus infinity.  Rows of out that belong to no listed sequence are left as
  * they are, and so are those of a sequence whose row or query numbers are out of range (QC_ERR_INVALID_ARG in the status
  * word).  A page id that is not in the pool is not followed: its keys count as absent (QC_ERR_BAD_PAGE).  A length
- * beyond the table's room is cut to it (QC_ERR_PLAN).  A batch that is too much for one call (over 2^32 rows of K, counted
+ * beyond the table's room is cut to it (QC_ERR_PLAN).  Lengths that another stream changes while a call runs make that call's
+ * rows wrong, and no later call's: a captured call is right again in its next replay.  A batch that is too much for one call (over 2^32 rows of K, counted
  * once per KV head and per 2, 4, 8 or 16 query rows, or a sequence with more than 2^28 of them) is not computed at all
  * (QC_ERR_PLAN): out stays as it was.
  * Query elements are kept to 2^-35 of the largest element of their row (token, head; a stream's); a row with an element of 2^101
