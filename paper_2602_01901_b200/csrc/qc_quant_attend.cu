@@ -51,7 +51,7 @@ constexpr int kUnitCost = 4;         // what a unit costs each warp besides its 
 template <int ROWS>
 constexpr uint32_t kFewTiles = ROWS == 2 ? 3 : 12;
 constexpr uint32_t kWholeTiles = 3;  // a unit of so many tiles per warp of a team is not cut (one sequence of 707 tokens, 32 heads: 9.6 us, cut 22.8)
-constexpr uint32_t kLeastStep = (127u - 101u) << 23;   // 2^-101, below every step but 0
+constexpr uint32_t kLeastStep = (127u - 104u) << 23;   // 2^-104, below every step but 0: a range is 15 steps, and 2^-100 at least
 
 struct StreamArgs {
   const uint16_t* q;
