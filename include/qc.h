@@ -469,7 +469,8 @@ typedef struct qc_quant_attend_args {
   const int32_t* starts_dev;     /* [n_seqs + 1] query tokens of each sequence, as qc_table_extend numbers them; null: one each */
   qc_quant_stream text;
   qc_quant_stream visual;        /* all null: one stream */
-  void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim] */
+  void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim]; over a q_dev only with each row at the place of its query
+                                    (anything else that overlaps: QC_ERR_INVALID_ARG), over no other argument */
   float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
   void* workspace_dev;           /* qc_quant_workspace_bytes; need not be cleared; one call at a time */
   size_t workspace_bytes;

@@ -1082,6 +1082,18 @@ int32_t check_stream(const qc_quant_stream* s, const qc_quant_attend_args* a, St
   return QC_OK;
 }
 
+// Whether the output lies over rows of queries that other blocks may still read.  At the very place of its query each row may be: a
+// unit's rows are written by the team that finishes it, when all of its teams have read them, and no other unit reads them.
+bool over_queries(const qc_quant_stream* s, const qc_quant_attend_args* a) {
+  const uint64_t row = static_cast<uint64_t>(a->n_q_heads) * a->head_dim * 2, stride = static_cast<uint64_t>(s->q_stride) * 2;
+  const uint64_t q = reinterpret_cast<uintptr_t>(s->q_dev), out = reinterpret_cast<uintptr_t>(a->out_dev), end = out + row * a->n_tokens;
+  if (a->n_tokens < 1 || (q == out && (stride == row || a->n_tokens == 1))) return false;
+  if (q >= end) return false;
+  if (q + row > out || stride == 0) return q + row > out;
+  const uint64_t token = (out - row - q) / stride + 1;      // the first whose row ends behind the output's beginning
+  return token < static_cast<uint64_t>(a->n_tokens) && q + token * stride < end;
+}
+
 int32_t check_sizes(const qc_quant_attend_args* a) {
   if (!a) return QC_ERR_INVALID_ARG;
   if (a->head_dim != 64 && a->head_dim != 128) return QC_ERR_UNSUPPORTED;
@@ -1174,6 +1186,7 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   A.has_visual = v.q_dev || v.k_pool_dev || v.v_pool_dev || v.pages_dev || v.lens_dev;
   if (A.has_visual)
     if (const int32_t bad = check_stream(&v, args, A.stream[1])) return bad;
+  if (over_queries(&args->text, args) || (A.has_visual && over_queries(&v, args))) return QC_ERR_INVALID_ARG;
   if (args->workspace_bytes < workspace_bytes(args) || !args->workspace_dev) return QC_ERR_INVALID_ARG;
   if (args->n_tokens == 0) return QC_OK;
   A.ids = args->seq_ids_dev, A.starts = args->starts_dev;

@@ -132,5 +132,6 @@ def attend(text: Stream, n_kv_heads: int, page_size: int, *, visual: Optional[St
     Sequence i is row ``seq_ids[i]`` (None: i) of the tables and has query tokens ``starts[i]`` to ``starts[i + 1] - 1`` (None:
     token i), ``max_queries`` at most.  ``causal``: they are the last tokens of the text stream, and none sees what is behind
     it.  Returns (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); a query that sees nothing gets 0
-    and minus infinity; tokens of no sequence stay what they were in ``out`` (where it is made here, anything).  ``status``: an int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
+    and minus infinity; tokens of no sequence stay what they were in ``out`` (where it is made here, anything).
+    ``out`` may be a stream's ``q`` itself (dense); it may not overlap one in another way, nor any other argument.  ``status``: an int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
     return _native().attend(text, n_kv_heads, page_size, visual, seq_ids, starts, max_queries, causal, scale, out, status)
