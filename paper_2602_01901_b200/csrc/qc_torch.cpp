@@ -197,6 +197,10 @@ PyObject* py_extend(PyObject*, PyObject* const* a, Py_ssize_t n) {   // packed, 
     const int32_t most = a[6] == Py_None ? b.n : int32_of(a[6], "max_slots");
     if (most < 0) throw BadArgument("max_slots is negative");
     const at::Tensor& lens = tensor_of(a[7], "lens");
+    if (b.n == 0) {      // (the library lists one at least; no sequence, no token)
+      const auto options = at::TensorOptions().dtype(at::kInt).device(lens.device());
+      return pair(at::zeros({1}, options), at::full({most}, -1, options));
+    }
     const at::Tensor starts = empty({b.n + 1}, at::kInt, lens), slots = empty({most}, at::kInt, lens);
     check(qc_table_extend(b.index, stream_of(b.index), b.table, b.n, b.ids, b.count, most, starts.data_ptr<int32_t>(), most ? slots.data_ptr<int32_t>() : nullptr),
           "qc_table_extend");
@@ -208,6 +212,7 @@ PyObject* py_trim(PyObject*, PyObject* const* a, Py_ssize_t n) {   // packed, in
   return guarded([&]() -> PyObject* {
     need_args(n, 6);
     const Batch b = batch_of(a, "n_keep");
+    if (b.n == 0) Py_RETURN_NONE;
     check(qc_table_trim(b.index, stream_of(b.index), b.table, b.n, b.ids, b.count), "qc_table_trim");
     Py_RETURN_NONE;
   });
@@ -335,7 +340,7 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
     args.softmax_scale = static_cast<float>(scale);
     const at::Tensor out = out_of(a[9], q.sizes(), q, "out", index, false), lse = empty({q.size(0), q.size(1)}, at::kFloat, q);
-    if (q.size(0)) {
+    if (q.size(0) && seqs) {
       check(qc_quant_workspace_bytes(&args, &args.workspace_bytes), "qc_quant_attend");
       const at::Tensor workspace = empty({static_cast<int64_t>(args.workspace_bytes)}, at::kByte, q);   // the call's own, back to the allocator behind it
       args.out_dev = out.data_ptr(), args.lse_out_dev = lse.data_ptr<float>(), args.workspace_dev = workspace.data_ptr();

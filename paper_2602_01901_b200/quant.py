@@ -79,7 +79,8 @@ def table_extend(table: PageTable, n_new: Optional[torch.Tensor] = None, *, seq_
                  n_seqs: Optional[int] = None, max_slots: Optional[int] = None):
     """``n_new[i]`` (None: 1) more tokens for row ``seq_ids[i]`` (None: i).  Returns (starts [n + 1], slots [max_slots]):
     sequence i's new tokens are ``starts[i]`` to ``starts[i + 1] - 1`` of the call, token t goes to ``slots[t]``, and slots
-    behind the last token are -1.  ``max_slots`` may be left out where every sequence takes one token."""
+    behind the last token are -1.  ``max_slots`` may be left out where every sequence takes one token.  A list without sequences
+    changes nothing, here and below."""
     return _native().extend(*table.packed, n_new, seq_ids, n_seqs, max_slots, table.lens)
 
 
