@@ -370,8 +370,20 @@ PyMethodDef g_methods[] = {
     {"error_class", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_error_class)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
+#ifndef QC_BUILT_FOR
+#define QC_BUILT_FOR "an unknown torch"
+#endif
+const char g_built_for[] = "_qc_torch for " QC_BUILT_FOR ";";      // (build.py looks for it in the file)
+
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_qc_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__qc_torch() { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__qc_torch() {
+  PyObject* m = PyModule_Create(&g_module);
+  if (m && PyModule_AddStringConstant(m, "built_for", g_built_for) < 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}

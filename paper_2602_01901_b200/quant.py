@@ -22,6 +22,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding as qc
+from .build import built_for
 
 _calls = None
 
@@ -35,6 +36,9 @@ def _native():
             from . import _qc_torch
         except ImportError as e:
             raise RuntimeError(f"{e}: build it with `python -m paper_2602_01901_b200.build` (there is no CPU or PyTorch fallback)") from e
+        made_for = getattr(_qc_torch, "built_for", "_qc_torch of an earlier build;")
+        if made_for != f"_qc_torch for {built_for()};":
+            raise RuntimeError(f"{made_for} this is {built_for()}: build it again with `python -m paper_2602_01901_b200.build`")
         _qc_torch.error_class(qc.QcError)
         _calls = _qc_torch
     return _calls
