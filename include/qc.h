@@ -375,7 +375,8 @@ int32_t qc_attend_static(int32_t device, void* cuda_stream, const void* q_dev, c
  *
  * Device data that does not fit (an id out of range, too few pages) is met on the device: nothing outside the
  * given memory is touched, and a QC_ERR_* code is left in a status word that the caller may read when it likes
- * (the largest code stays; it is never cleared by the calls). */
+ * (the largest code stays; it is never cleared by the calls).  What a call writes overlaps nothing else that it is given, but
+ * where it says so. */
 #define QC_TABLE_MAX_BATCH 4096   /* sequences listed in one call */
 #define QC_TABLE_MAX_SEQS 65536   /* rows of a page table */
 #define QC_QUANT_MAX_HEADS 1024
@@ -399,7 +400,8 @@ typedef struct qc_table {
 int32_t qc_table_reset(int32_t device, void* cuda_stream, const qc_table* table);
 
 /* n_new_dev[i] (null: 1) more tokens for row seq_ids_dev[i] (null: i) of the table, i < n_seqs.  Pages are
- * taken in the order of the list, then of the tokens.
+ * taken in the order of the list, then of the tokens.  The counts may be the table's lengths, here and in qc_table_trim: they
+ * are read before any of it is written.
  *   starts_dev [n_seqs + 1]  the new tokens are numbered through the list: sequence i's are starts[i] .. starts[i + 1] - 1
  *   slots_dev  [max_slots]   where token t goes: page id * page_size + place in the page; -1 behind the last token
  * All or nothing: on an id out of range or a negative count (QC_ERR_INVALID_ARG), an id listed twice or lengths

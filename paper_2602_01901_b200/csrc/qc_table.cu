@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(1024) table_kernel(const TableArgs T) {
     const Seq s = seqs[i];
     if (TRIM) {
       if (s.start != s.len) T.lens[s.id] = s.start;
-    } else {
-      T.lens[s.id] = s.len + (T.count ? T.count[i] : 1);
+    } else {      // (the counts may lie in the table: they are not read again)
+      T.lens[s.id] = s.len + ((i + 1 < n_seqs ? seqs[i + 1].start : n_tokens) - s.start);
       T.starts[i] = s.start;
     }
   }
