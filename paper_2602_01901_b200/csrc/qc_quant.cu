@@ -356,7 +356,7 @@ extern "C" int32_t qc_quant_append(int32_t device, void* cuda_stream, const qc_q
   const dim3 grid = grid_of(a, k_dev && v_dev);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = launch_pdl(shape->head_dim == 128 ? quant_append_kernel<128> : quant_append_kernel<64>, grid, dim3(kRowWarps * 32), 0, stream, a);
-  return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  return status_of(e);
 }
 
 extern "C" int32_t qc_quant_read(int32_t device, void* cuda_stream, const qc_quant_shape* shape, int32_t n_tokens, const int32_t* slots_dev,
@@ -379,5 +379,5 @@ extern "C" int32_t qc_quant_read(int32_t device, void* cuda_stream, const qc_qua
   const dim3 grid = grid_of(a, k_out_dev && v_out_dev);
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = launch_pdl(shape->head_dim == 128 ? quant_read_kernel<128> : quant_read_kernel<64>, grid, dim3(kRowWarps * 32), 0, stream, a);
-  return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  return status_of(e);
 }

@@ -1209,5 +1209,5 @@ extern "C" int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_q
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int rows = unit_rows(args);
   const cudaError_t e = args->head_dim == 128 ? launch_rows<128>(A, rows, device, stream) : launch_rows<64>(A, rows, device, stream);
-  return e == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  return status_of(e);
 }

@@ -249,7 +249,8 @@ int32_t launch_table(const TableArgs& a, bool many, void* cuda_stream) {
   // 48 KB are there for a call's lists and the kernel's own variables (528 bytes) together; a longer list asks for more, well before
   // that.  (Always the most, so that two calls at once cannot take it from one another.)
   constexpr int kMost = kTableMaxBatch * static_cast<int>(sizeof(Seq)) + kTableMaxSeqs / 8;
-  if (smem > 32 * 1024 && cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess) return QC_ERR_CUDA;
+  if (smem > 32 * 1024)
+    if (const int32_t bad = status_of(cudaFuncSetAttribute(table_kernel<TRIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost))) return bad;
   const int32_t work = a.max_slots > a.n_seqs ? a.max_slots : a.n_seqs;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(many ? kCluster : 1);
@@ -263,7 +264,7 @@ int32_t launch_table(const TableArgs& a, bool many, void* cuda_stream) {
   attr[1].val.clusterDim.x = kCluster, attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = many ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, table_kernel<TRIM>, a) == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  return status_of(cudaLaunchKernelEx(&cfg, table_kernel<TRIM>, a));
 }
 
 }  // namespace
@@ -279,8 +280,9 @@ extern "C" int32_t qc_table_reset(int32_t device, void* cuda_stream, const qc_ta
   const int64_t entries = static_cast<int64_t>(a.max_seqs) * a.max_pages;
   const int64_t most = entries > a.n_pages ? entries : a.n_pages;
   const int blocks = static_cast<int>(most / 256 + 1 < 1184 ? most / 256 + 1 : 1184);
-  table_reset_kernel<<<blocks, 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? QC_OK : QC_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};      // (its own status: the last error may be another call's)
+  cfg.gridDim = dim3(blocks), cfg.blockDim = dim3(256), cfg.stream = static_cast<cudaStream_t>(cuda_stream);
+  return status_of(cudaLaunchKernelEx(&cfg, table_reset_kernel, a));
 }
 
 extern "C" int32_t qc_table_extend(int32_t device, void* cuda_stream, const qc_table* table, int32_t n_seqs, const int32_t* seq_ids_dev,
