@@ -98,3 +98,21 @@ def test_thousands_of_replays_in_a_workspace_of_their_own():
         wrong += (out != want).sum() + (lse != want_lse).sum()
         out.fill_(7)
     assert int(wrong) == 0
+
+
+@pytest.mark.parametrize("lens,kv_heads,group,head_dim", SHAPES, ids=[f"{len(s[0])}x{s[1]}x{s[2]}" for s in SHAPES])
+def test_lengths_that_change_between_replays(lens, kv_heads, group, head_dim):
+    """Plans of every kind after one another in one workspace: the bits of a call that is not captured."""
+    stream = cache(lens, kv_heads, group, head_dim, 32, 7)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = quant.attend(stream, kv_heads, 32)
+    g = gen(9)
+    for turn in range(60):
+        top = [1.0, 0.02, 0.3][turn % 3]
+        now = (torch.tensor(lens) * top * torch.rand(len(lens), generator=g)).to(torch.int32)
+        stream.lens.copy_(now.to(DEV))
+        want, want_lse = quant.attend(stream, kv_heads, 32)
+        out.fill_(7), lse.fill_(7)
+        graph.replay()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), turn
