@@ -24,12 +24,13 @@
 // With four query rows or fewer the eight columns hold them twice, with two or one four times.  Every lane then has the
 // scores of all four blocks of a tile for the same rows, and weighs one half or one quarter of them: each set of columns sums up
 // its own blocks, and the sets are put together like the sums of different warps.  (One row, eight sequences of 8 541
-// tokens, 32 heads: 67.0 us with eight columns of which one counts, 64.5 so; 16 sequences of 60 to 5 000: 32.6 and 29.7.)
+// tokens, 32 heads: 68.3 us with eight columns of which one counts, 65.9 so; 16 sequences of 60 to 5 000: 33.4 and 31.4.)
 //
-// What bounds it: the bytes, 68 per row of 128 elements, would take 45 us of those 64.5.  A tile of 64 keys is some 950
-// instructions of a warp, 68 of them products; masks and shifts run at half the rate of other instructions and the products at an
-// eighth, which together is about as long as the tile's bytes take.  Small batches are bound by a
-// block's start: the plan, page ids, first tiles, sums and the join follow one another, 9.6 us for one sequence.
+// What bounds it: the bytes, 68 per row of 128 elements, would take 45 us of 65.7 (those eight sequences now).  A tile of 64 keys is some
+// 950 instructions of a warp, 68 of them products; masks and shifts run at half the rate of other instructions and the products at an
+// eighth.  No pipe is full (issue slots 49 %, ALU 50 %, tensor 27 %): the three warps of a scheduler mostly wait for their own dependent
+// instructions.  Small batches are bound by a block's start: the plan, page ids, first tiles, sums and the join follow one
+// another, 9.6 us for one sequence.
 
 #include "../../include/qc.h"
 #include "qc_device.cuh"
@@ -43,8 +44,8 @@ namespace qc {
 namespace {
 
 constexpr int kTile = 64;            // keys that a warp takes at a time
-constexpr int kUnitCost = 4;         // what a unit costs each warp besides its tiles, in tiles (its first tiles' way, the sums; 1: 33.8 us instead of
-                                     // 29.7 for 16 sequences of 60 to 5 000 tokens, 32 heads; 70.4 instead of 65.0 for three of 90 000)
+constexpr int kUnitCost = 4;         // what a unit costs each warp besides its tiles, in tiles (its first tiles' way, the sums; 1: 35.2 us instead of
+                                     // 31.4 for 16 sequences of 60 to 5 000 tokens, 32 heads; 71.9 instead of 66.0 for three of 90 000)
 // Tiles per warp below which units are shared out among warps.  More rows make more of a unit's pieces: 24 ragged sequences with
 // five queries, 8 heads of 4, 64 wide, take 32.3 us with 3 and 26.2 with 6 or 12, 16 sequences of 4 000 tokens with five
 // queries, 4 heads of 4, 41.2 with 6 and 35.6 with 12, 16 ragged ones of one row 32.5 with 6 and 30.7 with 3.
@@ -719,7 +720,7 @@ struct Work {
   uint32_t per, longer, more, per_tile, team;   // cost of a range, ranges that cost one more, cost of a unit besides its tiles, and of a tile
 };
 
-// One block per SM, of twelve warps (168 registers a thread; eight with 255 have too little on their way: 69.9 us instead of 64.5
+// One block per SM, of twelve warps (168 registers a thread; eight with 255 have too little on their way: 71.1 us instead of 65.9
 // for eight sequences of 8 541 tokens, 32 heads).  With sixteen rows to a unit eight warps, or its sums would not stay in registers.
 template <int NT>
 constexpr int kWarpsOf = NT == 1 ? 12 : 8;
@@ -1106,7 +1107,7 @@ int32_t check_sizes(const qc_quant_attend_args* a) {
 }
 
 // Query rows of a unit: as many columns of a product as they need.  Sixteen only where they are all taken (16 sequences of 8 000
-// tokens, 4 heads of 8, 64 wide, two queries: 31.2 us against 37.3 with units of eight; with one to five queries on 4 heads of
+// tokens, 4 heads of 8, 64 wide, two queries: 34.3 us against 36.3 with units of eight; with one to five queries on 4 heads of
 // 4, 128 wide, 30 against 26).
 int unit_rows(const qc_quant_attend_args* a) {
   const int64_t rows = static_cast<int64_t>(a->max_queries) * (a->n_q_heads / a->n_kv_heads);
