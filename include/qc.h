@@ -495,6 +495,65 @@ int32_t qc_quant_workspace_bytes(const qc_quant_attend_args* args, size_t* bytes
  * or more in size, infinite or no number gets NaN, and no other row is different for it. */
 int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend_args* args);
 
+/* ---- Positions, and a cache in bf16 pages ------------------------------------------------------
+ *
+ * The paper has no counterpart to these calls.  Everything above takes rotated queries and keys; qc_rotate makes them
+ * (per-head norm and rotation by positions of one or several axes), and qc_paged_append does the same on a key's way into a
+ * cache.  The cache is bf16 pages behind the page tables above (qc_table_*): a pool holds one tensor (K or V) of one layer and
+ * stream as bf16 [n_pages][n_kv_heads][page_size][head_dim], and a token is at its slot, page id * page_size + place.  As above
+ * each call is complete in itself, asynchronous on `cuda_stream`, may be captured and replayed, and reads what changes from
+ * step to step on the device. */
+#define QC_ROTATE_MAX_AXES 4
+#define QC_PAGED_MAX_HEADS 1024
+#define QC_PAGED_MAX_TOKENS (1 << 24)   /* tokens of one qc_rotate or qc_paged_append */
+
+/* A row x of one token and head becomes y = x / sqrt(mean x^2 + eps) * w where its norm weights are given, and then each pair i of
+ * its first rotary_dim elements is turned by the angle positions[axes[i]][token] * freqs[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where `adjacent`.
+ * In fp32 throughout, rounded once; an angle is exact to 2^-30 turns for every position.  Squares are summed in fp32: elements are
+ * below 2^60 in size.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
+ * Rows are bf16 [n_tokens][heads][head_dim], heads dense, tokens `stride` elements apart (multiples of 8, pointers 16-byte
+ * aligned).  An output lies over its own input (same pointer and stride) or over nothing. */
+typedef struct qc_rotate_args {
+  int32_t n_tokens, n_q_heads, n_kv_heads;
+  int32_t head_dim;              /* 64 or 128 */
+  int32_t rotary_dim;            /* elements that turn: a multiple of 16, at most head_dim; 0: none */
+  int32_t adjacent;              /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2 i, 2 i + 1) */
+  int32_t n_axes;                /* 1..QC_ROTATE_MAX_AXES */
+  int32_t norm_f32;              /* norm weights are fp32 (1) or bf16 (0) */
+  const float* freqs_dev;        /* [rotary_dim / 2] radians per position */
+  const int32_t* axes_dev;       /* [rotary_dim / 2] the axis of each pair; null: 0 */
+  const int32_t* positions_dev;  /* [n_axes][n_tokens], axes position_stride elements apart */
+  int64_t position_stride;
+  const void* q_norm_dev;        /* [head_dim] weights; null: no norm */
+  const void* k_norm_dev;
+  float eps;                     /* of both norms */
+  const void* q_dev;             /* either of q and k may be null */
+  int64_t q_stride;
+  void* q_out_dev;
+  int64_t q_out_stride;
+  const void* k_dev;
+  int64_t k_stride;
+  void* k_out_dev;               /* qc_paged_append: null, K goes to its pool */
+  int64_t k_out_stride;
+} qc_rotate_args;
+
+int32_t qc_rotate(int32_t device, void* cuda_stream, const qc_rotate_args* args);
+
+typedef struct qc_paged_append_args {
+  qc_rotate_args rows;           /* q optional; k null where the layer stores none */
+  const void* v_dev;             /* bf16 [n_tokens][n_kv_heads][head_dim], stored as it is; null: none */
+  int64_t v_stride;
+  const int32_t* slots_dev;      /* [n_tokens] */
+  int32_t page_size, n_pages;    /* 16, 32 or 64; n_pages * page_size < 2^31 */
+  void* k_pool_dev;
+  void* v_pool_dev;
+} qc_paged_append_args;
+
+/* The same, K and V stored at their slots.  A slot that is negative or not in the pool is left out (its query is still made).
+ * Slots are distinct; of rows with the same slot, what that row holds afterwards is not specified. */
+int32_t qc_paged_append(int32_t device, void* cuda_stream, const qc_paged_append_args* args);
+
 const char* qc_status_string(int32_t status);
 
 #ifdef __cplusplus

@@ -35,7 +35,7 @@ EXPORTS = (
     "qc_debug_read_qcache", "qc_debug_read_row", "qc_set_option", "qc_get_profile", "qc_status_string",
     "qc_attend_static", "qc_decode_begin", "qc_decode_layer",
     "qc_table_reset", "qc_table_extend", "qc_table_trim", "qc_quant_pool_bytes", "qc_quant_append", "qc_quant_read",
-    "qc_quant_workspace_bytes", "qc_quant_attend",
+    "qc_quant_workspace_bytes", "qc_quant_attend", "qc_rotate", "qc_paged_append",
 )
 
 
@@ -97,6 +97,24 @@ class qc_quant_attend_args(C.Structure):
     ]
 
 
+class qc_rotate_args(C.Structure):
+    _fields_ = [
+        ("n_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("rotary_dim", C.c_int32), ("adjacent", C.c_int32), ("n_axes", C.c_int32), ("norm_f32", C.c_int32),
+        ("freqs_dev", C.c_void_p), ("axes_dev", C.c_void_p), ("positions_dev", C.c_void_p), ("position_stride", C.c_int64),
+        ("q_norm_dev", C.c_void_p), ("k_norm_dev", C.c_void_p), ("eps", C.c_float), ("q_dev", C.c_void_p),
+        ("q_stride", C.c_int64), ("q_out_dev", C.c_void_p), ("q_out_stride", C.c_int64), ("k_dev", C.c_void_p),
+        ("k_stride", C.c_int64), ("k_out_dev", C.c_void_p), ("k_out_stride", C.c_int64),
+    ]
+
+
+class qc_paged_append_args(C.Structure):
+    _fields_ = [
+        ("rows", qc_rotate_args), ("v_dev", C.c_void_p), ("v_stride", C.c_int64), ("slots_dev", C.c_void_p),
+        ("page_size", C.c_int32), ("n_pages", C.c_int32), ("k_pool_dev", C.c_void_p), ("v_pool_dev", C.c_void_p),
+    ]
+
+
 class QcError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -148,6 +166,8 @@ def load() -> C.CDLL:
         "qc_quant_read": [i32, vp, C.POINTER(qc_quant_shape), i32, vp, vp, vp, vp, vp],
         "qc_quant_workspace_bytes": [C.POINTER(qc_quant_attend_args), C.POINTER(C.c_size_t)],
         "qc_quant_attend": [i32, vp, C.POINTER(qc_quant_attend_args)],
+        "qc_rotate": [i32, vp, C.POINTER(qc_rotate_args)],
+        "qc_paged_append": [i32, vp, C.POINTER(qc_paged_append_args)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -377,3 +397,18 @@ def qc_quant_workspace_bytes(args: qc_quant_attend_args) -> int:
 
 def qc_quant_attend(device: int, cuda_stream: int, args: qc_quant_attend_args) -> None:
     _check(load().qc_quant_attend(device, cuda_stream, args), "qc_quant_attend")
+
+
+# ---- positions, and a cache in bf16 pages -----------------------------------------------------------------------
+
+QC_ROTATE_MAX_AXES = 4
+QC_PAGED_MAX_HEADS = 1024
+QC_PAGED_MAX_TOKENS = 1 << 24
+
+
+def qc_rotate(device: int, cuda_stream: int, args: qc_rotate_args) -> None:
+    _check(load().qc_rotate(device, cuda_stream, args), "qc_rotate")
+
+
+def qc_paged_append(device: int, cuda_stream: int, args: qc_paged_append_args) -> None:
+    _check(load().qc_paged_append(device, cuda_stream, args), "qc_paged_append")

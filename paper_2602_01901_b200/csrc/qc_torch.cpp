@@ -1,4 +1,4 @@
-// The calls on a 4-bit cache taken straight from torch tensors (module _qc_torch, used by quant.py).
+// The calls on a 4-bit cache, on positions and on bf16 pages taken straight from torch tensors (module _qc_torch, used by quant.py and paged.py).
 //
 // What a call checks and packs is some forty tensor attributes.  An attention call, its allocations and its launch took the host
 // 28 us from Python through ctypes, more than the kernel runs for a small batch; from here they take 8.  The calls keep nothing, enqueue on the current stream of the tensors' device, and raise ValueError for
@@ -350,6 +350,148 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- rows turned by their positions, bf16 pages ---------------------------------------------------------------------
+
+// Rotation (freqs, axes, adjacent) and positions into `r`.
+void rotation_of(qc_rotate_args& r, PyObject* rotation, PyObject* positions, int32_t index) {
+  if (rotation == Py_None) {
+    if (positions != Py_None) throw BadArgument("positions without a rotation");
+    return;
+  }
+  if (!PyTuple_Check(rotation) || PyTuple_GET_SIZE(rotation) != 3) throw BadArgument("rotation has to be a Rotation");
+  PyObject* const f = PyTuple_GET_ITEM(rotation, 0);
+  const at::Tensor& freqs = tensor_of(f, "rotation.freqs");
+  if (freqs.scalar_type() != at::kFloat || !on(freqs, index) || !freqs.is_contiguous())
+    throw BadArgument("rotation.freqs has to be a dense float32 tensor on " + cuda_name(index));
+  if (freqs.numel() < 1) throw BadArgument("rotation.freqs is empty");
+  r.rotary_dim = size32(2 * freqs.numel(), "rotation.freqs");
+  r.freqs_dev = freqs.data_ptr<float>();
+  r.axes_dev = ints(PyTuple_GET_ITEM(rotation, 1), "rotation.axes", index, freqs.numel());
+  const int adjacent = PyObject_IsTrue(PyTuple_GET_ITEM(rotation, 2));
+  if (adjacent < 0) throw PythonError{};
+  r.adjacent = adjacent;
+  const at::Tensor& p = tensor_of(positions, "positions");
+  const int64_t n = p.dim() ? p.size(p.dim() - 1) : -1;
+  if (p.scalar_type() != at::kInt || !on(p, index) || p.dim() < 1 || p.dim() > 2 || n != r.n_tokens || (n > 1 && p.stride(p.dim() - 1) != 1))
+    throw BadArgument("positions has to be an int32 tensor [tokens] or [axes, tokens] on " + cuda_name(index) + ", an axis's tokens dense");
+  r.n_axes = p.dim() == 2 ? size32(p.size(0), "positions") : 1;
+  r.position_stride = p.dim() == 2 && r.n_axes > 1 ? p.stride(0) : 0;
+  r.positions_dev = static_cast<const int32_t*>(p.data_ptr());
+}
+
+// Norm weights [head_dim], both of the same type.
+void norms_of(qc_rotate_args& r, PyObject* q_norm, PyObject* k_norm, PyObject* eps, int32_t index) {
+  int seen = 0;
+  for (int i = 0; i < 2; ++i) {
+    PyObject* const o = i ? k_norm : q_norm;
+    const char* const name = i ? "k_norm" : "q_norm";
+    if (o == Py_None) continue;
+    const at::Tensor& w = tensor_of(o, name);
+    const bool f32 = w.scalar_type() == at::kFloat;
+    if ((!f32 && w.scalar_type() != at::kBFloat16) || !on(w, index) || !w.is_contiguous() || w.numel() != r.head_dim)
+      throw BadArgument(std::string(name) + " has to be a dense bfloat16 or float32 tensor [head_dim] on " + cuda_name(index));
+    if (seen && f32 != (r.norm_f32 != 0)) throw BadArgument("q_norm and k_norm have to have the same type");
+    r.norm_f32 = f32, seen = 1;
+    (i ? r.k_norm_dev : r.q_norm_dev) = w.data_ptr();
+  }
+  const double e = PyFloat_AsDouble(eps);
+  if (e == -1.0 && PyErr_Occurred()) throw PythonError{};
+  r.eps = static_cast<float>(e);
+}
+
+// Rows in and out: `out` is made where it is None.
+at::Tensor turned_rows(const at::Tensor& x, PyObject* out, const char* name, const char* out_name, int32_t index, int64_t& stride, int64_t& out_stride) {
+  stride = rows_of(x, name, index);
+  if (out == Py_None) {
+    const at::Tensor made = empty(x.sizes(), at::kBFloat16, x);
+    out_stride = x.size(1) * x.size(2);
+    return made;
+  }
+  const at::Tensor& t = tensor_of(out, out_name);
+  out_stride = rows_of(t, out_name, index);
+  if (t.sizes() != x.sizes()) throw BadArgument(std::string(out_name) + " has to have the shape of " + name);
+  return t;
+}
+
+// q, k, positions, rotation, q_norm, k_norm, eps, q_out, k_out
+PyObject* py_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 9);
+    const bool has_q = a[0] != Py_None, has_k = a[1] != Py_None;
+    if (!has_q && !has_k) throw BadArgument("one of q and k at least");
+    if ((!has_q && a[7] != Py_None) || (!has_k && a[8] != Py_None)) throw BadArgument("an output without its rows");
+    const at::Tensor& rows = tensor_of(has_q ? a[0] : a[1], has_q ? "q" : "k");
+    const int32_t index = device_of(rows, has_q ? "q" : "k");
+    if (rows.dim() != 3) throw BadArgument("q and k have to be [tokens, heads, head_dim]");
+    qc_rotate_args r{};
+    r.n_tokens = size32(rows.size(0), "tokens"), r.head_dim = size32(rows.size(2), "head_dim");
+    at::Tensor q, k;
+    if (has_q) q = turned_rows(rows, a[7], "q", "q_out", index, r.q_stride, r.q_out_stride), r.n_q_heads = size32(rows.size(1), "heads"), r.q_dev = rows.data_ptr(), r.q_out_dev = q.data_ptr();
+    if (has_k) {
+      const at::Tensor& t = tensor_of(a[1], "k");
+      k = turned_rows(t, a[8], "k", "k_out", index, r.k_stride, r.k_out_stride);
+      if (t.size(0) != rows.size(0) || t.size(2) != rows.size(2)) throw BadArgument("q and k have to have the same tokens and head_dim");
+      r.n_kv_heads = size32(t.size(1), "heads"), r.k_dev = t.data_ptr(), r.k_out_dev = k.data_ptr();
+    }
+    rotation_of(r, a[3], a[2], index);
+    norms_of(r, a[4], a[5], a[6], index);
+    if (rows.size(0)) check(qc_rotate(index, stream_of(index), &r), "qc_rotate");
+    if (has_q && has_k) return pair(q, k);
+    PyObject* one = THPVariable_Wrap(has_q ? q : k);
+    if (!one) throw PythonError{};
+    return has_q ? Py_BuildValue("NO", one, Py_None) : Py_BuildValue("ON", Py_None, one);
+  });
+}
+
+// A pool of bf16 pages [n_pages, heads, page, head_dim].
+void* bf16_pool_of(const at::Tensor& t, const char* name, int32_t index) {
+  if (t.scalar_type() != at::kBFloat16 || !on(t, index) || !t.is_contiguous() || t.dim() != 4)
+    throw BadArgument(std::string(name) + " has to be a dense bfloat16 tensor [pages, heads, page size, head_dim] on " + cuda_name(index));
+  return t.data_ptr();
+}
+
+// k_pool, v_pool, slots, k, v, q, positions, rotation, q_norm, k_norm, eps, q_out
+PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 12);
+    const bool has_k = a[3] != Py_None, has_v = a[4] != Py_None, has_q = a[5] != Py_None;
+    if ((!has_k && !has_v) || has_k != (a[0] != Py_None) || has_v != (a[1] != Py_None)) throw BadArgument("a pool for every tensor, and one of k and v at least");
+    if (!has_q && a[11] != Py_None) throw BadArgument("an output without its rows");
+    const at::Tensor& rows = tensor_of(has_k ? a[3] : a[4], has_k ? "k" : "v");
+    const int32_t index = device_of(rows, has_k ? "k" : "v");
+    if (rows.dim() != 3) throw BadArgument("k and v have to be [tokens, heads, head_dim]");
+    qc_paged_append_args p{};
+    qc_rotate_args& r = p.rows;
+    r.n_tokens = size32(rows.size(0), "tokens"), r.n_kv_heads = size32(rows.size(1), "heads"), r.head_dim = size32(rows.size(2), "head_dim");
+    const at::Tensor& pool = tensor_of(has_k ? a[0] : a[1], has_k ? "k_pool" : "v_pool");
+    if (has_k) r.k_stride = rows_of(rows, "k", index), r.k_dev = rows.data_ptr(), p.k_pool_dev = bf16_pool_of(pool, "k_pool", index);
+    if (has_v) {
+      const at::Tensor& t = tensor_of(a[4], "v");
+      const at::Tensor& v_pool = tensor_of(a[1], "v_pool");
+      p.v_stride = rows_of(t, "v", index), p.v_dev = t.data_ptr(), p.v_pool_dev = bf16_pool_of(v_pool, "v_pool", index);
+      if (t.sizes() != rows.sizes() || v_pool.sizes() != pool.sizes()) throw BadArgument("k and v, and their pools, have to have the same shape");
+    }
+    if (pool.size(1) != rows.size(1) || pool.size(3) != rows.size(2)) throw BadArgument("the pools have to have the heads and the head_dim of k and v");
+    p.n_pages = size32(pool.size(0), "pages"), p.page_size = size32(pool.size(2), "page size");
+    at::Tensor q;
+    if (has_q) {
+      const at::Tensor& t = tensor_of(a[5], "q");
+      q = turned_rows(t, a[11], "q", "q_out", index, r.q_stride, r.q_out_stride);
+      if (t.size(0) != rows.size(0) || t.size(2) != rows.size(2)) throw BadArgument("q has to have the tokens and the head_dim of k and v");
+      r.n_q_heads = size32(t.size(1), "heads"), r.q_dev = t.data_ptr(), r.q_out_dev = q.data_ptr();
+    }
+    tensor_of(a[2], "slots");
+    p.slots_dev = ints(a[2], "slots", index, rows.size(0));
+    rotation_of(r, a[7], a[6], index);
+    norms_of(r, a[8], a[9], a[10], index);
+    if (rows.size(0)) check(qc_paged_append(index, stream_of(index), &p), "qc_paged_append");
+    if (!has_q) Py_RETURN_NONE;
+    PyObject* out = THPVariable_Wrap(q);
+    if (!out) throw PythonError{};
+    return out;
+  });
+}
+
 PyObject* py_error_class(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     need_args(n, 1);
@@ -367,6 +509,8 @@ PyMethodDef g_methods[] = {
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_append)), METH_FASTCALL, nullptr},
     {"read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_read)), METH_FASTCALL, nullptr},
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_attend)), METH_FASTCALL, nullptr},
+    {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_rotate)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_paged_append)), METH_FASTCALL, nullptr},
     {"error_class", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_error_class)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
