@@ -498,14 +498,17 @@ int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend
 /* ---- Positions, and a cache in bf16 pages ------------------------------------------------------
  *
  * The paper has no counterpart to these calls.  Everything above takes rotated queries and keys; qc_rotate makes them
- * (per-head norm and rotation by positions of one or several axes), and qc_paged_append does the same on a key's way into a
- * cache.  The cache is bf16 pages behind the page tables above (qc_table_*): a pool holds one tensor (K or V) of one layer and
+ * (per-head norm and rotation by positions of one or several axes), qc_paged_append does the same on a key's way into a
+ * cache, and qc_paged_attend attends over that cache where sequences share a prefix (many questions about one image).
+ * The cache is bf16 pages behind the page tables above (qc_table_*): a pool holds one tensor (K or V) of one layer and
  * stream as bf16 [n_pages][n_kv_heads][page_size][head_dim], and a token is at its slot, page id * page_size + place.  As above
  * each call is complete in itself, asynchronous on `cuda_stream`, may be captured and replayed, and reads what changes from
  * step to step on the device. */
 #define QC_ROTATE_MAX_AXES 4
 #define QC_PAGED_MAX_HEADS 1024
-#define QC_PAGED_MAX_TOKENS (1 << 24)   /* tokens of one qc_rotate or qc_paged_append */
+#define QC_PAGED_MAX_SEQS 2048     /* sequences in one qc_paged_attend */
+#define QC_PAGED_MAX_QUERIES 128   /* query tokens of one sequence in one qc_paged_attend */
+#define QC_PAGED_MAX_TOKENS (1 << 24)   /* tokens of one qc_rotate, qc_paged_append or qc_paged_attend */
 
 /* A row x of one token and head becomes y = x / sqrt(mean x^2 + eps) * w where its norm weights are given, and then each pair i of
  * its first rotary_dim elements is turned by the angle positions[axes[i]][token] * freqs[i]:
@@ -553,6 +556,54 @@ typedef struct qc_paged_append_args {
 /* The same, K and V stored at their slots.  A slot that is negative or not in the pool is left out (its query is still made).
  * Slots are distinct; of rows with the same slot, what that row holds afterwards is not specified. */
 int32_t qc_paged_append(int32_t device, void* cuda_stream, const qc_paged_append_args* args);
+
+/* One stream as qc_paged_attend reads it. */
+typedef struct qc_paged_stream {
+  const void* q_dev;             /* bf16 [n_tokens][n_q_heads][head_dim], tokens q_stride elements apart (0: one row for all) */
+  int64_t q_stride;
+  const void* k_pool_dev;
+  const void* v_pool_dev;
+  const int32_t* pages_dev;      /* [rows][max_pages] of the stream's table */
+  const int32_t* lens_dev;       /* [rows] */
+  int32_t max_pages, n_pages, rows;
+} qc_paged_stream;
+
+typedef struct qc_paged_attend_args {
+  int32_t n_q_heads, n_kv_heads, head_dim, page_size;
+  int32_t n_seqs;                /* sequences of the call */
+  int32_t n_tokens;              /* query tokens: rows of q and out */
+  int32_t max_queries;           /* most query tokens of one sequence, 1..QC_PAGED_MAX_QUERIES */
+  int32_t causal;                /* 1: the queries' own tokens are the last of the own stream, and a query sees none behind its own */
+  float softmax_scale;           /* 0 => 1/sqrt(head_dim) */
+  int32_t n_groups;              /* 0 without a shared stream */
+  const int32_t* seq_ids_dev;    /* [n_seqs] row of the own table of each sequence; null: i */
+  const int32_t* starts_dev;     /* [n_seqs + 1] query tokens of each sequence, as qc_table_extend numbers them; null: one each */
+  const int32_t* groups_dev;     /* [n_groups + 1] sequences groups[g] .. groups[g + 1] - 1 of the call share a prefix; null: one
+                                    group of all sequences */
+  const int32_t* shared_ids_dev; /* [n_groups] its row of the shared table; null: g */
+  qc_paged_stream own;
+  qc_paged_stream shared;        /* all null: no sequence has a prefix */
+  void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim], over no other argument */
+  float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
+  void* workspace_dev;           /* qc_paged_workspace_bytes, 16-byte aligned; need not be cleared; one call at a time */
+  size_t workspace_bytes;
+  int32_t* status_dev;           /* optional status word */
+} qc_paged_attend_args;
+
+int32_t qc_paged_workspace_bytes(const qc_paged_attend_args* args, size_t* bytes);
+
+/* Attention of each sequence's query tokens over its prefix, if it is in a group, and its own cached tokens: one softmax over the
+ * prefix's keys scored by shared.q_dev and its own keys scored by own.q_dev (an ordinary layer: the same queries twice; a
+ * lazy layer whose prefix is the image: the Q Cache on the leader's visual K).  A prefix is read once for all query rows of its
+ * group (once per 128 of a KV head's), whose sequences are adjacent in the list; sequences before the first group and behind the last have none.
+ * All tokens of a prefix are seen by every query.  A query that sees no key gets 0 and lse minus infinity, and so does one whose
+ * scores are all minus infinity.  What the pools hold where no token is counts for nothing, whatever it is.
+ * All or nothing: rows out of range, starts or groups that do not ascend or reach outside, more queries than max_queries
+ * (QC_ERR_INVALID_ARG in the status word) and batches with over 2^24 tiles of 64 keys, counted once per KV head and 128 query rows
+ * (QC_ERR_PLAN), leave out as it was.  A page id that is not in the pool is not followed: its keys count as absent
+ * (QC_ERR_BAD_PAGE).  A length beyond the table's room is cut to it (QC_ERR_PLAN).  Rows of out that belong to no sequence are
+ * left as they are. */
+int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_paged_attend_args* args);
 
 const char* qc_status_string(int32_t status);
 

@@ -36,6 +36,7 @@ EXPORTS = (
     "qc_attend_static", "qc_decode_begin", "qc_decode_layer",
     "qc_table_reset", "qc_table_extend", "qc_table_trim", "qc_quant_pool_bytes", "qc_quant_append", "qc_quant_read",
     "qc_quant_workspace_bytes", "qc_quant_attend", "qc_rotate", "qc_paged_append",
+    "qc_paged_workspace_bytes", "qc_paged_attend",
 )
 
 
@@ -115,6 +116,25 @@ class qc_paged_append_args(C.Structure):
     ]
 
 
+class qc_paged_stream(C.Structure):
+    _fields_ = [
+        ("q_dev", C.c_void_p), ("q_stride", C.c_int64), ("k_pool_dev", C.c_void_p), ("v_pool_dev", C.c_void_p),
+        ("pages_dev", C.c_void_p), ("lens_dev", C.c_void_p), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
+        ("rows", C.c_int32),
+    ]
+
+
+class qc_paged_attend_args(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+        ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_queries", C.c_int32), ("causal", C.c_int32),
+        ("softmax_scale", C.c_float), ("n_groups", C.c_int32), ("seq_ids_dev", C.c_void_p), ("starts_dev", C.c_void_p),
+        ("groups_dev", C.c_void_p), ("shared_ids_dev", C.c_void_p), ("own", qc_paged_stream), ("shared", qc_paged_stream),
+        ("out_dev", C.c_void_p), ("lse_out_dev", C.c_void_p), ("workspace_dev", C.c_void_p),
+        ("workspace_bytes", C.c_size_t), ("status_dev", C.c_void_p),
+    ]
+
+
 class QcError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -168,6 +188,8 @@ def load() -> C.CDLL:
         "qc_quant_attend": [i32, vp, C.POINTER(qc_quant_attend_args)],
         "qc_rotate": [i32, vp, C.POINTER(qc_rotate_args)],
         "qc_paged_append": [i32, vp, C.POINTER(qc_paged_append_args)],
+        "qc_paged_workspace_bytes": [C.POINTER(qc_paged_attend_args), C.POINTER(C.c_size_t)],
+        "qc_paged_attend": [i32, vp, C.POINTER(qc_paged_attend_args)],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -403,6 +425,8 @@ def qc_quant_attend(device: int, cuda_stream: int, args: qc_quant_attend_args) -
 
 QC_ROTATE_MAX_AXES = 4
 QC_PAGED_MAX_HEADS = 1024
+QC_PAGED_MAX_SEQS = 2048
+QC_PAGED_MAX_QUERIES = 128
 QC_PAGED_MAX_TOKENS = 1 << 24
 
 
@@ -412,3 +436,13 @@ def qc_rotate(device: int, cuda_stream: int, args: qc_rotate_args) -> None:
 
 def qc_paged_append(device: int, cuda_stream: int, args: qc_paged_append_args) -> None:
     _check(load().qc_paged_append(device, cuda_stream, args), "qc_paged_append")
+
+
+def qc_paged_workspace_bytes(args: qc_paged_attend_args) -> int:
+    n = C.c_size_t()
+    _check(load().qc_paged_workspace_bytes(args, C.byref(n)), "qc_paged_workspace_bytes")
+    return n.value
+
+
+def qc_paged_attend(device: int, cuda_stream: int, args: qc_paged_attend_args) -> None:
+    _check(load().qc_paged_attend(device, cuda_stream, args), "qc_paged_attend")

@@ -492,6 +492,74 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+qc_paged_stream paged_stream(PyObject* o, const char* name, at::IntArrayRef sizes, const at::Tensor* like, int32_t index) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 5) throw BadArgument(std::string(name) + " has to be a Stream");
+  const std::string at = name;
+  const at::Tensor& q = tensor_of(PyTuple_GET_ITEM(o, 0), (at + ".q").c_str());
+  const at::Tensor& k = tensor_of(PyTuple_GET_ITEM(o, 1), (at + ".k_pool").c_str());
+  const at::Tensor& v = tensor_of(PyTuple_GET_ITEM(o, 2), (at + ".v_pool").c_str());
+  const at::Tensor& pages = tensor_of(PyTuple_GET_ITEM(o, 3), (at + ".pages").c_str());
+  tensor_of(PyTuple_GET_ITEM(o, 4), (at + ".lens").c_str());
+  qc_paged_stream s{};
+  s.q_stride = rows_of(q, (at + ".q").c_str(), index);
+  if (q.sizes() != sizes) throw BadArgument(at + ".q has to have the shape of the own stream's");
+  if (pages.dim() != 2) throw BadArgument(at + ".pages has to be [rows, pages]");
+  s.q_dev = q.data_ptr();
+  s.k_pool_dev = bf16_pool_of(k, (at + ".k_pool").c_str(), index), s.v_pool_dev = bf16_pool_of(v, (at + ".v_pool").c_str(), index);
+  if (k.sizes() != v.sizes()) throw BadArgument(at + ": the pools have to have the same shape");
+  if (k.size(3) != sizes[2] || (like && (k.size(1) != like->size(1) || k.size(2) != like->size(2))))
+    throw BadArgument(at + ": the pools have to have the head_dim of q, and the heads and the page size of the own stream's");
+  s.pages_dev = ints(PyTuple_GET_ITEM(o, 3), (at + ".pages").c_str(), index);
+  s.lens_dev = ints(PyTuple_GET_ITEM(o, 4), (at + ".lens").c_str(), index, pages.size(0));
+  s.max_pages = size32(pages.size(1), "pages"), s.n_pages = size32(k.size(0), "pages"), s.rows = size32(pages.size(0), "pages");
+  return s;
+}
+
+// own, shared, groups, shared_ids, seq_ids, starts, max_queries, causal, scale, out, status
+PyObject* py_paged_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need_args(n, 11);
+    if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 5) throw BadArgument("own has to be a Stream");
+    const at::Tensor& q = tensor_of(PyTuple_GET_ITEM(a[0], 0), "own.q");
+    const int32_t index = device_of(q, "own.q");
+    if (q.dim() != 3) throw BadArgument("own.q has to be [tokens, heads, head_dim]");
+    qc_paged_attend_args args{};
+    args.own = paged_stream(a[0], "own", q.sizes(), nullptr, index);
+    const at::Tensor& pool = THPVariable_Unpack(PyTuple_GET_ITEM(a[0], 1));
+    args.n_q_heads = size32(q.size(1), "heads"), args.head_dim = size32(q.size(2), "head_dim"), args.n_tokens = size32(q.size(0), "tokens");
+    args.n_kv_heads = size32(pool.size(1), "heads"), args.page_size = size32(pool.size(2), "page size"), args.max_queries = int32_of(a[6], "max_queries");
+    int64_t seqs = q.size(0);
+    if (a[4] != Py_None) seqs = tensor_of(a[4], "seq_ids").numel();
+    else if (a[5] != Py_None) seqs = tensor_of(a[5], "starts").numel() - 1;
+    args.n_seqs = size32(seqs, "seq_ids");
+    args.seq_ids_dev = ints(a[4], "seq_ids", index, seqs), args.starts_dev = ints(a[5], "starts", index, seqs + 1), args.status_dev = ints(a[10], "status", index, 1);
+    if (a[1] != Py_None) {
+      args.shared = paged_stream(a[1], "shared", q.sizes(), &pool, index);
+      int64_t groups = 1;
+      if (a[2] != Py_None) groups = tensor_of(a[2], "groups").numel() - 1;
+      if (groups < 0) throw BadArgument("groups has one entry more than there are groups");
+      args.n_groups = size32(groups, "groups");
+      args.groups_dev = ints(a[2], "groups", index), args.shared_ids_dev = ints(a[3], "shared_ids", index, groups);
+    } else if (a[2] != Py_None || a[3] != Py_None) {
+      throw BadArgument("groups without a shared stream");
+    }
+    const int causal = PyObject_IsTrue(a[7]);
+    if (causal < 0) throw PythonError{};
+    args.causal = causal;
+    const double scale = PyFloat_AsDouble(a[8]);
+    if (scale == -1.0 && PyErr_Occurred()) throw PythonError{};
+    args.softmax_scale = static_cast<float>(scale);
+    const at::Tensor out = out_of(a[9], q.sizes(), q, "out", index, false), lse = empty({q.size(0), q.size(1)}, at::kFloat, q);
+    if (q.size(0) && seqs) {
+      check(qc_paged_workspace_bytes(&args, &args.workspace_bytes), "qc_paged_attend");
+      const at::Tensor workspace = empty({static_cast<int64_t>(args.workspace_bytes)}, at::kByte, q);   // the call's own, back to the allocator behind it
+      args.out_dev = out.data_ptr(), args.lse_out_dev = lse.data_ptr<float>(), args.workspace_dev = workspace.data_ptr();
+      check(qc_paged_attend(index, stream_of(index), &args), "qc_paged_attend");
+    }
+    return pair(out, lse);
+  });
+}
+
 PyObject* py_error_class(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     need_args(n, 1);
@@ -511,6 +579,7 @@ PyMethodDef g_methods[] = {
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_attend)), METH_FASTCALL, nullptr},
     {"rotate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_rotate)), METH_FASTCALL, nullptr},
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_paged_append)), METH_FASTCALL, nullptr},
+    {"paged_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_paged_attend)), METH_FASTCALL, nullptr},
     {"error_class", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_error_class)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -11,6 +11,8 @@ are ``quant``'s: their slots do for both kinds of cache.  No gradient flows thro
     k_pool, v_pool = (empty_pool(n_kv_heads, head_dim, page_size, n_pages) for _ in "kv")      # of each layer
     starts, slots = table_extend(table, n_new, seq_ids=ids, max_slots=n_tokens)                # once a step
     q = append(k_pool, v_pool, slots, k, v, q=q, positions=positions, rotation=rotation)       # each layer
+    out, lse = attend(Stream(q, k_pool, v_pool, table.pages, table.lens), seq_ids=ids, starts=starts, max_queries=most,
+                      shared=Stream(q, k_image, v_image, images.pages, images.lens), groups=groups, shared_ids=image_ids)
 """
 
 from __future__ import annotations
@@ -55,3 +57,18 @@ def append(k_pool: Optional[torch.Tensor], v_pool: Optional[torch.Tensor], slots
     pair of pool and rows may be None (a lazy layer that stores no K).  Returns ``q``'s rows as ``rotate`` makes them, of all tokens
     (None without ``q``)."""
     return _native().paged_append(k_pool, v_pool, slots, k, v, q, positions, rotation, q_norm, k_norm, eps, q_out)
+
+
+def attend(own: Stream, *, shared: Optional[Stream] = None, groups: Optional[torch.Tensor] = None, shared_ids: Optional[torch.Tensor] = None,
+           seq_ids: Optional[torch.Tensor] = None, starts: Optional[torch.Tensor] = None, max_queries: int = 1, causal: bool = True,
+           scale: float = 0.0, out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Attention of each sequence's query tokens over the prefix that its group shares and its own cached rows, the queries' own among
+    them (``qc_paged_attend``): one softmax over the prefix's keys, scored by ``shared.q``, and its own, scored by ``own.q``.  Sequence i
+    is row ``seq_ids[i]`` (None: i) of the own table and has query tokens ``starts[i]`` to ``starts[i + 1] - 1`` (None: token i),
+    ``max_queries`` at most.  Sequences ``groups[g]`` to ``groups[g + 1] - 1`` share row ``shared_ids[g]`` (None: g) of the shared
+    stream's table (``groups`` None: all share one); sequences before and behind the groups have no prefix.  A prefix is read
+    once for its group.  ``causal``: the queries are the last tokens of their own stream, and none sees what is behind it.  Returns
+    (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); a query that sees nothing gets 0 and minus infinity; tokens
+    of no sequence stay what they were in ``out`` (where it is made here, anything).  ``out`` overlaps no other argument.  ``status``: an
+    int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
+    return _native().paged_attend(own, shared, groups, shared_ids, seq_ids, starts, max_queries, causal, scale, out, status)

@@ -123,3 +123,53 @@ def test_host_tensors_are_refused():
                  lambda: paged.rotate(None, x, slots, None, q_out=x), lambda: paged.rotate([1], x, slots, None)):
         with pytest.raises(ValueError):
             call()
+
+
+# ---- attention ----------------------------------------------------------------------------------------------
+
+STREAM = dict(q_dev=BIG, q_stride=512, k_pool_dev=64, v_pool_dev=64, pages_dev=64, lens_dev=64, max_pages=4, n_pages=9, rows=3)
+
+
+def attend_args(own=None, shared=None, **change):
+    a = qc.qc_paged_attend_args(n_q_heads=4, n_kv_heads=2, head_dim=128, page_size=16, n_seqs=2, n_tokens=2, max_queries=1, causal=1, out_dev=2 * BIG, workspace_dev=256,
+                                workspace_bytes=1 << 40, own=qc.qc_paged_stream(**{**STREAM, **(own or {})}))
+    if shared is not None:
+        a.shared, a.n_groups = qc.qc_paged_stream(**{**STREAM, **shared}), 1
+    for name, value in change.items():
+        setattr(a, name, value)
+    return a
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(head_dim=80), 2), (dict(page_size=48), 2), (dict(n_q_heads=5), 1), (dict(n_q_heads=0), 1), (dict(n_kv_heads=0), 1), (dict(n_seqs=0), 1), (dict(n_seqs=4, n_tokens=4), 1),
+    (dict(n_tokens=-1), 1), (dict(n_tokens=1), 1), (dict(n_tokens=qc.QC_PAGED_MAX_TOKENS + 1), 2), (dict(max_queries=0), 1), (dict(max_queries=qc.QC_PAGED_MAX_QUERIES + 1), 2),
+    (dict(n_seqs=qc.QC_PAGED_MAX_SEQS + 1, seq_ids_dev=64), 2), (dict(n_q_heads=2 * qc.QC_PAGED_MAX_HEADS), 2), (dict(own=dict(q_dev=0)), 1), (dict(out_dev=0), 1), (dict(out_dev=2 * BIG + 8), 1),
+    (dict(lse_out_dev=66), 1), (dict(status_dev=65), 1), (dict(seq_ids_dev=66), 1), (dict(starts_dev=66), 1), (dict(softmax_scale=-1.0), 1), (dict(softmax_scale=math.nan), 1),
+    (dict(softmax_scale=math.inf), 1), (dict(workspace_dev=264), 1), (dict(workspace_dev=0), 1), (dict(workspace_bytes=8), 1), (dict(out_dev=BIG), 1), (dict(out_dev=BIG + 2032), 1), (dict(out_dev=BIG - 1024), 1),
+    (dict(own=dict(q_dev=BIG + 8)), 1), (dict(own=dict(q_stride=-8)), 1), (dict(own=dict(q_stride=12)), 1), (dict(own=dict(k_pool_dev=0)), 1), (dict(own=dict(v_pool_dev=24)), 1),
+    (dict(own=dict(pages_dev=0)), 1), (dict(own=dict(lens_dev=62)), 1), (dict(own=dict(max_pages=0)), 1), (dict(own=dict(n_pages=0)), 1), (dict(own=dict(rows=0)), 1),
+    (dict(own=dict(max_pages=1 << 27)), 2), (dict(own=dict(n_pages=1 << 27)), 2), (dict(own=dict(n_pages=1 << 26)), 2),
+    (dict(n_groups=1), 1), (dict(groups_dev=64), 1), (dict(shared_ids_dev=64), 1), (dict(shared=dict(q_dev=0)), 1), (dict(shared=dict(rows=0)), 1), (dict(shared={}, n_groups=2), 1),
+    (dict(shared={}, n_groups=-1), 1), (dict(shared={}, n_groups=4, groups_dev=64), 1), (dict(shared={}, n_groups=qc.QC_PAGED_MAX_SEQS + 1, groups_dev=64, shared_ids_dev=64), 2),
+    (dict(shared=dict(q_dev=2 * BIG + 1024)), 1), (dict(shared=dict(n_pages=1 << 28)), 2), (dict(shared={}, groups_dev=66), 1), (dict(shared={}, shared_ids_dev=66), 1),
+])
+def test_attention_refuses_what_it_can_see_on_the_host(change, status):
+    assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, attend_args(**change))) == status
+
+
+def test_attention_refuses_a_workspace_that_is_too_small(lib):
+    a = attend_args(shared={})
+    need = qc.qc_paged_workspace_bytes(a)
+    for size, status in ((need - 1, qc.QC_ERR_INVALID_ARG), (need, qc.QC_ERR_CUDA)):
+        a.workspace_bytes = size
+        assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, a)) == status
+    n = C.c_size_t()
+    assert lib.qc_paged_attend(0, None, None) == lib.qc_paged_workspace_bytes(None, C.byref(n)) == lib.qc_paged_workspace_bytes(C.byref(a), None) == qc.QC_ERR_INVALID_ARG
+
+
+def test_host_tensors_of_streams_are_refused():
+    x, ids, pool = torch.zeros(2, 1, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), torch.zeros(1, 1, 16, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="CUDA"):
+        paged.attend(paged.Stream(x, pool, pool, ids[None], ids))
+    with pytest.raises(ValueError, match="Stream"):
+        paged.attend((x, pool))
