@@ -1,13 +1,40 @@
 // Attention of a step's queries over bf16 pages, where adjacent sequences of a batch share a prefix.
 //
 //   out = softmax(scale [q_shared K_prefix ; q_own K_own]) [V_prefix ; V_own]
+//
+// A prefix's keys are scored by all query rows of its group at once (its tokens times the query heads of a KV head), a sequence's
+// own by its own rows: both are units of at most 128 rows over a run of keys, and one kernel takes them all, on the tensor
+// cores.  What a unit finds of a row is (largest score, sum, weighted values); a second kernel puts a row's parts together.
+//
+// The batch is one row of units, prefixes first, whose costs (tiles of 64 keys, and a constant for a unit) are laid end to
+// end and cut into equal ranges, one per block, two blocks an SM.  A unit inside one range leaves its rows at their queries' places; one that a border
+// cuts leaves a piece per block.  Every number of this plan comes from the lists and lengths on the device.
+//
+// Per tile: S[128 x 64] = Q K^T and O[128 x D] += P V by tcgen05.mma, Q, K and V in shared memory (K and V by tensor-map copies of
+// pages), S, P and O in tensor memory.  Four warps hold a row per thread, one issues products, one fetches.
+// Units of few rows hold them two or four times (rows r and r + 64, or r + 32 and so on): every copy weighs another half or quarter of
+// a tile's keys, so that all four warps take part in the exponentials; the copies are added up when the unit ends.
 
 #include "../../include/qc.h"
-#include "qc_device.cuh"
 #include "qc_quant.h"
+#include "qc_umma.cuh"
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
 
 namespace qc {
 namespace {
+
+constexpr int kRows = 128;       // query rows of a unit
+constexpr int kKeys = 64;        // keys of a tile
+constexpr int kBlock = kRows + 64;
+constexpr int kUnits = 4;        // units that are known to the block at a time
+constexpr int kMeta = 8;         // tiles whose places are
+constexpr uint32_t kScoresAt = 0, kOutAt = 128, kColumns = 256;   // tensor memory: two score buffers of 64 columns, D of the sums
+constexpr float kRescale = 8.f;  // the reference of a row moves when its scores have grown by 2^8
+constexpr uint32_t kUnitCost = 2, kTileCost = 1;
+constexpr uint32_t kMostCost = 1u << 27;
 
 struct StreamArgs {
   const uint16_t* q;
@@ -19,7 +46,22 @@ struct StreamArgs {
   int32_t max_pages, n_pages, rows;
 };
 
+// What the second kernel knows of a prefix or a sequence.
+struct Record {
+  uint32_t base;           // where its costs begin
+  int32_t tiles, token0, queries;
+  int32_t group;           // a sequence's prefix, or -1
+  int32_t spare[3];
+};
+
+struct Plan {
+  int32_t fine;
+  uint32_t cost, workers;
+  int32_t spare;
+};
+
 struct AttendArgs {
+  CUtensorMap map[2][2];  // K and V of own and shared pages, as rows of 64 elements, a page's tokens of a head at a time
   StreamArgs stream[2];   // own, shared
   const int32_t* ids;
   const int32_t* starts;
@@ -27,7 +69,11 @@ struct AttendArgs {
   const int32_t* shared_ids;
   uint16_t* out;
   float* lse;
-  int32_t* plan;          // [1] whether the batch is computed
+  Plan* plan;
+  Record* records;        // [groups + sequences]
+  float* rows;            // [kinds][tokens * heads][D] sums of whole units
+  float2* row_ml;         // [kinds][tokens * heads]
+  float* pieces;          // [workers][2][128 * (D + 2)]
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, n_groups, n_tokens, max_queries, causal;
@@ -38,51 +84,130 @@ __device__ __forceinline__ void report(const AttendArgs& A, int code) {
   if (A.status) atomicMax(A.status, code);
 }
 
-__device__ __forceinline__ int length_of(const AttendArgs& A, const StreamArgs& S, int row) {
+__device__ __forceinline__ int length_of(const AttendArgs& A, const StreamArgs& S, int row, bool tell) {
   const int64_t len = __ldg(S.lens + row), room = static_cast<int64_t>(S.max_pages) << A.page_shift;
   if (len >= 0 && len <= room) return static_cast<int>(len);
-  report(A, QC_ERR_PLAN);
+  if (tell) report(A, QC_ERR_PLAN);
   return len < 0 ? 0 : static_cast<int>(room);
 }
 
-struct Seq {
-  int32_t token0, queries, row;
+// A prefix (items 0 .. n_groups - 1) or a sequence's own tokens.
+struct Item {
+  int32_t token0, queries, row, len, tiles;
+  uint32_t units, per_head;      // units; those of a KV head
+  bool fine;
 };
-__device__ __forceinline__ bool seq_of(const AttendArgs& A, int i, Seq& s) {
-  int64_t a = i, b = i + 1;
-  if (A.starts) a = __ldg(A.starts + i), b = __ldg(A.starts + i + 1);
-  s.token0 = static_cast<int32_t>(a), s.queries = static_cast<int32_t>(b - a), s.row = A.ids ? __ldg(A.ids + i) : i;
-  return a >= 0 && b >= a && b <= A.n_tokens && b - a <= A.max_queries && s.row >= 0 && s.row < A.stream[0].rows;
+__device__ __forceinline__ Item item_of(const AttendArgs& A, int i, bool tell) {
+  Item u{};
+  const bool shared = i < A.n_groups;
+  int64_t a, b;
+  if (shared) {
+    a = A.groups ? __ldg(A.groups + i) : 0, b = A.groups ? __ldg(A.groups + i + 1) : A.n_seqs;
+    u.row = A.shared_ids ? __ldg(A.shared_ids + i) : i;
+    u.fine = a >= 0 && b >= a && b <= A.n_seqs;
+    if (u.fine && A.starts) a = __ldg(A.starts + a), b = __ldg(A.starts + b);
+  } else {
+    const int seq = i - A.n_groups;
+    a = seq, b = seq + 1;
+    if (A.starts) a = __ldg(A.starts + seq), b = __ldg(A.starts + seq + 1);
+    u.row = A.ids ? __ldg(A.ids + seq) : seq;
+    u.fine = b - a <= A.max_queries;
+  }
+  const StreamArgs& S = A.stream[shared];
+  u.fine = u.fine && a >= 0 && b >= a && b <= A.n_tokens && u.row >= 0 && u.row < S.rows;
+  if (!u.fine) return u;
+  u.token0 = static_cast<int32_t>(a), u.queries = static_cast<int32_t>(b - a);
+  if (u.queries == 0) return u;
+  u.len = length_of(A, S, u.row, tell);
+  u.tiles = (u.len + kKeys - 1) / kKeys;
+  u.per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
+  u.units = u.tiles ? min(static_cast<uint64_t>(u.per_head) * A.hkv, static_cast<uint64_t>(kMostCost)) : 0;
+  return u;
+}
+__device__ __forceinline__ uint32_t unit_cost(int tiles) { return kUnitCost + tiles * kTileCost; }
+// kMostCost + 1: too much
+__device__ __forceinline__ uint32_t cost_of(const Item& u) {
+  return static_cast<uint32_t>(min(static_cast<uint64_t>(u.units) * unit_cost(u.tiles), static_cast<uint64_t>(kMostCost) + 1));
 }
 
-struct Group {
-  int32_t first, last, row;
-};
-__device__ __forceinline__ bool group_of(const AttendArgs& A, int g, Group& u) {
-  u.first = A.groups ? __ldg(A.groups + g) : 0, u.last = A.groups ? __ldg(A.groups + g + 1) : A.n_seqs;
-  u.row = A.shared_ids ? __ldg(A.shared_ids + g) : g;
-  return u.first >= 0 && u.last >= u.first && u.last <= A.n_seqs && u.row >= 0 && u.row < A.stream[1].rows;
+// Ranges: worker w has the costs [range_begin(w), range_begin(w + 1)); every range is as long as a tile at least.
+__device__ __forceinline__ uint32_t range_begin(uint32_t cost, uint32_t workers, uint32_t w) { return static_cast<uint32_t>(static_cast<uint64_t>(cost) * w / workers); }
+__device__ __forceinline__ uint32_t worker_at(uint32_t cost, uint32_t workers, uint32_t at) {
+  return static_cast<uint32_t>(((static_cast<uint64_t>(at) + 1) * workers - 1) / cost);
 }
 
-__global__ void __launch_bounds__(256) paged_plan_kernel(const __grid_constant__ AttendArgs A) {
-  pdl_wait();
-  bool fine = true;
-  Seq s;
-  Group u;
-  for (int i = threadIdx.x; i < A.n_seqs; i += 256) fine &= seq_of(A, i, s);
-  for (int i = threadIdx.x; i < A.n_groups; i += 256) fine &= group_of(A, i, u);
-  fine = __syncthreads_and(fine);
-  if (threadIdx.x == 0) {
-    A.plan[0] = fine;
-    if (!fine) report(A, QC_ERR_INVALID_ARG);
+struct Unit {
+  int64_t row0;                  // its first query row among the item's
+  int32_t token0, queries, n_here, kvh, shared, row, first, tiles, len;
+  int32_t all_see;               // keys that every row sees
+  int32_t place;                 // of a piece: worker * 2, + 1 where the unit begins in the range; -1: the unit is whole
+};
+
+struct Meta {
+  int32_t y[4];                  // of a tile's pages: the first row in the pool, -1: the page is not there
+  int32_t on, shared;            // blocks of 16 keys that are there
+  int32_t spare[2];
+};
+
+template <int D>
+struct Shape {
+  static constexpr int kK = D == 128 ? 3 : 4, kV = D == 128 ? 2 : 4;      // tiles under way
+  static constexpr uint32_t kTile = kKeys * D * 2, kHalf = kKeys * 128, kQ = kRows * D * 2, kQHalf = kRows * 128;
+  static constexpr uint32_t kTiles = kQ + (kK + kV) * kTile;
+};
+
+struct Control {
+  uint64_t s[2], p[2], o[2], k[4], v[4], k_free[4], v_free[4], full[kUnits], empty[kUnits], q;
+  uint64_t sums[8];
+  Unit units[kUnits];
+  Meta meta[kMeta];
+  uint32_t tmem, beat, redo[4];
+  int32_t failed;
+};
+static_assert(sizeof(Control) <= 1024, "two blocks and their tiles are all of an SM's shared memory");
+
+template <int D>
+__device__ __forceinline__ void scores(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc) {
+  if constexpr (D == 128) {
+    umma_scores<kRows * 128, kKeys * 128>(tmem_d, a, b, idesc);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred e, pz, po;\n\t.reg .b64 da, db;\n\t"
+        "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 pz, 0, 0;\n\tsetp.eq.b32 po, 0, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, pz;\n\t"
+        "add.u64 da, %1, 2;\n\tadd.u64 db, %2, 2;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
+        "add.u64 da, %1, 4;\n\tadd.u64 db, %2, 4;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
+        "add.u64 da, %1, 6;\n\tadd.u64 db, %2, 6;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t}"
+        ::"r"(tmem_d), "l"(a), "l"(b), "r"(idesc) : "memory");
   }
 }
 
-// One warp per row: a key at a time.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Whether all rows' warps say so: they go on together or not at all, so none waits at a barrier for one that has given up.
+__device__ __forceinline__ bool rows_all(bool x) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(x)), "n"(kRows) : "memory");
+  return all != 0;
+}
+__device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kRows) : "memory"); }
+
+// Keys [from, to) of a table row for one query, by one warp, a key at a time: what the tensor cores cannot give where a value that is
+// infinite or no number stands behind a weight of 0 (0 times it is no number).  Replaces those of the row's sums that are no finite
+// numbers, on the row's reference.
 template <int D>
-__device__ __forceinline__ void sweep(const AttendArgs& A, const StreamArgs& S, int row, int kvh, int64_t token, int head, int seen, float (&o)[D / 32], float& m,
-                                      float& l, int lane) {
-  float q[D / 32], k[D / 32];
+__device__ __noinline__ void sweep(const AttendArgs& A, const StreamArgs& S, int row, int kvh, int64_t token, int head, int from, int to, float* sums, const float2* ml,
+                                   uint32_t* beat, int lane) {
+  float o[D / 32] = {}, m = -INFINITY, l = 0.f, q[D / 32];
   const auto load = [&](const uint16_t* p, float (&f)[D / 32]) {
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) {
@@ -91,56 +216,693 @@ __device__ __forceinline__ void sweep(const AttendArgs& A, const StreamArgs& S, 
     }
   };
   load(S.q + token * S.q_stride + static_cast<int64_t>(head) * D, q);
-  for (int j = 0; j < seen; ++j) {
+#pragma unroll 2
+  for (int j = from; j < to; ++j) {
+    if (lane == 0 && (j & 63) == 0) atomicAdd(beat, 1u);
     const int32_t id = __ldg(S.pages + static_cast<int64_t>(row) * S.max_pages + (j >> A.page_shift));
-    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(S.n_pages)) {
-      report(A, QC_ERR_BAD_PAGE);
-      continue;
-    }
+    if (static_cast<uint32_t>(id) >= static_cast<uint32_t>(S.n_pages)) continue;
     const int64_t at = (((static_cast<int64_t>(id) * A.hkv + kvh) << A.page_shift) + (j & (A.page - 1))) * D;
+    float k[D / 32], v[D / 32];
     load(S.k_pool + at, k);
+    load(S.v_pool + at, v);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) s = fmaf(q[i], k[i], s);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
     s *= A.scale_log2;
-    const float top = fmaxf(m, s);
     if (s == -INFINITY) continue;      // (weighs nothing)
-    const float before = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(m - top), p = exp2f(s - (top == -INFINITY ? 0.f : top));   // (a score that is no number has no place in an order)
-    load(S.v_pool + at, k);
+    const float top = fmaxf(m, s), before = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : exp2f(m - top), p = exp2f(s - (top == -INFINITY ? 0.f : top));
     l = fmaf(l, before, p);
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(o[i], before, p * k[i]);
+    for (int i = 0; i < D / 32; ++i) o[i] = fmaf(o[i], before, p * v[i]);
     m = top;
   }
+  const float scale = m == -INFINITY && l == 0.f ? 0.f : exp2f(m - ml->x);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float* const to_here = sums + (i * 32 + lane) * 2 + e;
+      if (!isfinite(*to_here)) *to_here = l == 0.f ? 0.f : o[2 * i + e] * scale;
+    }
 }
 
-// Grid: (sequences, query heads).
+__device__ __forceinline__ void store_32(float* p, const uint32_t* r, float f) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(__uint_as_float(r[0]) * f), "f"(__uint_as_float(r[1]) * f),
+               "f"(__uint_as_float(r[2]) * f), "f"(__uint_as_float(r[3]) * f), "f"(__uint_as_float(r[4]) * f), "f"(__uint_as_float(r[5]) * f),
+               "f"(__uint_as_float(r[6]) * f), "f"(__uint_as_float(r[7]) * f)
+               : "memory");
+}
+
+// Warps 0-3: a query row per thread; warp 4 issues products; warp 5 finds units and fetches.  Hand-offs (mbarriers, all waits bounded):
+//   full[u], empty[u]   warp 5 -> the others: unit u % 4 is described; back: its place is free
+//   q                   rows -> warp 4: the unit's queries are in shared memory
+//   k[i], v[i]          copies -> warp 4 (and v to rows that clear what no token has): a tile has landed
+//   s[b]                tensor core -> rows: scores of tile t in buffer b = t & 1
+//   p[b]                rows -> warp 4: its weights are there, over the scores
+//   o[b]                tensor core -> warp 4, rows: its value products are done
+//   k_free[i], v_free[i]  tensor core -> warp 5: the tile's place may be written
+// No barrier runs two completions ahead of a waiter: the next completion needs something that the waiter does after it has seen
+// the one before.  Tiles are counted through all units of the block.
 template <int D>
-__global__ void __launch_bounds__(128) paged_attend_kernel(const __grid_constant__ AttendArgs A) {
-  pdl_wait();
-  if (!A.plan[0]) return;
-  const int seq = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31, kvh = head / A.group;
-  Seq s;
-  seq_of(A, seq, s);
-  int prefix = 0, shared_row = 0;
-  for (int g = 0; g < A.n_groups; ++g) {
-    Group u;
-    group_of(A, g, u);
-    if (seq >= u.first && seq < u.last) prefix = length_of(A, A.stream[1], u.row), shared_row = u.row;
+__global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_constant__ AttendArgs A) {
+  using Z = Shape<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kK * Z::kTile;
+  Control& C = *reinterpret_cast<Control*>(smem + Z::kTiles);
+  volatile int32_t& failed = C.failed;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (sQ & 1023u) {      // (there is no static shared memory, so it begins at a multiple of 1024; products never run on a misplaced tile)
+    if (threadIdx.x == 0) report(A, QC_ERR_PLAN);
+    return;
   }
-  const int len = length_of(A, A.stream[0], s.row);
-  for (int i = threadIdx.x >> 5; i < s.queries; i += 4) {
-    float o[D / 32] = {}, m = -INFINITY, l = 0.f;
-    const int64_t token = s.token0 + i;
-    if (prefix) sweep<D>(A, A.stream[1], shared_row, kvh, token, head, prefix, o, m, l, lane);
-    sweep<D>(A, A.stream[0], s.row, kvh, token, head, A.causal ? len - (s.queries - 1 - i) : len, o, m, l, lane);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const size_t row = token * A.hq + head;
+  if (warp == 5) {
+    if (lane == 0) {
+      for (int i = 0; i < 2; ++i) mbar_init(&C.s[i], 1), mbar_init(&C.p[i], kRows), mbar_init(&C.o[i], 1);
+      for (int i = 0; i < 4; ++i) mbar_init(&C.k[i], 1), mbar_init(&C.v[i], 1), mbar_init(&C.k_free[i], 1), mbar_init(&C.v_free[i], 1);
+      for (int i = 0; i < kUnits; ++i) mbar_init(&C.full[i], 1), mbar_init(&C.empty[i], kRows + 1);
+      mbar_init(&C.q, kRows);
+      fence_mbar_init();
+      C.failed = 0, C.beat = 0;
+    }
+  } else if (warp == 4) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&C.tmem)), "n"(kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+
+  // ---- the plan: costs of the items before each one, in the tiles' place until they come
+  uint32_t* const before = reinterpret_cast<uint32_t*>(smem + Z::kQ);      // [items + 1]
+  const int n_items = A.n_groups + A.n_seqs;
+  uint32_t total = 0;
+  bool fine = true;
+  for (int i0 = 0; i0 < n_items; i0 += kBlock) {
+    const int i = i0 + threadIdx.x;
+    uint32_t x = 0;
+    Item u{};
+    if (i < n_items) {
+      u = item_of(A, i, blockIdx.x == 0);
+      x = cost_of(u);
+      fine &= u.fine;
+    }
+    const uint32_t mine = x;
+    uint64_t sum = x;      // (a warp's sum may pass 32 bits)
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x) reinterpret_cast<uint32_t*>(A.out + row * D)[x * 32 + lane] = pack_bf16x2(o[2 * x] * inv, o[2 * x + 1] * inv);
-    if (A.lse && lane == 0) A.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 31) C.sums[warp] = sum;
+    __syncthreads();
+    uint64_t base = total, all = total;
+#pragma unroll
+    for (int w = 0; w < kBlock / 32; ++w) base += w < warp ? C.sums[w] : 0, all += C.sums[w];
+    total = static_cast<uint32_t>(min(all, static_cast<uint64_t>(kMostCost) + 1));
+    const uint32_t at = static_cast<uint32_t>(min(base + sum - mine, static_cast<uint64_t>(kMostCost) + 1));
+    if (i < n_items) {
+      before[i] = at;
+      if (blockIdx.x == 0) {
+        int group = -1;
+        if (i >= A.n_groups && A.n_groups) {      // the last group that begins at or before the sequence, if it reaches it
+          const int seq = i - A.n_groups;
+          if (A.groups) {
+            int lo = 0, hi = A.n_groups;
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (__ldg(A.groups + mid + 1) > seq) hi = mid;
+              else lo = mid + 1;
+            }
+            if (lo < A.n_groups && __ldg(A.groups + lo) <= seq) group = lo;
+          } else {
+            group = 0;
+          }
+        }
+        A.records[i] = Record{at, u.units ? u.tiles : 0, u.token0, u.queries, group, {}};
+      }
+    }
+    __syncthreads();
+  }
+  fine = __syncthreads_and(fine);
+  const bool few = total <= kMostCost;
+  const uint32_t workers = max(1u, min(gridDim.x, total / kTileCost));
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *A.plan = Plan{fine && few, total, workers, 0};
+    if (!fine) report(A, QC_ERR_INVALID_ARG);
+    else if (!few) report(A, QC_ERR_PLAN);
+  }
+  tc5_fence_before();
+  __syncthreads();
+  tc5_fence_after();
+  const uint32_t tmem = C.tmem;
+  const bool works = fine && few && total && blockIdx.x < workers;
+
+  if (works && warp == 5) {
+    // ------------------------------------------------------------------ units and tiles
+    uint32_t at = range_begin(total, workers, blockIdx.x);
+    const uint32_t end = range_begin(total, workers, blockIdx.x + 1);
+    int item;
+    uint32_t item_at;
+    {
+      int lo = 0, hi = n_items - 1;      // the last item that begins at or before the range
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= at) lo = mid;
+        else hi = mid - 1;
+      }
+      item = lo, item_at = before[lo];
+    }
+    __syncwarp();
+    fence_proxy_async();      // (the costs have been read before copies take their place)
+    Item u = item_of(A, item, false), u_next{};
+    if (item + 1 < n_items) u_next = item_of(A, item + 1, false);
+    // the next unit of the range
+    const auto find = [&](Unit& w) -> bool {
+      while (at < end) {
+        const uint32_t cost = cost_of(u), one = unit_cost(u.tiles);
+        if (u.units == 0 || at >= item_at + cost) {
+          if (++item >= n_items) return false;
+          item_at += cost, u = u_next;
+          if (item + 1 < n_items) u_next = item_of(A, item + 1, false);
+          if (at < item_at) at = item_at;
+          continue;
+        }
+        const uint32_t unit = (at - item_at) / one, unit_at = item_at + unit * one, tiles_at = unit_at + kUnitCost;
+        const int first = at > tiles_at ? (at - tiles_at + kTileCost - 1) / kTileCost : 0;
+        const int last = end > tiles_at ? min(static_cast<uint32_t>(u.tiles), (end - tiles_at + kTileCost - 1) / kTileCost) : 0;
+        at = unit_at + one;
+        if (first >= last) continue;
+        const int kvh = unit / u.per_head, part = unit - kvh * u.per_head;
+        w.row0 = static_cast<int64_t>(part) * kRows;
+        const int64_t rows = static_cast<int64_t>(u.queries) * A.group;
+        w.n_here = static_cast<int32_t>(min(static_cast<int64_t>(kRows), rows - w.row0));
+        w.token0 = u.token0, w.queries = u.queries, w.kvh = kvh, w.shared = item < A.n_groups, w.row = u.row, w.first = first, w.tiles = last - first, w.len = u.len;
+        w.all_see = w.shared || !A.causal ? u.len : max(0, u.len - (u.queries - 1 - static_cast<int>(w.row0 / A.group)));
+        w.place = first == 0 && last == u.tiles ? -1 : static_cast<int>(blockIdx.x) * 2 + (first == 0 ? 1 : 0);
+        return true;
+      }
+      return false;
+    };
+    Unit w{};
+    bool has = find(w), stopped = false;
+    uint32_t n_units = 0;      // described
+    bool described = false;
+    int tile = 0;              // of the unit, next to be fetched
+    uint32_t k_next = 0, v_next = 0;
+    int32_t ids = 0, next_ids = 0, batch = 0;      // page ids, one per lane, from page `batch` of the unit's row on
+    const int per_tile = kKeys >> A.page_shift;
+    const auto ask = [&](int from) -> int32_t {
+      const int page = from + lane;
+      return static_cast<int64_t>(page) << A.page_shift < w.len ? __ldg(A.stream[w.shared].pages + static_cast<int64_t>(w.row) * A.stream[w.shared].max_pages + page) : -1;
+    };
+    constexpr int kHalves = D / 64;
+    const int half = lane % kHalves, page_of_tile = lane / kHalves;
+    const auto copy = [&](const Meta& m, int which, uint32_t dst, uint64_t* bar) {
+      const int y = page_of_tile < per_tile ? m.y[page_of_tile] : -1;
+      const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
+      if (lane == 0) mbar_expect_tx(bar, n * A.page * 128);
+      __syncwarp();
+      if (y >= 0) tensor_g2s_2d(dst + half * Z::kHalf + page_of_tile * A.page * 128, &A.map[m.shared][which], half * 64, y, bar);
+    };
+    uint32_t idle = 0, beat = 0;
+    bool ok = true;
+    while (ok && (!stopped || v_next < k_next)) {
+      bool progress = false;
+      if (!stopped && !described) {      // tell the others about the unit, or that there is none
+        const uint32_t slot = n_units % kUnits;
+        if (n_units < kUnits || __all_sync(0xffffffffu, mbar_test_wait(&C.empty[slot], (n_units / kUnits - 1) & 1u))) {
+          if (lane == 0) {
+            Unit& d = C.units[slot];
+            d = w;
+            if (!has) d.tiles = 0;
+            mbar_arrive(&C.full[slot]);
+          }
+          __syncwarp();
+          ++n_units;
+          progress = true;
+          if (!has) {
+            stopped = true;
+          } else {
+            described = true, tile = 0;
+            batch = w.first * per_tile;
+            ids = ask(batch), next_ids = ask(batch + 32);
+          }
+        }
+      }
+      if (described) {
+        const uint32_t i = k_next % Z::kK;
+        if (k_next < Z::kK || __all_sync(0xffffffffu, mbar_test_wait(&C.k_free[i], (k_next / Z::kK - 1) & 1u))) {
+          const int t = w.first + tile, page0 = t * per_tile;
+          if (page0 - batch >= 32) batch += 32, ids = next_ids, next_ids = ask(batch + 32);
+          const int32_t id = __shfl_sync(0xffffffffu, ids, min(31, page0 - batch + page_of_tile));
+          const bool exists = page_of_tile < per_tile && static_cast<int64_t>(page0 + page_of_tile) << A.page_shift < w.len;
+          const bool there = exists && static_cast<uint32_t>(id) < static_cast<uint32_t>(A.stream[w.shared].n_pages);
+          if (exists && !there) report(A, QC_ERR_BAD_PAGE);
+          Meta& m = C.meta[k_next % kMeta];
+          const uint32_t pages = __ballot_sync(0xffffffffu, there && half == 0);
+          if (half == 0 && page_of_tile < 4) m.y[page_of_tile] = there ? (id * A.hkv + w.kvh) << A.page_shift : -1;
+          if (lane == 0) {
+            int on = 0;
+            for (int b = 0; b < kKeys / 16; ++b) on |= (pages >> ((b * 16 >> A.page_shift) * kHalves) & 1) << b;
+            m.on = on, m.shared = w.shared;
+          }
+          __syncwarp();
+          copy(m, 0, sK + i * Z::kTile, &C.k[i]);
+          ++k_next;
+          progress = true;
+          if (++tile == w.tiles) described = false, has = find(w);
+        }
+      }
+      if (v_next < k_next) {
+        const uint32_t i = v_next % Z::kV;
+        if (v_next < Z::kV || __all_sync(0xffffffffu, mbar_test_wait(&C.v_free[i], (v_next / Z::kV - 1) & 1u))) {
+          copy(C.meta[v_next % kMeta], 1, sV + i * Z::kTile, &C.v[i]);
+          ++v_next;
+          progress = true;
+        }
+      }
+      if (progress) {
+        idle = 0;
+      } else if (++idle > (1u << 20) || ((idle & 1023u) == 0 && failed)) {
+        const uint32_t now = *reinterpret_cast<volatile uint32_t*>(&C.beat);
+        if (failed || now == beat) ok = false;
+        beat = now, idle = 0;
+      }
+    }
+    if (!ok) failed = 1;
+  } else if (works && warp == 4) {
+    // ------------------------------------------------------------------ products
+    constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((kKeys >> 3) << 17) | ((kRows >> 4) << 24);
+    constexpr uint32_t kIdescO = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((D >> 3) << 17) | ((kRows >> 4) << 24);
+    bool ok = true;
+    const auto wait_on = [&](uint64_t* bar, uint32_t parity) {      // warp-uniform, bounded: as long as something moves
+      if (!ok || __all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+      uint32_t beat = *reinterpret_cast<volatile uint32_t*>(&C.beat);
+      while (!__all_sync(0xffffffffu, bounded_wait(bar, parity))) {
+        const uint32_t now = *reinterpret_cast<volatile uint32_t*>(&C.beat);
+        if (failed || __all_sync(0xffffffffu, now == beat)) {
+          ok = false;
+          break;
+        }
+        beat = now;
+      }
+    };
+    const uint64_t qd = umma_desc(sQ, 16, 1024);
+    uint32_t s_next = 0, o_next = 0;      // tiles
+    const auto issue_scores = [&]() {
+      const uint32_t b = s_next & 1u, i = s_next % Z::kK;
+      // the buffer holds the weights of the tile before the last one until their products are done (products with different sums are
+      // not documented to run in the order of their issue)
+      if (s_next >= 2) wait_on(&C.o[b], (s_next / 2 - 1) & 1u);
+      wait_on(&C.k[i], (s_next / Z::kK) & 1u);
+      if (!ok) return;
+      tc5_fence_after();
+      scores<D>(tmem + kScoresAt + b * kKeys, qd, umma_desc(sK + i * Z::kTile, 16, 1024), kIdescS);
+      umma_commit(&C.s[b]);
+      umma_commit(&C.k_free[i]);
+      ++s_next;
+    };
+    for (uint32_t n = 0; ok; ++n) {
+      const uint32_t slot = n % kUnits;
+      wait_on(&C.full[slot], (n / kUnits) & 1u);
+      if (!ok) break;
+      const int tiles = *reinterpret_cast<volatile int32_t*>(&C.units[slot].tiles);
+      if (tiles == 0) break;
+      wait_on(&C.q, n & 1u);
+      for (int t = 0; t < 2 && t < tiles && ok; ++t) issue_scores();
+      for (int t = 0; t < tiles && ok; ++t) {
+        const uint32_t b = o_next & 1u, i = o_next % Z::kV;
+        wait_on(&C.p[b], (o_next / 2) & 1u);
+        wait_on(&C.v[i], (o_next / Z::kV) & 1u);
+        if (!ok) break;
+        tc5_fence_after();
+        umma_values(tmem + kOutAt, tmem + kScoresAt + b * kKeys, umma_desc(sV + i * Z::kTile, Z::kHalf, 1024), kIdescO, t > 0 ? 1u : 0u);
+        umma_commit(&C.o[b]);
+        umma_commit(&C.v_free[i]);
+        ++o_next;
+        if (t + 2 < tiles) issue_scores();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&C.empty[slot]);
+    }
+    // (nothing arrives behind the block's end)
+    if (s_next) wait_on(&C.k_free[(s_next - 1) % Z::kK], ((s_next - 1) / Z::kK) & 1u);
+    if (o_next) wait_on(&C.v_free[(o_next - 1) % Z::kV], ((o_next - 1) / Z::kV) & 1u);
+    if (!ok) failed = 1;
+    __syncwarp();
+  } else if (works) {
+    // ------------------------------------------------------------------ rows
+    const uint32_t t_row = tmem + (static_cast<uint32_t>(warp * 32) << 16);   // this warp's 32 lanes of tensor memory
+    bool ok = true;
+    const auto wait_on = [&](uint64_t* bar, uint32_t parity) {
+      if (!ok || __all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+      uint32_t beat = *reinterpret_cast<volatile uint32_t*>(&C.beat);
+      while (!__all_sync(0xffffffffu, bounded_wait(bar, parity))) {
+        const uint32_t now = *reinterpret_cast<volatile uint32_t*>(&C.beat);
+        if (failed || __all_sync(0xffffffffu, now == beat)) {
+          ok = false;
+          break;
+        }
+        beat = now;
+      }
+    };
+    uint32_t t0 = 0;      // tiles of the units before
+    // a unit as this thread sees it: its row (of n_here, held `copies` times), the row's query
+    struct Mine {
+      Unit u;
+      int copies, row, copy, seen;
+      int64_t token;
+      int head;
+      bool real;
+    };
+    const auto take = [&](uint32_t n, Mine& x) {
+      wait_on(&C.full[n % kUnits], (n / kUnits) & 1u);
+      if (!ok) return;
+      x.u = C.units[n % kUnits];
+      x.copies = x.u.n_here <= 32 ? 4 : x.u.n_here <= 64 ? 2 : 1;
+      const int each = kRows / x.copies;
+      x.copy = static_cast<int>(threadIdx.x) / each, x.row = static_cast<int>(threadIdx.x) - x.copy * each;
+      x.real = x.row < x.u.n_here;
+      const int flat = static_cast<int>(x.u.row0 % A.group) + x.row, more = flat / A.group;      // (32 bits: the row inside its query's heads)
+      const int64_t query = x.u.row0 / A.group + more;
+      x.head = x.u.kvh * A.group + flat - more * A.group;
+      x.token = x.u.token0 + query;
+      x.seen = x.u.shared || !A.causal ? x.u.len : max(0, x.u.len - (x.u.queries - 1 - static_cast<int>(query)));
+    };
+    uint4 q[D / 8];
+    const auto ask_query = [&](const Mine& x) {
+      const StreamArgs& S = A.stream[x.u.shared];
+      const uint4* p = reinterpret_cast<const uint4*>(S.q + x.token * S.q_stride + static_cast<int64_t>(x.head) * D);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) q[i] = x.real ? __ldg(p + i) : make_uint4(0, 0, 0, 0);
+    };
+    const auto put_query = [&]() {
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) sts128(sQ + (i >> 3) * Z::kQHalf + threadIdx.x * 128 + (((i & 7) ^ (threadIdx.x & 7)) << 4), q[i]);
+      fence_proxy_async();
+      mbar_arrive(&C.q);
+    };
+    Mine x;
+    take(0, x);
+    if (ok && x.u.tiles) ask_query(x), put_query();
+    for (uint32_t n = 0;; ++n) {
+      if (!rows_all(ok) || x.u.tiles == 0) break;
+      float ref = -INFINITY, sum = 0.f;
+      const bool idle = x.copies == 1 && warp * 32 >= x.u.n_here;      // a warp without rows
+      const auto weigh = [&](auto tag, int t, uint32_t gt, uint32_t on, bool masked) {
+        constexpr int REP = decltype(tag)::value, N = kKeys / REP;
+        const uint32_t at = t_row + kScoresAt + (gt & 1u) * kKeys;
+        const int col0 = REP == 1 ? 0 : x.copy * N;
+        float p[N];
+        if constexpr (REP == 1) {
+          uint32_t r0[32], r1[32];
+          tmem_ld32_nowait(at, r0);
+          tmem_ld32_nowait(at + 32, r1);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) p[j] = __uint_as_float(r0[j]), p[32 + j] = __uint_as_float(r1[j]);
+        } else if constexpr (REP == 2) {
+          uint32_t r[32];
+          tmem_ld32(at + col0, r);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) p[j] = __uint_as_float(r[j]);
+        } else {
+          uint32_t r[16];
+          tmem_ld16(at + col0, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) p[j] = __uint_as_float(r[j]);
+        }
+        if (masked) {
+          const int left = x.seen - (t * kKeys + col0);
+          const uint32_t here = on >> (col0 / 16);
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (j >= left || !(here >> (j / 16) & 1u)) p[j] = -INFINITY;
+        }
+        float mx[4] = {p[0], p[1], p[2], p[3]};
+#pragma unroll
+        for (int j = 4; j < N; j += 2) mx[(j >> 1) & 3] = max3(mx[(j >> 1) & 3], p[j], p[j + 1]);
+        const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * A.scale_log2;   // (the scale is positive)
+        float corr = 1.f;
+        if ((top > ref + kRescale || ref == -INFINITY) && top != -INFINITY) {
+          corr = exp2f(ref - top);      // 0 on the first keys
+          ref = top;
+        }
+        const float less = ref == -INFINITY ? 0.f : -ref;
+        float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          const float2 y = fma2(make_float2(p[j], p[j + 1]), make_float2(A.scale_log2, A.scale_log2), make_float2(less, less));
+          p[j] = ex2_approx(y.x);
+          p[j + 1] = ex2_approx(y.y);
+          ps[(j >> 1) & 1] = add2(ps[(j >> 1) & 1], make_float2(p[j], p[j + 1]));
+        }
+        sum = sum * corr + ((ps[0].x + ps[0].y) + (ps[1].x + ps[1].y));
+        if (gt != t0 && __any_sync(0xffffffffu, corr != 1.f)) {      // rare: the sums so far go to the new reference
+          wait_on(&C.o[(gt - 1) & 1u], ((gt - 1) / 2) & 1u);
+          if (!ok) return;
+          tc5_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t r[32];
+            tmem_ld32(t_row + kOutAt + c, r);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * corr);
+            tmem_st32(t_row + kOutAt + c, r);
+          }
+          tmem_wait_st();
+        }
+        uint32_t w[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          constexpr int kEach = N / 2;
+          const uint32_t y = pack_bf16x2(p[j % kEach * 2], p[j % kEach * 2 + 1]);
+          w[j] = REP == 1 || j / kEach == x.copy ? y : 0u;      // (the other copies' keys weigh nothing in this one)
+        }
+        tmem_st32(at, w);
+        tmem_wait_st();
+      };
+      for (int i = 0; i < x.u.tiles && ok; ++i) {
+        const uint32_t gt = t0 + i;
+        const int t = x.u.first + i;
+        wait_on(&C.s[gt & 1u], (gt / 2) & 1u);
+        if (!ok) break;
+        tc5_fence_after();
+        const uint32_t on = *reinterpret_cast<volatile int32_t*>(&C.meta[gt % kMeta].on);
+        const int left = x.u.len - t * kKeys;
+        if (!idle) {
+          const bool masked = on != 15u || (t + 1) * kKeys > x.u.all_see;
+          if (x.copies == 4) weigh(std::integral_constant<int, 4>{}, t, gt, on, masked);
+          else if (x.copies == 2) weigh(std::integral_constant<int, 2>{}, t, gt, on, masked);
+          else weigh(std::integral_constant<int, 1>{}, t, gt, on, masked);
+        }
+        if (on != 15u || left < kKeys) {      // values that no token has may be anything: a weight of 0 does not cancel a NaN
+          const uint32_t v = gt % Z::kV;
+          wait_on(&C.v[v], (gt / Z::kV) & 1u);
+          const int key = threadIdx.x & 63, h = threadIdx.x >> 6;
+          if (ok && h < D / 64 && (key >= left || !(on >> (key / 16) & 1u))) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sts128(sV + v * Z::kTile + h * Z::kHalf + key * 128 + c * 16, make_uint4(0, 0, 0, 0));
+          }
+          fence_proxy_async();
+        }
+        if (!ok) break;
+        tc5_fence_before();
+        mbar_arrive(&C.p[gt & 1u]);
+      }
+      t0 += x.u.tiles;
+      Mine next;
+      if (ok) take(n + 1, next);
+      if (ok && next.u.tiles) ask_query(next);      // on their way while this unit ends
+      wait_on(&C.o[(t0 - 1) & 1u], ((t0 - 1) / 2) & 1u);
+      if (!rows_all(ok)) {
+        ok = false;
+        break;
+      }
+      tc5_fence_after();
+
+      // ---- the unit's rows: to their queries' places, or as a piece
+      const size_t heads = static_cast<size_t>(A.n_tokens) * A.hq;
+      const auto to_of = [&](int row, int64_t token, int head) -> float* {
+        return x.u.place < 0 ? A.rows + (x.u.shared * heads + token * A.hq + head) * D : A.pieces + static_cast<size_t>(x.u.place) * (kRows * (D + 2)) + row * D;
+      };
+      const auto ml_of = [&](int row, int64_t token, int head) -> float2* {
+        return x.u.place < 0 ? A.row_ml + x.u.shared * heads + token * A.hq + head
+                             : reinterpret_cast<float2*>(A.pieces + static_cast<size_t>(x.u.place) * (kRows * (D + 2)) + kRows * D) + row;
+      };
+      float2* const ml = reinterpret_cast<float2*>(smem);      // [128], where the queries were: every product has read them
+      if (threadIdx.x < 4) C.redo[threadIdx.x] = 0;
+      // (the second half of the queries' place: the copies' sums)
+      if (x.copies > 1) ml[threadIdx.x] = make_float2(ref, sum);
+      rows_barrier();
+      float factor = 1.f, top = ref, all = sum;
+      if (x.copies > 1) {
+        const int each = kRows / x.copies;
+        top = -INFINITY, all = 0.f;
+        for (int c = 0; c < x.copies; ++c) top = fmaxf(top, ml[c * each + x.row].x);
+        for (int c = 0; c < x.copies; ++c) {
+          const float2 y = ml[c * each + x.row];
+          if (y.y != 0.f) all = fmaf(y.y, y.x == -INFINITY ? 1.f : ex2_approx(y.x - top), all);      // (a sum on no reference is no number)
+        }
+        factor = sum == 0.f ? 0.f : ref == -INFINITY ? 1.f : ex2_approx(ref - top);
+      }
+      bool strange = false;      // a sum that is no finite number although the row's weights are numbers
+      if (x.copies == 1) {
+        float* const to = to_of(x.row, x.token, x.head);
+        if (!idle) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t r[32];
+            tmem_ld32(t_row + kOutAt + c, r);
+            uint32_t most = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) most = max(most, r[j] & 0x7fffffffu);
+            strange |= most >= 0x7f800000u;
+            if (x.real)
+#pragma unroll
+              for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j, 1.f);
+          }
+        }
+        if (x.real) *ml_of(x.row, x.token, x.head) = make_float2(ref, sum);
+      } else {
+        // D / 2 elements of all rows at a time through the queries' place
+        constexpr int kRound = D / 2, kChunks = kRound / 4;
+        rows_barrier();      // (the references have been read)
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += kRound) {
+#pragma unroll 1
+          for (int c = 0; c < kRound; c += 32) {
+            uint32_t r[32];
+            tmem_ld32(t_row + kOutAt + c0 + c, r);
+            uint32_t most = 0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) most = max(most, r[j] & 0x7fffffffu);
+            strange |= most >= 0x7f800000u;
+            if (x.real) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const auto part = [&](int e) { return factor == 0.f ? 0u : __float_as_uint(__uint_as_float(r[4 * j + e]) * factor); };
+                sts128(sQ + threadIdx.x * (kRound * 4) + (((c / 4 + j) ^ (threadIdx.x & 7)) << 4), make_uint4(part(0), part(1), part(2), part(3)));
+              }
+            }
+          }
+          rows_barrier();
+          const int each = kRows / x.copies;
+          for (int i = threadIdx.x; i < x.u.n_here * kChunks; i += kRows) {
+            const int row = i / kChunks, chunk = i - row * kChunks;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = 0; c < x.copies; ++c) {
+              const int from = c * each + row;
+              const uint4 z = lds128(sQ + from * (kRound * 4) + ((chunk ^ (from & 7)) << 4));
+              y.x += __uint_as_float(z.x), y.y += __uint_as_float(z.y), y.z += __uint_as_float(z.z), y.w += __uint_as_float(z.w);
+            }
+            const int flat = static_cast<int>(x.u.row0 % A.group) + row, more = flat / A.group;
+            float* const to = to_of(row, x.u.token0 + x.u.row0 / A.group + more, x.u.kvh * A.group + flat - more * A.group);
+            reinterpret_cast<float4*>(to + c0)[chunk] = y;
+          }
+          rows_barrier();
+        }
+        if (x.real && x.copy == 0) *ml_of(x.row, x.token, x.head) = make_float2(top, all);
+      }
+      if (strange && x.real && isfinite(all)) atomicOr(&C.redo[x.row >> 5], 1u << (x.row & 31));
+      rows_barrier();
+      if (C.redo[0] | C.redo[1] | C.redo[2] | C.redo[3]) {      // rare: rows whose sums a value behind a weight of 0 may have spoiled, by hand
+        for (int row = warp; row < x.u.n_here; row += 4) {
+          if (!(C.redo[row >> 5] >> (row & 31) & 1u)) continue;
+          const int flat = static_cast<int>(x.u.row0 % A.group) + row, more = flat / A.group;
+          const int64_t query = x.u.row0 / A.group + more, token = x.u.token0 + query;
+          const int head = x.u.kvh * A.group + flat - more * A.group;
+          const int seen = x.u.shared || !A.causal ? x.u.len : max(0, x.u.len - (x.u.queries - 1 - static_cast<int>(query)));
+          sweep<D>(A, A.stream[x.u.shared], x.u.row, x.u.kvh, token, head, x.u.first * kKeys, min(seen, (x.u.first + x.u.tiles) * kKeys), to_of(row, token, head),
+                   ml_of(row, token, head), &C.beat, lane);
+        }
+        rows_barrier();
+      }
+      tc5_fence_before();
+      mbar_arrive(&C.empty[n % kUnits]);
+      x = next;
+      if (x.u.tiles) put_query();
+    }
+    if (!ok) failed = 1;
+  }
+  __syncwarp();
+  tc5_fence_before();
+  __syncthreads();
+  if (works && failed && threadIdx.x == 0) report(A, QC_ERR_TIMEOUT);
+  if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns) : "memory");
+}
+
+// What a part with reference m and a sum counts for on reference top.  Minus infinity with a sum means that its scores were no numbers.
+__device__ __forceinline__ float weight_of(float2 ml, float top) { return ml.y == 0.f ? 0.f : ml.x == -INFINITY ? NAN : exp2f(ml.x - top); }
+
+// Puts the parts of each row together: a warp per row, a part's reference and sum per lane.  Grid: (sequences, parts of their rows).
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttendArgs A) {
+  pdl_wait();
+  const Plan plan = *A.plan;
+  if (!plan.fine) return;
+  const int lane = threadIdx.x & 31, step = gridDim.y * 8;
+  const Record own = A.records[A.n_groups + blockIdx.x];
+  Record prefix{};
+  if (own.group >= 0) prefix = A.records[own.group];
+  const size_t heads = static_cast<size_t>(A.n_tokens) * A.hq;
+  for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < own.queries * A.hq; r += step) {
+    const int query = r / A.hq, head = r - query * A.hq, kvh = head / A.group;
+    const int64_t token = own.token0 + query;
+    const size_t at = token * A.hq + head;
+    float m = -INFINITY, l = 0.f, o[D / 32] = {};
+#pragma unroll 1
+    for (int kind = own.group >= 0 ? 1 : 0; kind >= 0; --kind) {
+      const Record& u = kind ? prefix : own;
+      if (u.tiles == 0) continue;
+      const int64_t flat = (token - u.token0) * A.group + head - kvh * A.group;
+      const uint32_t per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
+      const uint32_t tiles_at = u.base + (kvh * per_head + static_cast<uint32_t>(flat / kRows)) * unit_cost(u.tiles) + kUnitCost;
+      const uint32_t first = worker_at(plan.cost, plan.workers, tiles_at), last = worker_at(plan.cost, plan.workers, tiles_at + (u.tiles - 1) * kTileCost);
+      const int row = static_cast<int>(flat % kRows);
+      const auto part = [&](uint32_t w) -> const float* {
+        return first == last ? A.rows + (kind * heads + at) * D : A.pieces + (static_cast<size_t>(w) * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + row * D;
+      };
+      for (uint32_t w0 = first; w0 <= last; w0 += 32) {
+        const uint32_t w = w0 + lane;
+        const int n = min(32u, last + 1 - w0);
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (lane < n)
+          ml = __ldcg(first == last ? A.row_ml + kind * heads + at
+                                    : reinterpret_cast<const float2*>(A.pieces + (static_cast<size_t>(w) * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + kRows * D) + row);
+        float top = ml.x;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        top = fmaxf(top, m);
+        const float f = weight_of(ml, top), old = weight_of(make_float2(m, l), top);
+        float sum = ml.y * f;
+#pragma unroll
+        for (int k = 16; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        l = l * old + sum, m = top;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) o[k] = old == 0.f ? 0.f : o[k] * old;
+#pragma unroll 4
+        for (int k = 0; k < n; ++k) {
+          const float fk = __shfl_sync(0xffffffffu, f, k);
+          const float* p = part(w0 + k);
+          float v[D / 32];
+          if constexpr (D == 128) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(p) + lane);
+            v[0] = y.x, v[1] = y.y, v[2] = y.z, v[3] = y.w;
+          } else {
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(p) + lane);
+            v[0] = y.x, v[1] = y.y;
+          }
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e) o[e] += fk == 0.f ? 0.f : v[e] * fk;
+        }
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (D == 128) reinterpret_cast<uint2*>(A.out + at * D)[lane] = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    else reinterpret_cast<uint32_t*>(A.out + at * D)[lane] = pack_bf16x2(o[0] * inv, o[1] * inv);
+    if (A.lse && lane == 0) A.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
   }
 }
 
@@ -172,7 +934,60 @@ int32_t check_sizes(const qc_paged_attend_args* a) {
   return QC_OK;
 }
 
-size_t workspace_bytes(const qc_paged_attend_args* a) { return 256; }
+// The workspace: plan and records, then the sums of whole units' rows, then pieces, each part at a multiple of 256 bytes.
+constexpr int kMostWorkers = 320;
+struct Layout {
+  size_t records, rows, row_ml, pieces, bytes;
+};
+Layout layout_of(const qc_paged_attend_args* a) {
+  const auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
+  const size_t heads = static_cast<size_t>(a->n_tokens) * a->n_q_heads * (a->n_groups ? 2 : 1);
+  Layout w{};
+  w.records = 256;
+  w.rows = w.records + up(static_cast<size_t>(a->n_groups + a->n_seqs) * sizeof(Record));
+  w.row_ml = w.rows + up(heads * a->head_dim * 4);
+  w.pieces = w.row_ml + up(heads * 8);
+  w.bytes = w.pieces + static_cast<size_t>(kMostWorkers) * 2 * kRows * (a->head_dim + 2) * 4;
+  return w;
+}
+size_t workspace_bytes(const qc_paged_attend_args* a) { return layout_of(a).bytes; }
+
+// A pool as rows of D elements: a copy brings 64 of them from the tokens of one page and head, with the 128-byte swizzle.
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int32_t make_map(CUtensorMap* out, const void* pool, const qc_paged_attend_args* a, int32_t n_pages) {
+  static const EncodeFn encode = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) fn = nullptr;
+    return reinterpret_cast<EncodeFn>(fn);
+  }();
+  if (!encode) return QC_ERR_CUDA;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a->head_dim), static_cast<cuuint64_t>(n_pages) * a->n_kv_heads * a->page_size};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a->head_dim) * 2};
+  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(a->page_size)}, steps[2] = {1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? QC_OK
+             : QC_ERR_CUDA;
+}
+
+template <int D>
+cudaError_t launch(const AttendArgs& A, int device, cudaStream_t stream) {
+  constexpr int kBytes = Shape<D>::kTiles + sizeof(Control);
+  static std::atomic<bool> configured[64] = {};     // per device: the kernel may take that much
+  cudaError_t e;
+  if (device >= 64 || !configured[device].load(std::memory_order_relaxed)) {
+    e = cudaFuncSetAttribute(paged_attend_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    if (device < 64) configured[device].store(true, std::memory_order_relaxed);
+  }
+  int sms = 0;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) != cudaSuccess) return e;
+  if ((e = launch_pdl(paged_attend_kernel<D>, dim3(min(2 * sms, kMostWorkers)), dim3(kBlock), kBytes, stream, A)) != cudaSuccess) return e;
+  const int64_t rows = static_cast<int64_t>(A.starts ? A.max_queries : 1) * A.hq;
+  return launch_pdl(paged_join_kernel<D>, dim3(A.n_seqs, static_cast<unsigned>(min((rows + 7) / 8, static_cast<int64_t>(65535)))), dim3(256), 0, stream, A);
+}
 
 // Whether the rows written lie over rows of queries.
 bool over_queries(const qc_paged_stream& s, const qc_paged_attend_args* a) {
@@ -196,7 +1011,7 @@ extern "C" int32_t qc_paged_workspace_bytes(const qc_paged_attend_args* args, si
 extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_paged_attend_args* args) {
   if (const int32_t bad = check_sizes(args)) return bad;
   if (!args->out_dev || off(args->out_dev, 16) || off(args->lse_out_dev, 4) || off(args->status_dev, 4) || off(args->seq_ids_dev, 4) || off(args->starts_dev, 4) ||
-      off(args->groups_dev, 4) || off(args->shared_ids_dev, 4) || off(args->workspace_dev, 16))
+      off(args->groups_dev, 4) || off(args->shared_ids_dev, 4) || off(args->workspace_dev, 256))
     return QC_ERR_INVALID_ARG;
   if (!(args->softmax_scale >= 0.f) || !isfinite(args->softmax_scale)) return QC_ERR_INVALID_ARG;
   if (!args->starts_dev && args->n_tokens < args->n_seqs) return QC_ERR_INVALID_ARG;
@@ -216,7 +1031,10 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   if (over_queries(args->own, args) || (shared && over_queries(args->shared, args))) return QC_ERR_INVALID_ARG;
   A.ids = args->seq_ids_dev, A.starts = args->starts_dev, A.groups = args->groups_dev, A.shared_ids = args->shared_ids_dev;
   A.out = static_cast<uint16_t*>(args->out_dev), A.lse = args->lse_out_dev, A.status = args->status_dev;
-  A.plan = static_cast<int32_t*>(args->workspace_dev);
+  uint8_t* const work = static_cast<uint8_t*>(args->workspace_dev);
+  const Layout w = layout_of(args);
+  A.plan = reinterpret_cast<Plan*>(work), A.records = reinterpret_cast<Record*>(work + w.records), A.rows = reinterpret_cast<float*>(work + w.rows);
+  A.row_ml = reinterpret_cast<float2*>(work + w.row_ml), A.pieces = reinterpret_cast<float*>(work + w.pieces);
   A.hq = args->n_q_heads, A.hkv = args->n_kv_heads, A.group = A.hq / A.hkv, A.page = args->page_size;
   A.page_shift = A.page == 16 ? 4 : A.page == 32 ? 5 : 6;
   A.n_seqs = args->n_seqs, A.n_groups = args->n_groups, A.n_tokens = args->n_tokens, A.max_queries = args->max_queries, A.causal = args->causal != 0;
@@ -225,6 +1043,10 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (const int32_t bad = status_of(launch_pdl(paged_plan_kernel, dim3(1), dim3(256), 0, stream, A))) return bad;
-  return status_of(launch_pdl(args->head_dim == 128 ? paged_attend_kernel<128> : paged_attend_kernel<64>, dim3(A.n_seqs, A.hq), dim3(128), 0, stream, A));
+  for (int i = 0; i <= (shared ? 1 : 0); ++i) {
+    const qc_paged_stream& s = i ? args->shared : args->own;
+    if (const int32_t bad = make_map(&A.map[i][0], s.k_pool_dev, args, s.n_pages)) return bad;
+    if (const int32_t bad = make_map(&A.map[i][1], s.v_pool_dev, args, s.n_pages)) return bad;
+  }
+  return status_of(args->head_dim == 128 ? launch<128>(A, device, stream) : launch<64>(A, device, stream));
 }

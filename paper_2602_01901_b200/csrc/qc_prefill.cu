@@ -10,7 +10,7 @@
 // (mma.m16n8k16 bf16 -> fp32); the score accumulators of a warp are re-used in registers as the
 // A operand of the value product.  Softmax is online, in the log2 domain, fp32.
 
-#include "qc_device.cuh"
+#include "qc_umma.cuh"
 
 namespace qc {
 namespace {
@@ -333,117 +333,6 @@ constexpr int kTD = 128;        // head dim
 constexpr uint32_t kTmemCols = 256;
 constexpr uint32_t kColS = 0, kColO = 128;   // scores: two buffers of 64 columns; accumulator: 128 columns
 constexpr float kRescaleThreshold = 8.f;   // log2 units
-
-__device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  // start address, leading / stride byte offsets (all >> 4), descriptor version 1, 128-byte swizzle
-  return static_cast<uint64_t>((saddr >> 4) & 0x3fff) | (static_cast<uint64_t>((lbo_bytes >> 4) & 0x3fff) << 16) |
-         (static_cast<uint64_t>((sbo_bytes >> 4) & 0x3fff) << 32) | (1ull << 46) | (2ull << 61);
-}
-// S = Q K^T for one tile: eight products (k-steps of 16 along the head dimension) issued by one
-// elected lane from warp-uniform code.  adesc/bdesc address k-step 0; a k-step advances the start
-// address by 32 bytes inside a 128-byte swizzle row, and the second 64 elements of the head
-// dimension sit one half-tile further (a_half / b_half bytes).
-template <uint32_t A_HALF, uint32_t B_HALF>
-__device__ __forceinline__ void umma_scores(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc) {
-  asm volatile(
-      "{\n\t.reg .pred e, pz, po;\n\t.reg .b64 da, db;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 pz, 0, 0;\n\tsetp.eq.b32 po, 0, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, pz;\n\t"
-      "add.u64 da, %1, 2;\n\tadd.u64 db, %2, 2;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, 4;\n\tadd.u64 db, %2, 4;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, 6;\n\tadd.u64 db, %2, 6;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, %4;\n\tadd.u64 db, %2, %5;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, %4 + 2;\n\tadd.u64 db, %2, %5 + 2;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, %4 + 4;\n\tadd.u64 db, %2, %5 + 4;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t"
-      "add.u64 da, %1, %4 + 6;\n\tadd.u64 db, %2, %5 + 6;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, po;\n\t}"
-      :: "r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "n"(A_HALF >> 4), "n"(B_HALF >> 4) : "memory");
-}
-// O (+)= P V for one tile of 64 keys: four products (k-steps of 16 keys).  The weights are read from
-// tensor memory (8 columns per k-step), the V rows MN-major from shared memory (16 rows = 2048 bytes
-// per k-step).  `accumulate` = 0 starts a new accumulator.
-__device__ __forceinline__ void umma_values(uint32_t tmem_d, uint32_t tmem_p, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred e, pa, po;\n\t.reg .b64 db;\n\t.reg .b32 ta;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 pa, %4, 0;\n\tsetp.eq.b32 po, 0, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, pa;\n\t"
-      "add.u32 ta, %1, 8;\n\tadd.u64 db, %2, 128;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %3, po;\n\t"
-      "add.u32 ta, %1, 16;\n\tadd.u64 db, %2, 256;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %3, po;\n\t"
-      "add.u32 ta, %1, 24;\n\tadd.u64 db, %2, 384;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], db, %3, po;\n\t}"
-      :: "r"(tmem_d), "r"(tmem_p), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar))
-      : "memory");
-}
-__device__ __forceinline__ void tc5_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc5_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      :: "r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-         "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-         "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-
-// Bounded wait on an mbarrier phase.
-__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity) {
-  constexpr uint32_t kLimit = 1u << 18;
-  uint32_t done = mbar_try_wait(bar, parity);
-  for (uint32_t spin = 0; !done && spin < kLimit; ++spin) done = mbar_try_wait(bar, parity);
-  return done != 0;
-}
-// one non-blocking look at an mbarrier phase
-__device__ __forceinline__ uint32_t mbar_test_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(done)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return done;
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 
 __device__ __forceinline__ void tensor_s2g_4d(const void* tmap, uint32_t src_smem, int32_t x, int32_t y, int32_t z, int32_t w) {
   asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::
