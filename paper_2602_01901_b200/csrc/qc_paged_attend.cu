@@ -35,6 +35,7 @@ constexpr uint32_t kScoresAt = 0, kOutAt = 128, kColumns = 256;   // tensor memo
 constexpr float kRescale = 8.f;  // the reference of a row moves when its scores have grown by 2^8
 constexpr uint32_t kUnitCost = 2, kTileCost = 1;
 constexpr uint32_t kMostCost = 1u << 27;
+constexpr int kMostHeld = 2048;  // items that a block keeps in shared memory while it looks for its range
 
 struct StreamArgs {
   const uint16_t* q;
@@ -54,10 +55,10 @@ struct Record {
   int32_t spare[3];
 };
 
+// Whether the batch is computed, and its ranges: the first `longer` workers have costs of `per` + 1, the others `per`.
 struct Plan {
   int32_t fine;
-  uint32_t cost, workers;
-  int32_t spare;
+  uint32_t per, longer, spare;
 };
 
 struct AttendArgs {
@@ -77,7 +78,7 @@ struct AttendArgs {
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, n_groups, n_tokens, max_queries, causal;
-  float scale_log2;
+  float scale_log2, inv_group;
 };
 
 __device__ __forceinline__ void report(const AttendArgs& A, int code) {
@@ -97,6 +98,20 @@ struct Item {
   uint32_t units, per_head;      // units; those of a KV head
   bool fine;
 };
+struct Held {
+  int32_t token0, queries, row, len;
+};
+__device__ __forceinline__ void count_units(const AttendArgs& A, Item& u) {
+  u.tiles = (u.len + kKeys - 1) / kKeys;
+  u.per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
+  u.units = u.tiles ? min(static_cast<uint64_t>(u.per_head) * A.hkv, static_cast<uint64_t>(kMostCost)) : 0;
+}
+__device__ __forceinline__ Item item_from(const AttendArgs& A, const Held& h) {
+  Item u{};
+  u.token0 = h.token0, u.queries = h.queries, u.row = h.row, u.len = h.len, u.fine = true;
+  if (u.queries) count_units(A, u);
+  return u;
+}
 __device__ __forceinline__ Item item_of(const AttendArgs& A, int i, bool tell) {
   Item u{};
   const bool shared = i < A.n_groups;
@@ -119,9 +134,7 @@ __device__ __forceinline__ Item item_of(const AttendArgs& A, int i, bool tell) {
   u.token0 = static_cast<int32_t>(a), u.queries = static_cast<int32_t>(b - a);
   if (u.queries == 0) return u;
   u.len = length_of(A, S, u.row, tell);
-  u.tiles = (u.len + kKeys - 1) / kKeys;
-  u.per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
-  u.units = u.tiles ? min(static_cast<uint64_t>(u.per_head) * A.hkv, static_cast<uint64_t>(kMostCost)) : 0;
+  count_units(A, u);
   return u;
 }
 __device__ __forceinline__ uint32_t unit_cost(int tiles) { return kUnitCost + tiles * kTileCost; }
@@ -130,18 +143,24 @@ __device__ __forceinline__ uint32_t cost_of(const Item& u) {
   return static_cast<uint32_t>(min(static_cast<uint64_t>(u.units) * unit_cost(u.tiles), static_cast<uint64_t>(kMostCost) + 1));
 }
 
-// Ranges: worker w has the costs [range_begin(w), range_begin(w + 1)); every range is as long as a tile at least.
-__device__ __forceinline__ uint32_t range_begin(uint32_t cost, uint32_t workers, uint32_t w) { return static_cast<uint32_t>(static_cast<uint64_t>(cost) * w / workers); }
-__device__ __forceinline__ uint32_t worker_at(uint32_t cost, uint32_t workers, uint32_t at) {
-  return static_cast<uint32_t>(((static_cast<uint64_t>(at) + 1) * workers - 1) / cost);
+// Every range is as long as a tile at least.
+__device__ __forceinline__ uint32_t range_begin(const Plan& p, uint32_t w) { return w * p.per + min(w, p.longer); }
+__device__ __forceinline__ uint32_t worker_at(const Plan& p, uint32_t at) {
+  const uint32_t turn = p.longer * (p.per + 1);
+  return at < turn ? at / (p.per + 1) : p.longer + (at - turn) / p.per;
 }
 
 struct Unit {
-  int64_t row0;                  // its first query row among the item's
-  int32_t token0, queries, n_here, kvh, shared, row, first, tiles, len;
+  int32_t token0;                // the token of its first row
+  int32_t head0;                 // and that row's head inside the KV head's group
+  int32_t query0, queries;       // the query of its first row among the item's
+  int32_t n_here, kvh, shared, row, first, tiles, len;
   int32_t all_see;               // keys that every row sees
   int32_t place;                 // of a piece: worker * 2, + 1 where the unit begins in the range; -1: the unit is whole
 };
+
+// How often a unit's rows are held: at blocks of 32 or 64 rows, where the copies' sums fit the place where they meet.
+__device__ __forceinline__ int copies_of(int n_here) { return n_here <= 30 ? 4 : n_here <= 60 ? 2 : 1; }
 
 struct Meta {
   int32_t y[4];                  // of a tile's pages: the first row in the pool, -1: the page is not there
@@ -151,9 +170,10 @@ struct Meta {
 
 template <int D>
 struct Shape {
-  static constexpr int kK = D == 128 ? 3 : 4, kV = D == 128 ? 2 : 4;      // tiles under way
+  static constexpr int kRing = D == 128 ? 2 : 4;      // tiles of K, and of V, under way
   static constexpr uint32_t kTile = kKeys * D * 2, kHalf = kKeys * 128, kQ = kRows * D * 2, kQHalf = kRows * 128;
-  static constexpr uint32_t kTiles = kQ + (kK + kV) * kTile;
+  static constexpr uint32_t kStage = kQ + 2 * kRing * kTile, kStageBytes = 15360, kRefs = kStage + kStageBytes;      // where the copies' sums meet, and their references
+  static constexpr uint32_t kTiles = kRefs + kRows * 8;
 };
 
 struct Control {
@@ -193,12 +213,14 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Whether all rows' warps say so: they go on together or not at all, so none waits at a barrier for one that has given up.
+// Whether all rows' threads say so, and whether any does.  Rows' warps go on together or not at all, so that none waits at a barrier for
+// one that has given up.
 __device__ __forceinline__ bool rows_all(bool x) {
   uint32_t all;
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(static_cast<uint32_t>(x)), "n"(kRows) : "memory");
   return all != 0;
 }
+__device__ __forceinline__ bool rows_any(bool x) { return !rows_all(!x); }
 __device__ __forceinline__ void rows_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kRows) : "memory"); }
 
 // Keys [from, to) of a table row for one query, by one warp, a key at a time: what the tensor cores cannot give where a value that is
@@ -248,10 +270,8 @@ __device__ __noinline__ void sweep(const AttendArgs& A, const StreamArgs& S, int
     }
 }
 
-__device__ __forceinline__ void store_32(float* p, const uint32_t* r, float f) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(__uint_as_float(r[0]) * f), "f"(__uint_as_float(r[1]) * f),
-               "f"(__uint_as_float(r[2]) * f), "f"(__uint_as_float(r[3]) * f), "f"(__uint_as_float(r[4]) * f), "f"(__uint_as_float(r[5]) * f),
-               "f"(__uint_as_float(r[6]) * f), "f"(__uint_as_float(r[7]) * f)
+__device__ __forceinline__ void store_32(float* p, const uint32_t* r) {      // 32 bytes, a sector
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
 
@@ -262,16 +282,17 @@ __device__ __forceinline__ void store_32(float* p, const uint32_t* r, float f) {
 //   s[b]                tensor core -> rows: scores of tile t in buffer b = t & 1
 //   p[b]                rows -> warp 4: its weights are there, over the scores
 //   o[b]                tensor core -> warp 4, rows: its value products are done
-//   k_free[i], v_free[i]  tensor core -> warp 5: the tile's place may be written
+//   k_free[i], v_free[i]  tensor core -> warp 5: the tile's place may be written (rings of two: s and o say so)
 // No barrier runs two completions ahead of a waiter: the next completion needs something that the waiter does after it has seen
 // the one before.  Tiles are counted through all units of the block.
 template <int D>
 __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_constant__ AttendArgs A) {
   using Z = Shape<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kK * Z::kTile;
+  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kRing * Z::kTile, sStage = sQ + Z::kStage;
   Control& C = *reinterpret_cast<Control*>(smem + Z::kTiles);
   volatile int32_t& failed = C.failed;
+  constexpr bool kLong = Z::kRing > 2;      // rings of two are free when the score buffer, or its weights, are
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (sQ & 1023u) {      // (there is no static shared memory, so it begins at a multiple of 1024; products never run on a misplaced tile)
     if (threadIdx.x == 0) report(A, QC_ERR_PLAN);
@@ -285,6 +306,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       mbar_init(&C.q, kRows);
       fence_mbar_init();
       C.failed = 0, C.beat = 0;
+      for (int i = 0; i < 4; ++i) C.redo[i] = 0;
     }
   } else if (warp == 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&C.tmem)), "n"(kColumns) : "memory");
@@ -293,8 +315,10 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
   pdl_wait();
 
   // ---- the plan: costs of the items before each one, in the tiles' place until they come
-  uint32_t* const before = reinterpret_cast<uint32_t*>(smem + Z::kQ);      // [items + 1]
+  uint32_t* const before = reinterpret_cast<uint32_t*>(smem);      // [items]
   const int n_items = A.n_groups + A.n_seqs;
+  Held* const held = reinterpret_cast<Held*>(smem + kMostHeld * 8);      // [items], where there are no more than that
+  const bool holds = n_items <= kMostHeld;
   uint32_t total = 0;
   bool fine = true;
   for (int i0 = 0; i0 < n_items; i0 += kBlock) {
@@ -322,6 +346,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
     const uint32_t at = static_cast<uint32_t>(min(base + sum - mine, static_cast<uint64_t>(kMostCost) + 1));
     if (i < n_items) {
       before[i] = at;
+      if (holds) held[i] = Held{u.token0, u.queries, u.row, u.len};
       if (blockIdx.x == 0) {
         int group = -1;
         if (i >= A.n_groups && A.n_groups) {      // the last group that begins at or before the sequence, if it reaches it
@@ -346,23 +371,24 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
   fine = __syncthreads_and(fine);
   const bool few = total <= kMostCost;
   const uint32_t workers = max(1u, min(gridDim.x, total / kTileCost));
+  const Plan plan{fine && few, total / workers, total % workers, 0};
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    *A.plan = Plan{fine && few, total, workers, 0};
+    *A.plan = plan;
     if (!fine) report(A, QC_ERR_INVALID_ARG);
     else if (!few) report(A, QC_ERR_PLAN);
   }
+  const bool works = plan.fine && total && blockIdx.x < workers;
   tc5_fence_before();
   __syncthreads();
   tc5_fence_after();
   const uint32_t tmem = C.tmem;
-  const bool works = fine && few && total && blockIdx.x < workers;
 
   if (works && warp == 5) {
     // ------------------------------------------------------------------ units and tiles
-    uint32_t at = range_begin(total, workers, blockIdx.x);
-    const uint32_t end = range_begin(total, workers, blockIdx.x + 1);
+    uint32_t at = range_begin(plan, blockIdx.x), item_at;
+    const uint32_t end = range_begin(plan, blockIdx.x + 1);
     int item;
-    uint32_t item_at;
+    Item u, u_next{};
     {
       int lo = 0, hi = n_items - 1;      // the last item that begins at or before the range
       while (lo < hi) {
@@ -371,11 +397,11 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         else hi = mid - 1;
       }
       item = lo, item_at = before[lo];
+      u = holds ? item_from(A, held[item]) : item_of(A, item, false);
+      if (item + 1 < n_items) u_next = holds ? item_from(A, held[item + 1]) : item_of(A, item + 1, false);
     }
     __syncwarp();
     fence_proxy_async();      // (the costs have been read before copies take their place)
-    Item u = item_of(A, item, false), u_next{};
-    if (item + 1 < n_items) u_next = item_of(A, item + 1, false);
     // the next unit of the range
     const auto find = [&](Unit& w) -> bool {
       while (at < end) {
@@ -393,28 +419,41 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         at = unit_at + one;
         if (first >= last) continue;
         const int kvh = unit / u.per_head, part = unit - kvh * u.per_head;
-        w.row0 = static_cast<int64_t>(part) * kRows;
-        const int64_t rows = static_cast<int64_t>(u.queries) * A.group;
-        w.n_here = static_cast<int32_t>(min(static_cast<int64_t>(kRows), rows - w.row0));
-        w.token0 = u.token0, w.queries = u.queries, w.kvh = kvh, w.shared = item < A.n_groups, w.row = u.row, w.first = first, w.tiles = last - first, w.len = u.len;
-        w.all_see = w.shared || !A.causal ? u.len : max(0, u.len - (u.queries - 1 - static_cast<int>(w.row0 / A.group)));
+        const int64_t row0 = static_cast<int64_t>(part) * kRows, rows = static_cast<int64_t>(u.queries) * A.group;
+        w.n_here = static_cast<int32_t>(min(static_cast<int64_t>(kRows), rows - row0));
+        w.query0 = part ? static_cast<int32_t>(row0 / A.group) : 0, w.head0 = part ? static_cast<int32_t>(row0 - static_cast<int64_t>(w.query0) * A.group) : 0;
+        w.token0 = u.token0 + w.query0, w.queries = u.queries, w.kvh = kvh, w.shared = item < A.n_groups, w.row = u.row, w.first = first, w.tiles = last - first, w.len = u.len;
+        w.all_see = w.shared || !A.causal ? u.len : max(0, u.len - (u.queries - 1 - w.query0));
         w.place = first == 0 && last == u.tiles ? -1 : static_cast<int>(blockIdx.x) * 2 + (first == 0 ? 1 : 0);
         return true;
       }
       return false;
     };
-    Unit w{};
-    bool has = find(w), stopped = false;
+    const int per_tile = kKeys >> A.page_shift;
+    // a unit, whether there is one, and page ids, one per lane: from page `batch` of its row on, and the 32 behind them
+    struct Ahead {
+      Unit w;
+      bool has;
+      int32_t batch, ids, next_ids;
+    };
+    const auto ask = [&](const Unit& w, int from) -> int32_t {
+      const int page = from + lane;
+      const StreamArgs& S = A.stream[w.shared];
+      return static_cast<int64_t>(page) << A.page_shift < w.len ? __ldg(S.pages + static_cast<int64_t>(w.row) * S.max_pages + page) : -1;
+    };
+    const auto look = [&](Ahead& x) {
+      x.has = find(x.w);
+      if (!x.has) return;
+      x.batch = x.w.first * per_tile;
+      x.ids = ask(x.w, x.batch), x.next_ids = ask(x.w, x.batch + 32);
+    };
+    Ahead now{}, then{};      // the unit at hand, and the next one, whose page ids are on their way
+    look(now);
+    if (now.has) look(then);
+    bool stopped = false, described = false;
     uint32_t n_units = 0;      // described
-    bool described = false;
     int tile = 0;              // of the unit, next to be fetched
     uint32_t k_next = 0, v_next = 0;
-    int32_t ids = 0, next_ids = 0, batch = 0;      // page ids, one per lane, from page `batch` of the unit's row on
-    const int per_tile = kKeys >> A.page_shift;
-    const auto ask = [&](int from) -> int32_t {
-      const int page = from + lane;
-      return static_cast<int64_t>(page) << A.page_shift < w.len ? __ldg(A.stream[w.shared].pages + static_cast<int64_t>(w.row) * A.stream[w.shared].max_pages + page) : -1;
-    };
     constexpr int kHalves = D / 64;
     const int half = lane % kHalves, page_of_tile = lane / kHalves;
     const auto copy = [&](const Meta& m, int which, uint32_t dst, uint64_t* bar) {
@@ -433,28 +472,24 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         if (n_units < kUnits || __all_sync(0xffffffffu, mbar_test_wait(&C.empty[slot], (n_units / kUnits - 1) & 1u))) {
           if (lane == 0) {
             Unit& d = C.units[slot];
-            d = w;
-            if (!has) d.tiles = 0;
+            d = now.w;
+            if (!now.has) d.tiles = 0;
             mbar_arrive(&C.full[slot]);
           }
           __syncwarp();
           ++n_units;
           progress = true;
-          if (!has) {
-            stopped = true;
-          } else {
-            described = true, tile = 0;
-            batch = w.first * per_tile;
-            ids = ask(batch), next_ids = ask(batch + 32);
-          }
+          if (now.has) described = true, tile = 0;
+          else stopped = true;
         }
       }
       if (described) {
-        const uint32_t i = k_next % Z::kK;
-        if (k_next < Z::kK || __all_sync(0xffffffffu, mbar_test_wait(&C.k_free[i], (k_next / Z::kK - 1) & 1u))) {
+        const uint32_t i = k_next % Z::kRing;
+        if (k_next < Z::kRing || __all_sync(0xffffffffu, mbar_test_wait(kLong ? &C.k_free[i] : &C.s[i], (k_next / Z::kRing - 1) & 1u))) {
+          const Unit& w = now.w;
           const int t = w.first + tile, page0 = t * per_tile;
-          if (page0 - batch >= 32) batch += 32, ids = next_ids, next_ids = ask(batch + 32);
-          const int32_t id = __shfl_sync(0xffffffffu, ids, min(31, page0 - batch + page_of_tile));
+          if (page0 - now.batch >= 32) now.batch += 32, now.ids = now.next_ids, now.next_ids = ask(w, now.batch + 32);
+          const int32_t id = __shfl_sync(0xffffffffu, now.ids, min(31, page0 - now.batch + page_of_tile));
           const bool exists = page_of_tile < per_tile && static_cast<int64_t>(page0 + page_of_tile) << A.page_shift < w.len;
           const bool there = exists && static_cast<uint32_t>(id) < static_cast<uint32_t>(A.stream[w.shared].n_pages);
           if (exists && !there) report(A, QC_ERR_BAD_PAGE);
@@ -470,12 +505,16 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
           copy(m, 0, sK + i * Z::kTile, &C.k[i]);
           ++k_next;
           progress = true;
-          if (++tile == w.tiles) described = false, has = find(w);
+          if (++tile == w.tiles) {
+            described = false;
+            now = then;
+            if (now.has) look(then);
+          }
         }
       }
       if (v_next < k_next) {
-        const uint32_t i = v_next % Z::kV;
-        if (v_next < Z::kV || __all_sync(0xffffffffu, mbar_test_wait(&C.v_free[i], (v_next / Z::kV - 1) & 1u))) {
+        const uint32_t i = v_next % Z::kRing;
+        if (v_next < Z::kRing || __all_sync(0xffffffffu, mbar_test_wait(kLong ? &C.v_free[i] : &C.o[i], (v_next / Z::kRing - 1) & 1u))) {
           copy(C.meta[v_next % kMeta], 1, sV + i * Z::kTile, &C.v[i]);
           ++v_next;
           progress = true;
@@ -510,16 +549,16 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
     const uint64_t qd = umma_desc(sQ, 16, 1024);
     uint32_t s_next = 0, o_next = 0;      // tiles
     const auto issue_scores = [&]() {
-      const uint32_t b = s_next & 1u, i = s_next % Z::kK;
+      const uint32_t b = s_next & 1u, i = s_next % Z::kRing;
       // the buffer holds the weights of the tile before the last one until their products are done (products with different sums are
       // not documented to run in the order of their issue)
       if (s_next >= 2) wait_on(&C.o[b], (s_next / 2 - 1) & 1u);
-      wait_on(&C.k[i], (s_next / Z::kK) & 1u);
+      wait_on(&C.k[i], (s_next / Z::kRing) & 1u);
       if (!ok) return;
       tc5_fence_after();
       scores<D>(tmem + kScoresAt + b * kKeys, qd, umma_desc(sK + i * Z::kTile, 16, 1024), kIdescS);
       umma_commit(&C.s[b]);
-      umma_commit(&C.k_free[i]);
+      if (kLong) umma_commit(&C.k_free[i]);
       ++s_next;
     };
     for (uint32_t n = 0; ok; ++n) {
@@ -531,14 +570,14 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       wait_on(&C.q, n & 1u);
       for (int t = 0; t < 2 && t < tiles && ok; ++t) issue_scores();
       for (int t = 0; t < tiles && ok; ++t) {
-        const uint32_t b = o_next & 1u, i = o_next % Z::kV;
+        const uint32_t b = o_next & 1u, i = o_next % Z::kRing;
         wait_on(&C.p[b], (o_next / 2) & 1u);
-        wait_on(&C.v[i], (o_next / Z::kV) & 1u);
+        wait_on(&C.v[i], (o_next / Z::kRing) & 1u);
         if (!ok) break;
         tc5_fence_after();
         umma_values(tmem + kOutAt, tmem + kScoresAt + b * kKeys, umma_desc(sV + i * Z::kTile, Z::kHalf, 1024), kIdescO, t > 0 ? 1u : 0u);
         umma_commit(&C.o[b]);
-        umma_commit(&C.v_free[i]);
+        if (kLong) umma_commit(&C.v_free[i]);
         ++o_next;
         if (t + 2 < tiles) issue_scores();
       }
@@ -546,8 +585,8 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       if (lane == 0) mbar_arrive(&C.empty[slot]);
     }
     // (nothing arrives behind the block's end)
-    if (s_next) wait_on(&C.k_free[(s_next - 1) % Z::kK], ((s_next - 1) / Z::kK) & 1u);
-    if (o_next) wait_on(&C.v_free[(o_next - 1) % Z::kV], ((o_next - 1) / Z::kV) & 1u);
+    if (kLong && s_next) wait_on(&C.k_free[(s_next - 1) % Z::kRing], ((s_next - 1) / Z::kRing) & 1u);
+    if (kLong && o_next) wait_on(&C.v_free[(o_next - 1) % Z::kRing], ((o_next - 1) / Z::kRing) & 1u);
     if (!ok) failed = 1;
     __syncwarp();
   } else if (works) {
@@ -567,48 +606,49 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       }
     };
     uint32_t t0 = 0;      // tiles of the units before
-    // a unit as this thread sees it: its row (of n_here, held `copies` times), the row's query
+    // rows of a unit are its first query's heads from head0 on, then the next query's
+    const auto query_of = [&](const Unit& u, int row) { return static_cast<int>((static_cast<float>(u.head0 + row) + 0.5f) * A.inv_group); };
+    // a unit as this thread sees it: its row, of n_here that are held `copies` times
     struct Mine {
-      Unit u;
+      int n_here, tiles, first, len, all_see, shared;
       int copies, row, copy, seen;
-      int64_t token;
-      int head;
       bool real;
     };
     const auto take = [&](uint32_t n, Mine& x) {
-      wait_on(&C.full[n % kUnits], (n / kUnits) & 1u);
-      if (!ok) return;
-      x.u = C.units[n % kUnits];
-      x.copies = x.u.n_here <= 32 ? 4 : x.u.n_here <= 64 ? 2 : 1;
-      const int each = kRows / x.copies;
-      x.copy = static_cast<int>(threadIdx.x) / each, x.row = static_cast<int>(threadIdx.x) - x.copy * each;
-      x.real = x.row < x.u.n_here;
-      const int flat = static_cast<int>(x.u.row0 % A.group) + x.row, more = flat / A.group;      // (32 bits: the row inside its query's heads)
-      const int64_t query = x.u.row0 / A.group + more;
-      x.head = x.u.kvh * A.group + flat - more * A.group;
-      x.token = x.u.token0 + query;
-      x.seen = x.u.shared || !A.causal ? x.u.len : max(0, x.u.len - (x.u.queries - 1 - static_cast<int>(query)));
+      const Unit& u = C.units[n % kUnits];
+      x.n_here = u.n_here, x.tiles = u.tiles, x.first = u.first, x.len = u.len, x.all_see = u.all_see, x.shared = u.shared;
+      x.copies = copies_of(x.n_here);
+      x.copy = threadIdx.x >> (x.copies == 4 ? 5 : x.copies == 2 ? 6 : 7), x.row = threadIdx.x & (x.copies == 4 ? 31 : x.copies == 2 ? 63 : 127);
+      x.real = x.row < x.n_here;
+      x.seen = x.shared || !A.causal ? x.len : max(0, x.len - (u.queries - 1 - u.query0 - query_of(u, x.row)));
     };
-    uint4 q[D / 8];
-    const auto ask_query = [&](const Mine& x) {
-      const StreamArgs& S = A.stream[x.u.shared];
-      const uint4* p = reinterpret_cast<const uint4*>(S.q + x.token * S.q_stride + static_cast<int64_t>(x.head) * D);
+    // the unit's queries, from their places straight into shared memory; rows that are none keep what was there
+    const auto ask_query = [&](uint32_t n) {
+      const Unit& u = C.units[n % kUnits];
+      const int copies = copies_of(u.n_here), row = threadIdx.x & (kRows / copies - 1), query = query_of(u, row);
+      const StreamArgs& S = A.stream[u.shared];
+      const uint16_t* p = S.q + (u.token0 + query) * S.q_stride + static_cast<int64_t>(u.kvh * A.group + u.head0 + row - query * A.group) * D;
+      if (row < u.n_here) {
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) q[i] = x.real ? __ldg(p + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D / 8; ++i)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sQ + (i >> 3) * Z::kQHalf + threadIdx.x * 128 + (((i & 7) ^ (threadIdx.x & 7)) << 4)), "l"(p + i * 8) : "memory");
+      }
     };
     const auto put_query = [&]() {
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) sts128(sQ + (i >> 3) * Z::kQHalf + threadIdx.x * 128 + (((i & 7) ^ (threadIdx.x & 7)) << 4), q[i]);
+      cp_async_wait_all();
       fence_proxy_async();
       mbar_arrive(&C.q);
     };
     Mine x;
-    take(0, x);
-    if (ok && x.u.tiles) ask_query(x), put_query();
+    wait_on(&C.full[0], 0u);
+    if (ok && C.units[0].tiles) ask_query(0), put_query();
     for (uint32_t n = 0;; ++n) {
-      if (!rows_all(ok) || x.u.tiles == 0) break;
+      if (!rows_all(ok)) break;
+      take(n, x);
+      if (x.tiles == 0) break;
       float ref = -INFINITY, sum = 0.f;
-      const bool idle = x.copies == 1 && warp * 32 >= x.u.n_here;      // a warp without rows
+      bool more = false;      // units
+      const bool idle = x.copies == 1 && warp * 32 >= x.n_here;      // a warp without rows
       const auto weigh = [&](auto tag, int t, uint32_t gt, uint32_t on, bool masked) {
         constexpr int REP = decltype(tag)::value, N = kKeys / REP;
         const uint32_t at = t_row + kScoresAt + (gt & 1u) * kKeys;
@@ -683,23 +723,29 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         tmem_st32(at, w);
         tmem_wait_st();
       };
-      for (int i = 0; i < x.u.tiles && ok; ++i) {
+      for (int i = 0; i < x.tiles && ok; ++i) {
         const uint32_t gt = t0 + i;
-        const int t = x.u.first + i;
+        const int t = x.first + i;
         wait_on(&C.s[gt & 1u], (gt / 2) & 1u);
         if (!ok) break;
         tc5_fence_after();
+        if (i + 1 == x.tiles) {      // the queries have been read for the last time: the next unit's are on their way while this one ends
+          wait_on(&C.full[(n + 1) % kUnits], ((n + 1) / kUnits) & 1u);
+          if (!ok) break;
+          more = C.units[(n + 1) % kUnits].tiles != 0;
+          if (more) ask_query(n + 1);
+        }
         const uint32_t on = *reinterpret_cast<volatile int32_t*>(&C.meta[gt % kMeta].on);
-        const int left = x.u.len - t * kKeys;
+        const int left = x.len - t * kKeys;
         if (!idle) {
-          const bool masked = on != 15u || (t + 1) * kKeys > x.u.all_see;
+          const bool masked = on != 15u || (t + 1) * kKeys > x.all_see;
           if (x.copies == 4) weigh(std::integral_constant<int, 4>{}, t, gt, on, masked);
           else if (x.copies == 2) weigh(std::integral_constant<int, 2>{}, t, gt, on, masked);
           else weigh(std::integral_constant<int, 1>{}, t, gt, on, masked);
         }
         if (on != 15u || left < kKeys) {      // values that no token has may be anything: a weight of 0 does not cancel a NaN
-          const uint32_t v = gt % Z::kV;
-          wait_on(&C.v[v], (gt / Z::kV) & 1u);
+          const uint32_t v = gt % Z::kRing;
+          wait_on(&C.v[v], (gt / Z::kRing) & 1u);
           const int key = threadIdx.x & 63, h = threadIdx.x >> 6;
           if (ok && h < D / 64 && (key >= left || !(on >> (key / 16) & 1u))) {
 #pragma unroll
@@ -711,10 +757,8 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         tc5_fence_before();
         mbar_arrive(&C.p[gt & 1u]);
       }
-      t0 += x.u.tiles;
-      Mine next;
-      if (ok) take(n + 1, next);
-      if (ok && next.u.tiles) ask_query(next);      // on their way while this unit ends
+      t0 += x.tiles;
+      if (more) put_query();
       wait_on(&C.o[(t0 - 1) & 1u], ((t0 - 1) / 2) & 1u);
       if (!rows_all(ok)) {
         ok = false;
@@ -723,34 +767,21 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       tc5_fence_after();
 
       // ---- the unit's rows: to their queries' places, or as a piece
-      const size_t heads = static_cast<size_t>(A.n_tokens) * A.hq;
-      const auto to_of = [&](int row, int64_t token, int head) -> float* {
-        return x.u.place < 0 ? A.rows + (x.u.shared * heads + token * A.hq + head) * D : A.pieces + static_cast<size_t>(x.u.place) * (kRows * (D + 2)) + row * D;
+      const Unit& u = C.units[n % kUnits];
+      const size_t rows0 = static_cast<size_t>(u.shared) * A.n_tokens;
+      const auto place_of = [&](int row) -> size_t {      // of whole units
+        const int query = query_of(u, row);
+        return (rows0 + u.token0 + query) * A.hq + u.kvh * A.group + u.head0 + row - query * A.group;
       };
-      const auto ml_of = [&](int row, int64_t token, int head) -> float2* {
-        return x.u.place < 0 ? A.row_ml + x.u.shared * heads + token * A.hq + head
-                             : reinterpret_cast<float2*>(A.pieces + static_cast<size_t>(x.u.place) * (kRows * (D + 2)) + kRows * D) + row;
-      };
-      float2* const ml = reinterpret_cast<float2*>(smem);      // [128], where the queries were: every product has read them
-      if (threadIdx.x < 4) C.redo[threadIdx.x] = 0;
-      // (the second half of the queries' place: the copies' sums)
-      if (x.copies > 1) ml[threadIdx.x] = make_float2(ref, sum);
-      rows_barrier();
-      float factor = 1.f, top = ref, all = sum;
-      if (x.copies > 1) {
-        const int each = kRows / x.copies;
-        top = -INFINITY, all = 0.f;
-        for (int c = 0; c < x.copies; ++c) top = fmaxf(top, ml[c * each + x.row].x);
-        for (int c = 0; c < x.copies; ++c) {
-          const float2 y = ml[c * each + x.row];
-          if (y.y != 0.f) all = fmaf(y.y, y.x == -INFINITY ? 1.f : ex2_approx(y.x - top), all);      // (a sum on no reference is no number)
-        }
-        factor = sum == 0.f ? 0.f : ref == -INFINITY ? 1.f : ex2_approx(ref - top);
-      }
-      bool strange = false;      // a sum that is no finite number although the row's weights are numbers
+      float* const piece = A.pieces + static_cast<size_t>(u.place) * (kRows * (D + 2));
+      const auto sums_of = [&](int row) -> float* { return u.place < 0 ? A.rows + place_of(row) * D : piece + row * D; };
+      const auto ml_of = [&](int row) -> float2* { return u.place < 0 ? A.row_ml + place_of(row) : reinterpret_cast<float2*>(piece + kRows * D) + row; };
+      bool strange = false;      // a sum that is no finite number although its row's weights are numbers
+      const auto flag = [&](int row) { atomicOr(&C.redo[row >> 5], 1u << (row & 31)), strange = true; };
       if (x.copies == 1) {
-        float* const to = to_of(x.row, x.token, x.head);
+        bool found = false;
         if (!idle) {
+          float* const to = sums_of(x.real ? x.row : 0);
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             uint32_t r[32];
@@ -758,71 +789,86 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
             uint32_t most = 0;
 #pragma unroll
             for (int j = 0; j < 32; ++j) most = max(most, r[j] & 0x7fffffffu);
-            strange |= most >= 0x7f800000u;
+            found |= most >= 0x7f800000u;
             if (x.real)
 #pragma unroll
-              for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j, 1.f);
+              for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j);
           }
+          if (x.real) *ml_of(x.row) = make_float2(ref, sum);
         }
-        if (x.real) *ml_of(x.row, x.token, x.head) = make_float2(ref, sum);
+        if (found && x.real && isfinite(sum)) flag(x.row);
       } else {
-        // D / 2 elements of all rows at a time through the queries' place
-        constexpr int kRound = D / 2, kChunks = kRound / 4;
-        rows_barrier();      // (the references have been read)
+        // The copies' sums meet in shared memory: whole rows, halves or quarters of all rows at a time, as they fit.
+        float2* const refs = reinterpret_cast<float2*>(smem + Z::kRefs);      // [copies][n_here]
+        const int held = x.copies * x.n_here, mine = x.copy * x.n_here + x.row;
+        if (x.real) refs[mine] = make_float2(ref, sum);
+        const auto meet = [&](auto cols_tag, auto copies_tag, int c0) {
+          constexpr int kCols = decltype(cols_tag)::value, kChunks = kCols / 4, kStep = kCols < 64 ? kCols : 64, kCopies = decltype(copies_tag)::value;
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += kRound) {
-#pragma unroll 1
-          for (int c = 0; c < kRound; c += 32) {
-            uint32_t r[32];
-            tmem_ld32(t_row + kOutAt + c0 + c, r);
-            uint32_t most = 0;
+          for (int c = 0; c < kCols; c += kStep) {
+            uint32_t r[kStep / 32][32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) most = max(most, r[j] & 0x7fffffffu);
-            strange |= most >= 0x7f800000u;
+            for (int i = 0; i < kStep / 32; ++i) tmem_ld32_nowait(t_row + kOutAt + c0 + c + i * 32, r[i]);
+            tmem_wait_ld();
             if (x.real) {
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const auto part = [&](int e) { return factor == 0.f ? 0u : __float_as_uint(__uint_as_float(r[4 * j + e]) * factor); };
-                sts128(sQ + threadIdx.x * (kRound * 4) + (((c / 4 + j) ^ (threadIdx.x & 7)) << 4), make_uint4(part(0), part(1), part(2), part(3)));
+              for (int j = 0; j < kStep / 4; ++j)
+                sts128(sStage + mine * (kCols * 4) + (((c / 4 + j) ^ (mine & 7)) << 4), make_uint4(r[j / 8][j % 8 * 4], r[j / 8][j % 8 * 4 + 1], r[j / 8][j % 8 * 4 + 2], r[j / 8][j % 8 * 4 + 3]));
+            }
+          }
+          rows_barrier();
+          for (int i = threadIdx.x; i < x.n_here * kChunks; i += kRows) {
+            const int row = i / kChunks, chunk = i % kChunks;
+            float2 z[kCopies];
+            uint4 v[kCopies];
+            float top = -INFINITY, all = 0.f;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const int at = k * x.n_here + row;
+              z[k] = refs[at], v[k] = lds128(sStage + at * (kCols * 4) + ((chunk ^ (at & 7)) << 4));
+              top = fmaxf(top, z[k].x);
+            }
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const float f = z[k].x == -INFINITY ? 1.f : ex2_approx(z[k].x - top);      // (a sum on no reference is no number)
+              if (z[k].y != 0.f) {
+                all = fmaf(z[k].y, f, all);
+                y.x = fmaf(__uint_as_float(v[k].x), f, y.x), y.y = fmaf(__uint_as_float(v[k].y), f, y.y);
+                y.z = fmaf(__uint_as_float(v[k].z), f, y.z), y.w = fmaf(__uint_as_float(v[k].w), f, y.w);
               }
             }
+            reinterpret_cast<float4*>(sums_of(row) + c0)[chunk] = y;
+            if (c0 + chunk == 0) *ml_of(row) = make_float2(top, all);
+            if (!(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w)) && isfinite(all)) flag(row);
           }
-          rows_barrier();
-          const int each = kRows / x.copies;
-          for (int i = threadIdx.x; i < x.u.n_here * kChunks; i += kRows) {
-            const int row = i / kChunks, chunk = i - row * kChunks;
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = 0; c < x.copies; ++c) {
-              const int from = c * each + row;
-              const uint4 z = lds128(sQ + from * (kRound * 4) + ((chunk ^ (from & 7)) << 4));
-              y.x += __uint_as_float(z.x), y.y += __uint_as_float(z.y), y.z += __uint_as_float(z.z), y.w += __uint_as_float(z.w);
+        };
+        const auto meet_all = [&](auto copies_tag) {
+          if (held * D * 4 <= static_cast<int>(Z::kStageBytes)) {
+            meet(std::integral_constant<int, D>{}, copies_tag, 0);
+          } else {
+#pragma unroll 1
+            for (int c = 0; c < D; c += 32) {
+              if (c) rows_barrier();      // (what was there has been read)
+              meet(std::integral_constant<int, 32>{}, copies_tag, c);
             }
-            const int flat = static_cast<int>(x.u.row0 % A.group) + row, more = flat / A.group;
-            float* const to = to_of(row, x.u.token0 + x.u.row0 / A.group + more, x.u.kvh * A.group + flat - more * A.group);
-            reinterpret_cast<float4*>(to + c0)[chunk] = y;
           }
-          rows_barrier();
-        }
-        if (x.real && x.copy == 0) *ml_of(x.row, x.token, x.head) = make_float2(top, all);
+        };
+        if (x.copies == 4) meet_all(std::integral_constant<int, 4>{});
+        else meet_all(std::integral_constant<int, 2>{});
       }
-      if (strange && x.real && isfinite(all)) atomicOr(&C.redo[x.row >> 5], 1u << (x.row & 31));
-      rows_barrier();
-      if (C.redo[0] | C.redo[1] | C.redo[2] | C.redo[3]) {      // rare: rows whose sums a value behind a weight of 0 may have spoiled, by hand
-        for (int row = warp; row < x.u.n_here; row += 4) {
+      if (rows_any(strange)) {      // rare: rows whose sums a value behind a weight of 0 may have spoiled, by hand
+        for (int row = warp; row < x.n_here; row += 4) {
           if (!(C.redo[row >> 5] >> (row & 31) & 1u)) continue;
-          const int flat = static_cast<int>(x.u.row0 % A.group) + row, more = flat / A.group;
-          const int64_t query = x.u.row0 / A.group + more, token = x.u.token0 + query;
-          const int head = x.u.kvh * A.group + flat - more * A.group;
-          const int seen = x.u.shared || !A.causal ? x.u.len : max(0, x.u.len - (x.u.queries - 1 - static_cast<int>(query)));
-          sweep<D>(A, A.stream[x.u.shared], x.u.row, x.u.kvh, token, head, x.u.first * kKeys, min(seen, (x.u.first + x.u.tiles) * kKeys), to_of(row, token, head),
-                   ml_of(row, token, head), &C.beat, lane);
+          const int query = query_of(u, row), head = u.kvh * A.group + u.head0 + row - query * A.group;
+          const int seen = x.shared || !A.causal ? x.len : max(0, x.len - (u.queries - 1 - u.query0 - query));
+          sweep<D>(A, A.stream[x.shared], u.row, u.kvh, u.token0 + query, head, x.first * kKeys, min(seen, (x.first + x.tiles) * kKeys), sums_of(row), ml_of(row), &C.beat, lane);
         }
         rows_barrier();
+        if (threadIdx.x < 4) C.redo[threadIdx.x] = 0;
       }
       tc5_fence_before();
       mbar_arrive(&C.empty[n % kUnits]);
-      x = next;
-      if (x.u.tiles) put_query();
     }
     if (!ok) failed = 1;
   }
@@ -859,7 +905,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
       const int64_t flat = (token - u.token0) * A.group + head - kvh * A.group;
       const uint32_t per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
       const uint32_t tiles_at = u.base + (kvh * per_head + static_cast<uint32_t>(flat / kRows)) * unit_cost(u.tiles) + kUnitCost;
-      const uint32_t first = worker_at(plan.cost, plan.workers, tiles_at), last = worker_at(plan.cost, plan.workers, tiles_at + (u.tiles - 1) * kTileCost);
+      const uint32_t first = worker_at(plan, tiles_at), last = worker_at(plan, tiles_at + (u.tiles - 1) * kTileCost);
       const int row = static_cast<int>(flat % kRows);
       const auto part = [&](uint32_t w) -> const float* {
         return first == last ? A.rows + (kind * heads + at) * D : A.pieces + (static_cast<size_t>(w) * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + row * D;
@@ -1039,7 +1085,7 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   A.page_shift = A.page == 16 ? 4 : A.page == 32 ? 5 : 6;
   A.n_seqs = args->n_seqs, A.n_groups = args->n_groups, A.n_tokens = args->n_tokens, A.max_queries = args->max_queries, A.causal = args->causal != 0;
   const float scale = args->softmax_scale > 0.f ? args->softmax_scale : 1.0f / sqrtf(static_cast<float>(args->head_dim));
-  A.scale_log2 = scale * 1.4426950408889634f;
+  A.scale_log2 = scale * 1.4426950408889634f, A.inv_group = 1.f / A.group;
   DeviceGuard guard(device);
   if (!guard.ok()) return QC_ERR_CUDA;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
