@@ -33,8 +33,10 @@ constexpr int kUnits = 4;        // units that are known to the block at a time
 constexpr int kMeta = 8;         // tiles whose places are
 constexpr uint32_t kScoresAt = 0, kOutAt = 128, kColumns = 256;   // tensor memory: two score buffers of 64 columns, D of the sums
 constexpr float kRescale = 8.f;  // the reference of a row moves when its scores have grown by 2^8
-constexpr uint32_t kUnitCost = 2, kTileCost = 1;
+constexpr uint32_t kUnitCost = 2;
+constexpr uint32_t kApart = 32, kLeastPiece = 4, kPieceShare = 4;
 constexpr uint32_t kMostCost = 1u << 27;
+constexpr int kSlim = 8;         // rows of a unit that four threads each hold in every warp
 constexpr int kMostHeld = 2048;  // items that a block keeps in shared memory while it looks for its range
 
 struct StreamArgs {
@@ -55,14 +57,19 @@ struct Record {
   int32_t spare[3];
 };
 
-// Whether the batch is computed, and its ranges: the first `longer` workers have costs of `per` + 1, the others `per`.
+// A row of costs, cut into ranges: the first `longer` workers have `per` + 1, the others `per`.
+struct Line {
+  uint32_t begin, per, longer, workers;
+  int32_t least;           // tiles of a piece
+};
+// Whether the batch is computed, and its rows of costs: prefixes and sequences in one, or in one each.
 struct Plan {
-  int32_t fine;
-  uint32_t per, longer, spare;
+  Line line[2];
+  int32_t fine, lines;
 };
 
 struct AttendArgs {
-  CUtensorMap map[2][2];  // K and V of own and shared pages, as rows of 64 elements, a page's tokens of a head at a time
+  CUtensorMap map[2][2];  // K and V of own and shared pages: a copy brings a page's tokens of a head, 64 elements of K or all of V
   StreamArgs stream[2];   // own, shared
   const int32_t* ids;
   const int32_t* starts;
@@ -74,7 +81,7 @@ struct AttendArgs {
   Record* records;        // [groups + sequences]
   float* rows;            // [kinds][tokens * heads][D] sums of whole units
   float2* row_ml;         // [kinds][tokens * heads]
-  float* pieces;          // [workers][2][128 * (D + 2)]
+  float* pieces;          // [workers][lines][2][128 * (D + 2)]
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, n_groups, n_tokens, max_queries, causal;
@@ -137,15 +144,26 @@ __device__ __forceinline__ Item item_of(const AttendArgs& A, int i, bool tell) {
   count_units(A, u);
   return u;
 }
-__device__ __forceinline__ uint32_t unit_cost(int tiles) { return kUnitCost + tiles * kTileCost; }
+__device__ __forceinline__ uint32_t unit_cost(int tiles) { return kUnitCost + tiles; }
 // kMostCost + 1: too much
 __device__ __forceinline__ uint32_t cost_of(const Item& u) {
   return static_cast<uint32_t>(min(static_cast<uint64_t>(u.units) * unit_cost(u.tiles), static_cast<uint64_t>(kMostCost) + 1));
 }
 
 // Every range is as long as a tile at least.
-__device__ __forceinline__ uint32_t range_begin(const Plan& p, uint32_t w) { return w * p.per + min(w, p.longer); }
-__device__ __forceinline__ uint32_t worker_at(const Plan& p, uint32_t at) {
+__device__ __forceinline__ Line line_of(uint32_t begin, uint32_t cost, uint32_t most) {
+  const uint32_t workers = max(1u, min(most, cost));
+  const uint32_t per = cost / workers;
+  return Line{begin, per, cost % workers, workers, static_cast<int32_t>(max(1u, min(kLeastPiece, per / kPieceShare)))};
+}
+// Where a border at tile t of a unit is: never so near to its first or last tile that a piece would hardly be worth its start.
+__device__ __forceinline__ int border(int least, int t, int tiles) {
+  if (tiles < 2 * least) return t <= tiles / 2 ? 0 : tiles;
+  return t < least ? 0 : t > tiles - least ? tiles : t;
+}
+__device__ __forceinline__ uint32_t range_begin(const Line& p, uint32_t w) { return p.begin + w * p.per + min(w, p.longer); }
+__device__ __forceinline__ uint32_t worker_at(const Line& p, uint32_t at) {
+  at -= p.begin;
   const uint32_t turn = p.longer * (p.per + 1);
   return at < turn ? at / (p.per + 1) : p.longer + (at - turn) / p.per;
 }
@@ -156,23 +174,24 @@ struct Unit {
   int32_t query0, queries;       // the query of its first row among the item's
   int32_t n_here, kvh, shared, row, first, tiles, len;
   int32_t all_see;               // keys that every row sees
-  int32_t place;                 // of a piece: worker * 2, + 1 where the unit begins in the range; -1: the unit is whole
+  int32_t place;                 // of a piece: worker * 4 + line * 2, + 1 where the unit begins in the range; -1: the unit is whole
 };
 
-// How often a unit's rows are held: at blocks of 32 or 64 rows, where the copies' sums fit the place where they meet.
+// How often a unit's rows are held, every 32, 64 or 128 rows: as often as the copies' sums, 32 elements at a time, fit the place where
+// they meet.
 __device__ __forceinline__ int copies_of(int n_here) { return n_here <= 30 ? 4 : n_here <= 60 ? 2 : 1; }
 
 struct Meta {
   int32_t y[4];                  // of a tile's pages: the first row in the pool, -1: the page is not there
   int32_t on, shared;            // blocks of 16 keys that are there
-  int32_t spare[2];
 };
 
 template <int D>
 struct Shape {
   static constexpr int kRing = D == 128 ? 2 : 4;      // tiles of K, and of V, under way
   static constexpr uint32_t kTile = kKeys * D * 2, kHalf = kKeys * 128, kQ = kRows * D * 2, kQHalf = kRows * 128;
-  static constexpr uint32_t kStage = kQ + 2 * kRing * kTile, kStageBytes = 15360, kRefs = kStage + kStageBytes;      // where the copies' sums meet, and their references
+  // where the copies' sums meet, their references behind them
+  static constexpr uint32_t kMeet = kQ + 2 * kRing * kTile, kMeetBytes = 15616, kRefs = kMeet + kMeetBytes;
   static constexpr uint32_t kTiles = kRefs + kRows * 8;
 };
 
@@ -184,8 +203,20 @@ struct Control {
   uint32_t tmem, beat, redo[4];
   int32_t failed;
 };
-static_assert(sizeof(Control) <= 1024, "two blocks and their tiles are all of an SM's shared memory");
+static_assert(2 * (Shape<128>::kTiles + sizeof(Control) + 1024) <= 228 * 1024, "two blocks share an SM");
 
+// O (+)= P V for one tile: a product for 16 keys, the weights 8 columns of tensor memory and the values at b0 .. b3.
+__device__ __forceinline__ void values(uint32_t tmem_d, uint32_t tmem_p, uint64_t b0, uint64_t b1, uint64_t b2, uint64_t b3, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred e, pa, po;\n\t.reg .b32 ta;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 pa, %7, 0;\n\tsetp.eq.b32 po, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %6, pa;\n\t"
+      "add.u32 ta, %1, 8;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], %3, %6, po;\n\t"
+      "add.u32 ta, %1, 16;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], %4, %6, po;\n\t"
+      "add.u32 ta, %1, 24;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [ta], %5, %6, po;\n\t}" ::"r"(tmem_d),
+      "r"(tmem_p), "l"(b0), "l"(b1), "l"(b2), "l"(b3), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 template <int D>
 __device__ __forceinline__ void scores(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc) {
   if constexpr (D == 128) {
@@ -211,9 +242,29 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
                  "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                : "r"(taddr));
 }
+// Rows 0-15 of a warp's lanes, a row shared out among four threads: 8 columns at a time, thread l has columns 2 (l % 4) and the next one of row
+// l / 4 (registers 0 and 1) and of the row 8 below (2 and 3); or 4 columns at a time, column l % 4 of row l / 4 and of the row 8 below.
+__device__ __forceinline__ void tmem_ld_quads16(uint32_t taddr, uint32_t (&r)[8]) {      // 16 columns
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_quads64(uint32_t taddr, uint32_t (&r)[32]) {      // 64 columns
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st_quads64(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_fours32(uint32_t taddr, const uint32_t (&r)[16]) {      // 32 columns
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Whether all rows' threads say so, and whether any does.  Rows' warps go on together or not at all, so that none waits at a barrier for
+// Whether all rows' threads say so.  Rows' warps go on together or not at all, so that none waits at a barrier for
 // one that has given up.
 __device__ __forceinline__ bool rows_all(bool x) {
   uint32_t all;
@@ -289,7 +340,7 @@ template <int D>
 __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_constant__ AttendArgs A) {
   using Z = Shape<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kRing * Z::kTile, sStage = sQ + Z::kStage;
+  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kRing * Z::kTile, sMeet = sQ + Z::kMeet;
   Control& C = *reinterpret_cast<Control*>(smem + Z::kTiles);
   volatile int32_t& failed = C.failed;
   constexpr bool kLong = Z::kRing > 2;      // rings of two are free when the score buffer, or its weights, are
@@ -370,14 +421,21 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
   }
   fine = __syncthreads_and(fine);
   const bool few = total <= kMostCost;
-  const uint32_t workers = max(1u, min(gridDim.x, total / kTileCost));
-  const Plan plan{fine && few, total / workers, total % workers, 0};
+  // Prefixes and sequences apart where every block has some of both
+  const uint32_t cut = A.n_groups < n_items ? before[A.n_groups] : total;
+  Plan plan{{}, fine && few, 1};
+  if (cut >= kApart * gridDim.x && total - cut >= kApart / 4 * gridDim.x) {
+    plan.lines = 2;
+    plan.line[0] = line_of(0, cut, gridDim.x), plan.line[1] = line_of(cut, total - cut, gridDim.x);
+  } else {
+    plan.line[0] = line_of(0, total, gridDim.x);
+  }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     *A.plan = plan;
     if (!fine) report(A, QC_ERR_INVALID_ARG);
     else if (!few) report(A, QC_ERR_PLAN);
   }
-  const bool works = plan.fine && total && blockIdx.x < workers;
+  const bool works = plan.fine && total && (blockIdx.x < plan.line[0].workers || (plan.lines == 2 && blockIdx.x < plan.line[1].workers));
   tc5_fence_before();
   __syncthreads();
   tc5_fence_after();
@@ -385,49 +443,85 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
 
   if (works && warp == 5) {
     // ------------------------------------------------------------------ units and tiles
-    uint32_t at = range_begin(plan, blockIdx.x), item_at;
-    const uint32_t end = range_begin(plan, blockIdx.x + 1);
-    int item;
-    Item u, u_next{};
-    {
+    // The block's ranges: of one row of costs, or of both; the second half of the blocks, which share their SMs with the first, begin with
+    // the sequences', so that prefixes' products and sequences' copies go side by side.
+    struct Range {
+      uint32_t at, end, item_at, begin;
+      int item, line, least;
+    };
+    const auto range_of = [&](int line) -> Range {
+      Range r{};
+      const Line p = line ? plan.line[1] : plan.line[0];
+      r.line = line, r.least = p.least;
+      if (blockIdx.x >= p.workers) return r;
+      r.at = r.begin = range_begin(p, blockIdx.x), r.end = range_begin(p, blockIdx.x + 1);
       int lo = 0, hi = n_items - 1;      // the last item that begins at or before the range
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (before[mid] <= at) lo = mid;
+        if (before[mid] <= r.at) lo = mid;
         else hi = mid - 1;
       }
-      item = lo, item_at = before[lo];
-      u = holds ? item_from(A, held[item]) : item_of(A, item, false);
-      if (item + 1 < n_items) u_next = holds ? item_from(A, held[item + 1]) : item_of(A, item + 1, false);
-    }
+      r.item = lo, r.item_at = before[lo];
+      return r;
+    };
+    const int begins_with = plan.lines == 2 && blockIdx.x >= gridDim.x / 2 ? 1 : 0;
+    Range range = range_of(begins_with), other{};
+    if (plan.lines == 2) other = range_of(1 - begins_with);
+    if (range.at >= range.end) range = other, other = Range{};
+    // 32 items, one per lane, from `first_held` on
+    Held mine{};
+    int first_held = range.item;
+    const auto hold = [&](int from) {
+      first_held = from;
+      if (from + lane < n_items) {
+        const Item x = item_of(A, from + lane, false);
+        mine = Held{x.token0, x.queries, x.row, x.len};
+      }
+    };
+    const auto held_at = [&](int item) -> Item {
+      const int from = item - first_held;
+      return item_from(A, Held{__shfl_sync(0xffffffffu, mine.token0, from), __shfl_sync(0xffffffffu, mine.queries, from), __shfl_sync(0xffffffffu, mine.row, from),
+                               __shfl_sync(0xffffffffu, mine.len, from)});
+    };
+    if (!holds) hold(range.item);
+    else if (range.item + lane < n_items) mine = held[range.item + lane];
     __syncwarp();
     fence_proxy_async();      // (the costs have been read before copies take their place)
-    // the next unit of the range
+    Item u = held_at(range.item);
+    // the next unit
     const auto find = [&](Unit& w) -> bool {
-      while (at < end) {
+      while (true) {
+        if (range.at >= range.end) {
+          if (other.at >= other.end) return false;
+          range = other, other = Range{};
+          hold(range.item);
+          u = held_at(range.item);
+        }
         const uint32_t cost = cost_of(u), one = unit_cost(u.tiles);
-        if (u.units == 0 || at >= item_at + cost) {
-          if (++item >= n_items) return false;
-          item_at += cost, u = u_next;
-          if (item + 1 < n_items) u_next = item_of(A, item + 1, false);
-          if (at < item_at) at = item_at;
+        if (u.units == 0 || range.at >= range.item_at + cost) {
+          if (++range.item >= n_items) {
+            range.at = range.end;
+            continue;
+          }
+          range.item_at += cost;
+          if (range.item == first_held + 32) hold(range.item);
+          u = held_at(range.item);
+          if (range.at < range.item_at) range.at = range.item_at;
           continue;
         }
-        const uint32_t unit = (at - item_at) / one, unit_at = item_at + unit * one, tiles_at = unit_at + kUnitCost;
-        const int first = at > tiles_at ? (at - tiles_at + kTileCost - 1) / kTileCost : 0;
-        const int last = end > tiles_at ? min(static_cast<uint32_t>(u.tiles), (end - tiles_at + kTileCost - 1) / kTileCost) : 0;
-        at = unit_at + one;
+        const uint32_t unit = (range.at - range.item_at) / one, unit_at = range.item_at + unit * one, tiles_at = unit_at + kUnitCost;
+        const int first = border(range.least, static_cast<int>(range.begin - tiles_at), u.tiles), last = border(range.least, static_cast<int>(range.end - tiles_at), u.tiles);
+        range.at = unit_at + one;
         if (first >= last) continue;
         const int kvh = unit / u.per_head, part = unit - kvh * u.per_head;
         const int64_t row0 = static_cast<int64_t>(part) * kRows, rows = static_cast<int64_t>(u.queries) * A.group;
         w.n_here = static_cast<int32_t>(min(static_cast<int64_t>(kRows), rows - row0));
         w.query0 = part ? static_cast<int32_t>(row0 / A.group) : 0, w.head0 = part ? static_cast<int32_t>(row0 - static_cast<int64_t>(w.query0) * A.group) : 0;
-        w.token0 = u.token0 + w.query0, w.queries = u.queries, w.kvh = kvh, w.shared = item < A.n_groups, w.row = u.row, w.first = first, w.tiles = last - first, w.len = u.len;
+        w.token0 = u.token0 + w.query0, w.queries = u.queries, w.kvh = kvh, w.shared = range.item < A.n_groups, w.row = u.row, w.first = first, w.tiles = last - first, w.len = u.len;
         w.all_see = w.shared || !A.causal ? u.len : max(0, u.len - (u.queries - 1 - w.query0));
-        w.place = first == 0 && last == u.tiles ? -1 : static_cast<int>(blockIdx.x) * 2 + (first == 0 ? 1 : 0);
+        w.place = first == 0 && last == u.tiles ? -1 : static_cast<int>(blockIdx.x) * 4 + range.line * 2 + (first == 0 ? 1 : 0);
         return true;
       }
-      return false;
     };
     const int per_tile = kKeys >> A.page_shift;
     // a unit, whether there is one, and page ids, one per lane: from page `batch` of its row on, and the 32 behind them
@@ -449,19 +543,26 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
     };
     Ahead now{}, then{};      // the unit at hand, and the next one, whose page ids are on their way
     look(now);
-    if (now.has) look(then);
+    bool looked = false;      // for the next one: behind the first copy
     bool stopped = false, described = false;
     uint32_t n_units = 0;      // described
     int tile = 0;              // of the unit, next to be fetched
     uint32_t k_next = 0, v_next = 0;
     constexpr int kHalves = D / 64;
     const int half = lane % kHalves, page_of_tile = lane / kHalves;
-    const auto copy = [&](const Meta& m, int which, uint32_t dst, uint64_t* bar) {
+    const auto copy_keys = [&](const Meta& m, uint32_t dst, uint64_t* bar) {
       const int y = page_of_tile < per_tile ? m.y[page_of_tile] : -1;
       const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
       if (lane == 0) mbar_expect_tx(bar, n * A.page * 128);
       __syncwarp();
-      if (y >= 0) tensor_g2s_2d(dst + half * Z::kHalf + page_of_tile * A.page * 128, &A.map[m.shared][which], half * 64, y, bar);
+      if (y >= 0) tensor_g2s_2d(dst + half * Z::kHalf + page_of_tile * A.page * 128, &A.map[m.shared][0], half * 64, y, bar);
+    };
+    const auto copy_values = [&](const Meta& m, uint32_t dst, uint64_t* bar) {
+      const int y = lane < per_tile ? m.y[lane] : -1;
+      const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
+      if (lane == 0) mbar_expect_tx(bar, n * A.page * (D * 2));
+      __syncwarp();
+      if (y >= 0) tensor_g2s_3d(dst + lane * A.page * (D * 2), &A.map[m.shared][1], 0, y, 0, bar);
     };
     uint32_t idle = 0, beat = 0;
     bool ok = true;
@@ -502,26 +603,28 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
             m.on = on, m.shared = w.shared;
           }
           __syncwarp();
-          copy(m, 0, sK + i * Z::kTile, &C.k[i]);
+          copy_keys(m, sK + i * Z::kTile, &C.k[i]);
           ++k_next;
           progress = true;
           if (++tile == w.tiles) {
+            if (!looked) look(then);
             described = false;
-            now = then;
-            if (now.has) look(then);
+            now = then, looked = !now.has;
           }
         }
       }
       if (v_next < k_next) {
         const uint32_t i = v_next % Z::kRing;
         if (v_next < Z::kRing || __all_sync(0xffffffffu, mbar_test_wait(kLong ? &C.v_free[i] : &C.o[i], (v_next / Z::kRing - 1) & 1u))) {
-          copy(C.meta[v_next % kMeta], 1, sV + i * Z::kTile, &C.v[i]);
+          copy_values(C.meta[v_next % kMeta], sV + i * Z::kTile, &C.v[i]);
           ++v_next;
           progress = true;
         }
       }
       if (progress) {
         idle = 0;
+      } else if (described && !looked) {      // the next unit is looked for while there is nothing else to do
+        look(then), looked = true;
       } else if (++idle > (1u << 20) || ((idle & 1023u) == 0 && failed)) {
         const uint32_t now = *reinterpret_cast<volatile uint32_t*>(&C.beat);
         if (failed || now == beat) ok = false;
@@ -547,6 +650,10 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       }
     };
     const uint64_t qd = umma_desc(sQ, 16, 1024);
+    // keys 16, 32 and 48 of a tile of values (pages one after the other, a page's halves of 64 elements too), in 16 bytes
+    uint32_t v_step[3];
+#pragma unroll
+    for (int j = 1; j < 4; ++j) v_step[j - 1] = ((16 * j >> A.page_shift) * A.page * (D * 2) + (16 * j & (A.page - 1)) * 128) >> 4;
     uint32_t s_next = 0, o_next = 0;      // tiles
     const auto issue_scores = [&]() {
       const uint32_t b = s_next & 1u, i = s_next % Z::kRing;
@@ -575,7 +682,8 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         wait_on(&C.v[i], (o_next / Z::kRing) & 1u);
         if (!ok) break;
         tc5_fence_after();
-        umma_values(tmem + kOutAt, tmem + kScoresAt + b * kKeys, umma_desc(sV + i * Z::kTile, Z::kHalf, 1024), kIdescO, t > 0 ? 1u : 0u);
+        const uint64_t vd = umma_desc(sV + i * Z::kTile, A.page * 128, 1024);
+        values(tmem + kOutAt, tmem + kScoresAt + b * kKeys, vd, vd + v_step[0], vd + v_step[1], vd + v_step[2], kIdescO, t > 0 ? 1u : 0u);
         umma_commit(&C.o[b]);
         if (kLong) umma_commit(&C.v_free[i]);
         ++o_next;
@@ -619,19 +727,30 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       x.n_here = u.n_here, x.tiles = u.tiles, x.first = u.first, x.len = u.len, x.all_see = u.all_see, x.shared = u.shared;
       x.copies = copies_of(x.n_here);
       x.copy = threadIdx.x >> (x.copies == 4 ? 5 : x.copies == 2 ? 6 : 7), x.row = threadIdx.x & (x.copies == 4 ? 31 : x.copies == 2 ? 63 : 127);
+      if (x.n_here <= kSlim) x.row = lane >> 2;      // four threads a row
       x.real = x.row < x.n_here;
       x.seen = x.shared || !A.causal ? x.len : max(0, x.len - (u.queries - 1 - u.query0 - query_of(u, x.row)));
     };
-    // the unit's queries, from their places straight into shared memory; rows that are none keep what was there
+    // the unit's queries, from their places straight into shared memory: a thread per row, or per 16 bytes where there are few; rows that are
+    // none keep what was there
     const auto ask_query = [&](uint32_t n) {
       const Unit& u = C.units[n % kUnits];
-      const int copies = copies_of(u.n_here), row = threadIdx.x & (kRows / copies - 1), query = query_of(u, row);
       const StreamArgs& S = A.stream[u.shared];
+      constexpr int kChunks = D / 8;
+      const int n_here = u.n_here, copies = copies_of(n_here);
+      const bool slim = n_here <= kSlim;
+      const int row = slim ? threadIdx.x / kChunks : threadIdx.x & (kRows / copies - 1), query = query_of(u, row);
       const uint16_t* p = S.q + (u.token0 + query) * S.q_stride + static_cast<int64_t>(u.kvh * A.group + u.head0 + row - query * A.group) * D;
-      if (row < u.n_here) {
+      if (row >= n_here) return;
+      const auto bring = [&](uint32_t to, const uint16_t* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); };
+      if (slim) {      // (kSlim rows are no more than the threads)
+        const int chunk = threadIdx.x % kChunks;
+        const uint32_t to = sQ + (chunk >> 3) * Z::kQHalf + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);      // (copies are multiples of 8 rows apart)
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sQ + (i >> 3) * Z::kQHalf + threadIdx.x * 128 + (((i & 7) ^ (threadIdx.x & 7)) << 4)), "l"(p + i * 8) : "memory");
+        for (int c = 0; c < 4; ++c) bring(to + c * (kRows / 4) * 128, p + chunk * 8);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) bring(sQ + (i >> 3) * Z::kQHalf + threadIdx.x * 128 + (((i & 7) ^ (threadIdx.x & 7)) << 4), p + i * 8);
       }
     };
     const auto put_query = [&]() {
@@ -723,6 +842,54 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         tmem_st32(at, w);
         tmem_wait_st();
       };
+      // the same for units of few rows: a warp's quarter of the keys, four of them a thread
+      const auto weigh_slim = [&](int t, uint32_t gt, uint32_t on, bool masked) {
+        const uint32_t at = t_row + kScoresAt + (gt & 1u) * kKeys;
+        const int key = warp * 16 + 2 * (lane & 3);      // and the next one, and those 8 behind
+        uint32_t r[8];
+        tmem_ld_quads16(at + warp * 16, r);
+        tmem_wait_ld();
+        float p[4] = {__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[4]), __uint_as_float(r[5])};
+        if (masked) {
+          const int left = x.seen - (t * kKeys + key);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if ((j & 1) + (j >> 1) * 8 >= left || !(on >> warp & 1u)) p[j] = -INFINITY;
+        }
+        float top = fmaxf(max3(p[0], p[1], p[2]), p[3]);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * A.scale_log2;
+        float corr = 1.f;
+        if ((top > ref + kRescale || ref == -INFINITY) && top != -INFINITY) {
+          corr = exp2f(ref - top);
+          ref = top;
+        }
+        const float less = ref == -INFINITY ? 0.f : -ref;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = ex2_approx(fmaf(p[j], A.scale_log2, less));
+        sum = sum * corr + ((p[0] + p[1]) + (p[2] + p[3]));
+        if (gt != t0 && __any_sync(0xffffffffu, corr != 1.f)) {
+          wait_on(&C.o[(gt - 1) & 1u], ((gt - 1) / 2) & 1u);
+          if (!ok) return;
+          tc5_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 64) {
+            uint32_t o[32];
+            tmem_ld_quads64(t_row + kOutAt + c, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * corr);      // (no row is 8 below one)
+            tmem_st_quads64(t_row + kOutAt + c, o);
+          }
+          tmem_wait_st();
+        }
+        const uint32_t near = pack_bf16x2(p[0], p[1]), far = pack_bf16x2(p[2], p[3]);
+        uint32_t w[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = j / 4 != warp || (j & 1) ? 0u : j & 2 ? far : near;
+        tmem_st_fours32(at, w);
+        tmem_wait_st();
+      };
       for (int i = 0; i < x.tiles && ok; ++i) {
         const uint32_t gt = t0 + i;
         const int t = x.first + i;
@@ -739,7 +906,8 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         const int left = x.len - t * kKeys;
         if (!idle) {
           const bool masked = on != 15u || (t + 1) * kKeys > x.all_see;
-          if (x.copies == 4) weigh(std::integral_constant<int, 4>{}, t, gt, on, masked);
+          if (x.n_here <= kSlim) weigh_slim(t, gt, on, masked);
+          else if (x.copies == 4) weigh(std::integral_constant<int, 4>{}, t, gt, on, masked);
           else if (x.copies == 2) weigh(std::integral_constant<int, 2>{}, t, gt, on, masked);
           else weigh(std::integral_constant<int, 1>{}, t, gt, on, masked);
         }
@@ -749,7 +917,8 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
           const int key = threadIdx.x & 63, h = threadIdx.x >> 6;
           if (ok && h < D / 64 && (key >= left || !(on >> (key / 16) & 1u))) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) sts128(sV + v * Z::kTile + h * Z::kHalf + key * 128 + c * 16, make_uint4(0, 0, 0, 0));
+            for (int c = 0; c < 8; ++c)
+              sts128(sV + v * Z::kTile + (key >> A.page_shift) * A.page * (D * 2) + (h * A.page + (key & (A.page - 1))) * 128 + c * 16, make_uint4(0, 0, 0, 0));
           }
           fence_proxy_async();
         }
@@ -786,10 +955,11 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
           for (int c = 0; c < D; c += 32) {
             uint32_t r[32];
             tmem_ld32(t_row + kOutAt + c, r);
-            uint32_t most = 0;
+            float2 none[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};      // (0 times what is no finite number is no number)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) most = max(most, r[j] & 0x7fffffffu);
-            found |= most >= 0x7f800000u;
+            for (int j = 0; j < 32; j += 2)
+              none[j / 2 & 1] = fma2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), make_float2(0.f, 0.f), none[j / 2 & 1]);
+            found |= !((none[0].x + none[0].y) + (none[1].x + none[1].y) == 0.f);
             if (x.real)
 #pragma unroll
               for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j);
@@ -799,24 +969,11 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         if (found && x.real && isfinite(sum)) flag(x.row);
       } else {
         // The copies' sums meet in shared memory: whole rows, halves or quarters of all rows at a time, as they fit.
-        float2* const refs = reinterpret_cast<float2*>(smem + Z::kRefs);      // [copies][n_here]
         const int held = x.copies * x.n_here, mine = x.copy * x.n_here + x.row;
-        if (x.real) refs[mine] = make_float2(ref, sum);
-        const auto meet = [&](auto cols_tag, auto copies_tag, int c0) {
-          constexpr int kCols = decltype(cols_tag)::value, kChunks = kCols / 4, kStep = kCols < 64 ? kCols : 64, kCopies = decltype(copies_tag)::value;
-#pragma unroll 1
-          for (int c = 0; c < kCols; c += kStep) {
-            uint32_t r[kStep / 32][32];
-#pragma unroll
-            for (int i = 0; i < kStep / 32; ++i) tmem_ld32_nowait(t_row + kOutAt + c0 + c + i * 32, r[i]);
-            tmem_wait_ld();
-            if (x.real) {
-#pragma unroll
-              for (int j = 0; j < kStep / 4; ++j)
-                sts128(sStage + mine * (kCols * 4) + (((c / 4 + j) ^ (mine & 7)) << 4), make_uint4(r[j / 8][j % 8 * 4], r[j / 8][j % 8 * 4 + 1], r[j / 8][j % 8 * 4 + 2], r[j / 8][j % 8 * 4 + 3]));
-            }
-          }
-          rows_barrier();
+        float2* const refs = reinterpret_cast<float2*>(smem + (x.n_here <= kSlim ? Z::kMeet + 4 * kSlim * 512 : Z::kRefs));      // [copies][n_here]
+        // elements c0 to c0 + kCols of all rows, from all copies
+        const auto gather = [&](auto cols_tag, auto copies_tag, int c0) {
+          constexpr int kCols = decltype(cols_tag)::value, kChunks = kCols / 4, kCopies = decltype(copies_tag)::value;
           for (int i = threadIdx.x; i < x.n_here * kChunks; i += kRows) {
             const int row = i / kChunks, chunk = i % kChunks;
             float2 z[kCopies];
@@ -825,7 +982,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
 #pragma unroll
             for (int k = 0; k < kCopies; ++k) {
               const int at = k * x.n_here + row;
-              z[k] = refs[at], v[k] = lds128(sStage + at * (kCols * 4) + ((chunk ^ (at & 7)) << 4));
+              z[k] = refs[at], v[k] = lds128(sMeet + at * (kCols * 4) + ((chunk ^ (at & 7)) << 4));
               top = fmaxf(top, z[k].x);
             }
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -843,8 +1000,25 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
             if (!(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w)) && isfinite(all)) flag(row);
           }
         };
+        const auto meet = [&](auto cols_tag, auto copies_tag, int c0) {
+          constexpr int kCols = decltype(cols_tag)::value, kStep = kCols < 64 ? kCols : 64;
+#pragma unroll 1
+          for (int c = 0; c < kCols; c += kStep) {
+            uint32_t r[kStep / 32][32];
+#pragma unroll
+            for (int i = 0; i < kStep / 32; ++i) tmem_ld32_nowait(t_row + kOutAt + c0 + c + i * 32, r[i]);
+            tmem_wait_ld();
+            if (x.real) {
+#pragma unroll
+              for (int j = 0; j < kStep / 4; ++j)
+                sts128(sMeet + mine * (kCols * 4) + (((c / 4 + j) ^ (mine & 7)) << 4), make_uint4(r[j / 8][j % 8 * 4], r[j / 8][j % 8 * 4 + 1], r[j / 8][j % 8 * 4 + 2], r[j / 8][j % 8 * 4 + 3]));
+            }
+          }
+          rows_barrier();
+          gather(cols_tag, copies_tag, c0);
+        };
         const auto meet_all = [&](auto copies_tag) {
-          if (held * D * 4 <= static_cast<int>(Z::kStageBytes)) {
+          if (held * D * 4 <= static_cast<int>(Z::kMeetBytes)) {
             meet(std::integral_constant<int, D>{}, copies_tag, 0);
           } else {
 #pragma unroll 1
@@ -854,8 +1028,30 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
             }
           }
         };
-        if (x.copies == 4) meet_all(std::integral_constant<int, 4>{});
-        else meet_all(std::integral_constant<int, 2>{});
+        if (x.n_here <= kSlim) {
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          if (x.real && (lane & 3) == 0) refs[mine] = make_float2(ref, sum);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 64) {
+            uint32_t r[32];
+            tmem_ld_quads64(t_row + kOutAt + c, r);
+            tmem_wait_ld();
+            if (x.real) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {      // elements c + 8 j + 2 (lane % 4) and the next one
+                const uint32_t to = sMeet + mine * (D * 4) + (((c / 4 + 2 * j + ((lane & 3) >> 1)) ^ (mine & 7)) << 4) + (lane & 1) * 8;
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(r[4 * j]), "r"(r[4 * j + 1]) : "memory");
+              }
+            }
+          }
+          rows_barrier();
+          gather(std::integral_constant<int, D>{}, std::integral_constant<int, 4>{}, 0);
+        } else {
+          if (x.real) refs[mine] = make_float2(ref, sum);
+          if (x.copies == 4) meet_all(std::integral_constant<int, 4>{});
+          else meet_all(std::integral_constant<int, 2>{});
+        }
       }
       if (rows_any(strange)) {      // rare: rows whose sums a value behind a weight of 0 may have spoiled, by hand
         for (int row = warp; row < x.n_here; row += 4) {
@@ -905,10 +1101,13 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
       const int64_t flat = (token - u.token0) * A.group + head - kvh * A.group;
       const uint32_t per_head = static_cast<uint32_t>((static_cast<int64_t>(u.queries) * A.group + kRows - 1) / kRows);
       const uint32_t tiles_at = u.base + (kvh * per_head + static_cast<uint32_t>(flat / kRows)) * unit_cost(u.tiles) + kUnitCost;
-      const uint32_t first = worker_at(plan, tiles_at), last = worker_at(plan, tiles_at + (u.tiles - 1) * kTileCost);
+      const int line = plan.lines == 2 && kind == 0 ? 1 : 0;
+      const Line p = line ? plan.line[1] : plan.line[0];
+      const bool cut = u.tiles >= 2 * p.least;
+      const uint32_t first = worker_at(p, tiles_at + (cut ? p.least - 1 : u.tiles / 2)), last = worker_at(p, tiles_at + (cut ? u.tiles - p.least : u.tiles / 2));
       const int row = static_cast<int>(flat % kRows);
       const auto part = [&](uint32_t w) -> const float* {
-        return first == last ? A.rows + (kind * heads + at) * D : A.pieces + (static_cast<size_t>(w) * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + row * D;
+        return first == last ? A.rows + (kind * heads + at) * D : A.pieces + (static_cast<size_t>(w) * 4 + line * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + row * D;
       };
       for (uint32_t w0 = first; w0 <= last; w0 += 32) {
         const uint32_t w = w0 + lane;
@@ -916,7 +1115,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
         float2 ml = make_float2(-INFINITY, 0.f);
         if (lane < n)
           ml = __ldcg(first == last ? A.row_ml + kind * heads + at
-                                    : reinterpret_cast<const float2*>(A.pieces + (static_cast<size_t>(w) * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + kRows * D) + row);
+                                    : reinterpret_cast<const float2*>(A.pieces + (static_cast<size_t>(w) * 4 + line * 2 + (w == first ? 1 : 0)) * (kRows * (D + 2)) + kRows * D) + row);
         float top = ml.x;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
@@ -931,13 +1130,13 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__
 #pragma unroll 4
         for (int k = 0; k < n; ++k) {
           const float fk = __shfl_sync(0xffffffffu, f, k);
-          const float* p = part(w0 + k);
+          const float* from = part(w0 + k);
           float v[D / 32];
           if constexpr (D == 128) {
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(p) + lane);
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(from) + lane);
             v[0] = y.x, v[1] = y.y, v[2] = y.z, v[3] = y.w;
           } else {
-            const float2 y = __ldcg(reinterpret_cast<const float2*>(p) + lane);
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(from) + lane);
             v[0] = y.x, v[1] = y.y;
           }
 #pragma unroll
@@ -981,7 +1180,7 @@ int32_t check_sizes(const qc_paged_attend_args* a) {
 }
 
 // The workspace: plan and records, then the sums of whole units' rows, then pieces, each part at a multiple of 256 bytes.
-constexpr int kMostWorkers = 320;
+constexpr int kMostWorkers = 296;
 struct Layout {
   size_t records, rows, row_ml, pieces, bytes;
 };
@@ -993,15 +1192,16 @@ Layout layout_of(const qc_paged_attend_args* a) {
   w.rows = w.records + up(static_cast<size_t>(a->n_groups + a->n_seqs) * sizeof(Record));
   w.row_ml = w.rows + up(heads * a->head_dim * 4);
   w.pieces = w.row_ml + up(heads * 8);
-  w.bytes = w.pieces + static_cast<size_t>(kMostWorkers) * 2 * kRows * (a->head_dim + 2) * 4;
+  w.bytes = w.pieces + static_cast<size_t>(kMostWorkers) * 4 * kRows * (a->head_dim + 2) * 4;
   return w;
 }
 size_t workspace_bytes(const qc_paged_attend_args* a) { return layout_of(a).bytes; }
 
-// A pool as rows of D elements: a copy brings 64 of them from the tokens of one page and head, with the 128-byte swizzle.
+// A pool as rows of D elements, from which a copy brings 64 of each token of a page and head; or the halves of the rows as a dimension of
+// their own, and a copy brings all of them, one half after the other.  With the 128-byte swizzle.
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-int32_t make_map(CUtensorMap* out, const void* pool, const qc_paged_attend_args* a, int32_t n_pages) {
+int32_t make_map(CUtensorMap* out, const void* pool, const qc_paged_attend_args* a, int32_t n_pages, bool values) {
   static const EncodeFn encode = [] {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult found;
@@ -1009,11 +1209,12 @@ int32_t make_map(CUtensorMap* out, const void* pool, const qc_paged_attend_args*
     return reinterpret_cast<EncodeFn>(fn);
   }();
   if (!encode) return QC_ERR_CUDA;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a->head_dim), static_cast<cuuint64_t>(n_pages) * a->n_kv_heads * a->page_size};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(a->head_dim) * 2};
-  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(a->page_size)}, steps[2] = {1, 1};
-  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+  const cuuint64_t d = a->head_dim, rows = static_cast<cuuint64_t>(n_pages) * a->n_kv_heads * a->page_size;
+  const cuuint32_t page = a->page_size, steps[3] = {1, 1, 1};
+  const cuuint64_t flat[2] = {d, rows}, halves[3] = {64, rows, d / 64}, strides[2] = {d * 2, 128};
+  const cuuint32_t box2[2] = {64, page}, box3[3] = {64, page, static_cast<cuuint32_t>(d / 64)};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, values ? 3 : 2, const_cast<void*>(pool), values ? halves : flat, strides, values ? box3 : box2, steps,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? QC_OK
              : QC_ERR_CUDA;
 }
@@ -1091,8 +1292,8 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   for (int i = 0; i <= (shared ? 1 : 0); ++i) {
     const qc_paged_stream& s = i ? args->shared : args->own;
-    if (const int32_t bad = make_map(&A.map[i][0], s.k_pool_dev, args, s.n_pages)) return bad;
-    if (const int32_t bad = make_map(&A.map[i][1], s.v_pool_dev, args, s.n_pages)) return bad;
+    if (const int32_t bad = make_map(&A.map[i][0], s.k_pool_dev, args, s.n_pages, false)) return bad;
+    if (const int32_t bad = make_map(&A.map[i][1], s.v_pool_dev, args, s.n_pages, true)) return bad;
   }
   return status_of(args->head_dim == 128 ? launch<128>(A, device, stream) : launch<64>(A, device, stream));
 }
