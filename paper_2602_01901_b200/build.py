@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libqcache.so")
 EXTENSION = os.path.join(HERE, "_qc_torch.so")
 SOURCES = ["qc_runtime.cu", "qc_kernels.cu", "qc_attend_tc.cu", "qc_rows.cu", "qc_prefill.cu", "qc_calib.cu", "qc_static.cu",
            "qc_table.cu", "qc_quant.cu", "qc_quant_attend.cu", "qc_paged.cu", "qc_paged_attend.cu"]
-HEADERS = ["qc_internal.h", "qc_device.cuh", "qc_umma.cuh", "qc_quant.h", "qc_quant.cuh", os.path.join("..", "..", "include", "qc.h")]
+HEADERS = ["qc_internal.h", "qc_device.cuh", "qc_umma.cuh", "qc_quant.h", "qc_quant.cuh", "qc_paged_attend.cuh", "qc_paged_few.cuh", os.path.join("..", "..", "include", "qc.h")]
 
 
 def _nvcc() -> str:
