@@ -94,7 +94,7 @@ struct Few {
   static constexpr bool kIsFew = true;
   static constexpr uint32_t kUnitCost = 6, kRange = 2, kPiece = 8;
 };
-constexpr float kManyTile = 3.5f;      // what a tile of many rows takes a block, in tiles that the warps of a block take together
+constexpr float kManyTile = 3.f, kManyMore = 6.f;      // what a tile of many rows takes a block, in tiles that the warps of a block take together
 
 // An item as it is held while units are looked for.
 struct Held {
@@ -221,12 +221,16 @@ __device__ __forceinline__ Plan plan_of(const Args& A, Found& found, uint64_t* s
   }
   fine = __syncthreads_and(fine);
   const bool small = total[0] <= kMostCost && total[1] <= kMostCost;
-  // All that can go side by side does, where there are blocks enough; else they are shared out by time.
+  // All that can go side by side does, where there are blocks enough (or nearly so); else they are shared out by time.  A tile of many rows takes
+  // a block as long as kManyTile tiles of few rows where blocks of its kind are alone, and up to kManyMore more where the others keep
+  // the memory busy: it has less under way.
   const uint32_t blocks = gridDim.x, warps = kBlock / 32;
   uint32_t many = min(blocks, total[0] / Many::kRange);
   const uint32_t few = (min(blocks * warps, max(1u, total[1] / Few::kRange)) + warps - 1) / warps;
-  if (total[1] && many + few > blocks && total[0])
-    many = max(1u, min(blocks - 1, static_cast<uint32_t>(blocks * (kManyTile * total[0] / (kManyTile * total[0] + total[1])) + 0.5f)));
+  if (total[1] && total[0] && many + few / 2 > blocks) {
+    const float share = total[1] / (kManyTile * total[0] + total[1]), tile = kManyTile + kManyMore * share;
+    many = max(1u, min(blocks - 1, static_cast<uint32_t>(blocks * (tile * total[0] / (tile * total[0] + total[1])) + 0.5f)));
+  }
   Plan p{};
   p.many = many;
   p.line[0] = line_of(total[0], max(1u, many), Many::kRange, Many::kPiece);

@@ -232,12 +232,14 @@ __device__ __forceinline__ void take_few(const Args& A, Walk<Few>& walk, uint32_
     x.batch = x.w.first * Few::kKeys >> A.page_shift;
     x.ids = ask_ids(A, x.w, x.batch, lane), x.next_ids = ask_ids(A, x.w, x.batch + 32, lane);
   };
-  Ahead now{};
-  for (look(now); now.has;) {
-    Ahead then{};
-    look(then);      // (its page ids are on their way meanwhile)
-    if (now.w.n_here <= 8) take_unit<D, 1>(A, now, ring, lane);
-    else take_unit<D, 2>(A, now, ring, lane);
+  // (a unit is looked for in one place: what runs once is bound by the way of its instructions)
+  for (Ahead now{}, then{};;) {
+    look(then);      // its page ids are on their way while the unit before it is taken
+    if (now.has) {
+      if (now.w.n_here <= 8) take_unit<D, 1>(A, now, ring, lane);
+      else take_unit<D, 2>(A, now, ring, lane);
+    }
+    if (!then.has) break;
     now = then;
   }
 }
