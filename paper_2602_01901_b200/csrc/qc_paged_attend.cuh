@@ -231,6 +231,7 @@ __device__ __forceinline__ Plan plan_of(const Args& A, Found& found, uint64_t* s
     const float share = total[1] / (kManyTile * total[0] + total[1]), tile = kManyTile + kManyMore * share;
     many = max(1u, min(blocks - 1, static_cast<uint32_t>(blocks * (tile * total[0] / (tile * total[0] + total[1])) + 0.5f)));
   }
+  if (total[1]) many = min(many, blocks - 1);
   Plan p{};
   p.many = many;
   p.line[0] = line_of(total[0], max(1u, many), Many::kRange, Many::kPiece);

@@ -77,6 +77,18 @@ def test_a_large_batch_of_short_sequences():
     b.check(out, lse, [0, 4, 5, 899, 900, 1999, 2000, 2047])
 
 
+@pytest.mark.parametrize("lens,prefix", [([0] * 19 + [5], 40000), ([0] * 19 + [70], 19000), ([9000] * 20, 1), ([20000] + [0] * 19, 65)])
+def test_little_of_one_kind_beside_much_of_the_other(lens, prefix):
+    """Rows that single warps take, and rows that a block takes, share the device out between them: neither gets nothing."""
+    run(Batch(18, lens, [1] * 20, [(0, 20, prefix)], 1, 1, 128, 64, lazy=True))
+
+
+@pytest.mark.parametrize("group", [1, 2, 5])
+def test_sequences_of_as_many_rows_as_a_warp_takes_and_more(group):
+    queries = [3, 8, 16, 9, 17, 1, 4, 33]
+    run(Batch(19, [700, 5, 90, 1300, 33, 2000, 64, 400], queries, [(1, 4, 130), (4, 6, 500)], 2, group, 64, 32))
+
+
 def test_many_groups_of_one():
     n = 300
     run(Batch(7, [3] * n, [1] * n, [(i, i + 1, i % 130) for i in range(n)], 1, 3, 128, 16, lazy=True))
