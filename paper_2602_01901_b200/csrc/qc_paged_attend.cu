@@ -530,9 +530,9 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
 
       // ---- the unit's rows: to their queries' places, or as a piece
       const Unit& u = C.units[n % kUnits];
-      float* const piece = A.pieces + static_cast<size_t>(max(0, u.place)) * (kRows * (D + 2));
-      const auto sums_of = [&](int row) -> float* { return u.place < 0 ? A.rows + place_of(A, u, row) * D : piece + row * D; };
-      const auto ml_of = [&](int row) -> float2* { return u.place < 0 ? A.row_ml + place_of(A, u, row) : reinterpret_cast<float2*>(piece + kRows * D) + row; };
+      const size_t piece = static_cast<size_t>(max(0, u.place)) * kRows;
+      const auto sums_of = [&](int row) -> float* { return u.place < 0 ? A.rows + place_of(A, u, row) * D : A.pieces + (piece + row) * D; };
+      const auto ml_of = [&](int row) -> float2* { return u.place < 0 ? A.row_ml + place_of(A, u, row) : A.piece_ml + piece + row; };
       bool strange = false;      // a sum that is no finite number although its row's weights are numbers
       const auto flag = [&](int row) { atomicOr(&C.redo[row >> 5], 1u << (row & 31)), strange = true; };
       if (x.copies == 1) {
@@ -674,18 +674,17 @@ __device__ __forceinline__ Parts parts_of(const Args& A, const Plan& plan, const
     return x;
   }
   const int rows = few ? kFew : kRows;
-  const int64_t size = static_cast<int64_t>(rows) * (D + 2);
-  x.sums = (few ? A.few_pieces : A.pieces) + first * 2 * size;      // the first worker's is its second piece, the others' their first
-  x.ml = reinterpret_cast<const float2*>(x.sums + static_cast<int64_t>(rows) * D) + row;
-  x.sums += row * D;
-  x.sums_step = 2 * size, x.ml_step = size;
+  const int64_t at = static_cast<int64_t>(first) * 2 * rows + row;      // the first worker's is its second piece, the others' their first
+  x.sums = (few ? A.few_pieces : A.pieces) + at * D;
+  x.ml = (few ? A.few_piece_ml : A.piece_ml) + at;
+  x.sums_step = 2 * rows * D, x.ml_step = 2 * rows;
   return x;
 }
 
 // Puts the parts of each row together: kLanes lanes of kWarps warps a row, a part's reference and sum per lane.  A block's rows have their parts
 // found first, a thread each.  Grid: (sequences, parts of their rows).
 template <int D, int kLanes, int kWarps>
-__global__ void __launch_bounds__(256, 4) paged_join_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(const __grid_constant__ Args A) {
   constexpr int kAtOnce = 8 / kWarps * (32 / kLanes), kOwn = D / kLanes, kVec = kOwn < 4 ? kOwn : 4;      // rows of a block; elements of a lane
   __shared__ Parts parts[2][kAtOnce];
   __shared__ float met[kWarps > 1 ? 8 : 1][D + 2];
@@ -710,7 +709,7 @@ __global__ void __launch_bounds__(256, 4) paged_join_kernel(const __grid_constan
       const Parts& x = parts[i < n_first ? 1 : 0][mine];
       const uint32_t at = i < n_first ? i : i - n_first;
       float2 ml = make_float2(-INFINITY, 0.f);
-      const float* from = nullptr;
+      const float* from = A.rows;      // (of parts that are none: anything, it weighs nothing)
       if (i < n) {      // (the first worker's piece is its second)
         ml = __ldcg(x.ml + at * x.ml_step + (x.n > 1 && at == 0 ? x.ml_step / 2 : 0));
         from = x.sums + at * x.sums_step + (x.n > 1 && at == 0 ? x.sums_step / 2 : 0);
@@ -727,25 +726,34 @@ __global__ void __launch_bounds__(256, 4) paged_join_kernel(const __grid_constan
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) o[k] = old == 0.f ? 0.f : o[k] * old;
       const int here = static_cast<int>(min(static_cast<uint32_t>(kLanes), (most - i0 + kWarps - 1) / kWarps));
-#pragma unroll 8
-      for (int k = 0; k < here; ++k) {
-        const float fk = __shfl_sync(0xffffffffu, f, k, kLanes);
-        const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), k, kLanes));
-        float v[kOwn] = {};
-        if (p) {
+      // So many parts under way at a time: where a warp has a row there are many of them (32 questions about one image: 21.6 us one after the
+      // other, 20.2 by eight), else mostly one or two (256 questions about a video: 169.6 us by four, 162.7 by two)
+      constexpr int kUnder = kLanes == 32 ? 8 : 2;
+#pragma unroll 1
+      for (int k0 = 0; k0 < here; k0 += kUnder) {
+        float v[kUnder][kOwn];
+#pragma unroll
+        for (int k = 0; k < kUnder; ++k) {
+          if (k0 + k >= here) break;
+          const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(from), k0 + k, kLanes));
 #pragma unroll
           for (int c = 0; c < kOwn / kVec; ++c) {
             if constexpr (kVec == 4) {
               const float4 y = __ldcg(reinterpret_cast<const float4*>(p) + c * kLanes + j);
-              v[4 * c] = y.x, v[4 * c + 1] = y.y, v[4 * c + 2] = y.z, v[4 * c + 3] = y.w;
+              v[k][4 * c] = y.x, v[k][4 * c + 1] = y.y, v[k][4 * c + 2] = y.z, v[k][4 * c + 3] = y.w;
             } else {
               const float2 y = __ldcg(reinterpret_cast<const float2*>(p) + c * kLanes + j);
-              v[2 * c] = y.x, v[2 * c + 1] = y.y;
+              v[k][2 * c] = y.x, v[k][2 * c + 1] = y.y;
             }
           }
         }
 #pragma unroll
-        for (int e = 0; e < kOwn; ++e) o[e] += fk == 0.f ? 0.f : v[e] * fk;
+        for (int k = 0; k < kUnder; ++k) {
+          if (k0 + k >= here) break;
+          const float fk = __shfl_sync(0xffffffffu, f, k0 + k, kLanes);
+#pragma unroll
+          for (int e = 0; e < kOwn; ++e) o[e] += fk == 0.f ? 0.f : v[k][e] * fk;
+        }
       }
     }
     if constexpr (kWarps > 1) {      // the warps of a row
@@ -816,21 +824,24 @@ int32_t check_sizes(const qc_paged_attend_args* a) {
   return QC_OK;
 }
 
-// The workspace: plan and records, then the sums of whole units' rows, then pieces, each part at a multiple of 256 bytes.
+// The workspace: plan and records, references, then the sums of whole units' rows and of pieces, each part at a multiple of 256 bytes.
 constexpr int kMostWorkers = 296;
 struct Layout {
-  size_t records, rows, row_ml, pieces, few_pieces, bytes;
+  size_t records, row_ml, piece_ml, few_piece_ml, rows, few_pieces, pieces, bytes;
 };
 Layout layout_of(const qc_paged_attend_args* a) {
   const auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
   const size_t heads = static_cast<size_t>(a->n_tokens) * a->n_q_heads * (a->n_groups ? 2 : 1);
   Layout w{};
+  const size_t pieces = static_cast<size_t>(kMostWorkers) * 2 * kRows, few_pieces = static_cast<size_t>(kMostWorkers) * (kBlock / 32) * 2 * kFew, row = a->head_dim * 4;
   w.records = 256;
-  w.rows = w.records + up(static_cast<size_t>(a->n_seqs) * 2 * sizeof(Record));
-  w.row_ml = w.rows + up(heads * a->head_dim * 4);
-  w.pieces = w.row_ml + up(heads * 8);
-  w.few_pieces = w.pieces + static_cast<size_t>(kMostWorkers) * 2 * kRows * (a->head_dim + 2) * 4;
-  w.bytes = w.few_pieces + static_cast<size_t>(kMostWorkers) * (kBlock / 32) * 2 * kFew * (a->head_dim + 2) * 4;
+  w.row_ml = w.records + up(static_cast<size_t>(a->n_seqs) * 2 * sizeof(Record));
+  w.piece_ml = w.row_ml + up(heads * 8);
+  w.few_piece_ml = w.piece_ml + up(pieces * 8);
+  w.rows = w.few_piece_ml + up(few_pieces * 8);
+  w.few_pieces = w.rows + up(heads * row);
+  w.pieces = w.few_pieces + up(few_pieces * row);
+  w.bytes = w.pieces + pieces * row;
   return w;
 }
 size_t workspace_bytes(const qc_paged_attend_args* a) { return layout_of(a).bytes; }
@@ -930,6 +941,7 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   A.plan = reinterpret_cast<Plan*>(work), A.records = reinterpret_cast<Record*>(work + w.records), A.rows = reinterpret_cast<float*>(work + w.rows);
   A.row_ml = reinterpret_cast<float2*>(work + w.row_ml), A.pieces = reinterpret_cast<float*>(work + w.pieces);
   A.few_pieces = reinterpret_cast<float*>(work + w.few_pieces);
+  A.piece_ml = reinterpret_cast<float2*>(work + w.piece_ml), A.few_piece_ml = reinterpret_cast<float2*>(work + w.few_piece_ml);
   A.hq = args->n_q_heads, A.hkv = args->n_kv_heads, A.group = A.hq / A.hkv, A.page = args->page_size;
   A.page_shift = A.page == 16 ? 4 : A.page == 32 ? 5 : 6;
   A.n_seqs = args->n_seqs, A.n_groups = args->n_groups, A.n_tokens = args->n_tokens, A.max_queries = args->max_queries, A.causal = args->causal != 0;

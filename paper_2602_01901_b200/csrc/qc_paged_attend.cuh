@@ -61,8 +61,10 @@ struct Args {
   Record* records;         // [sequences][2] its own tokens, its prefix
   float* rows;             // [kinds][tokens * heads][D] sums of whole units
   float2* row_ml;          // [kinds][tokens * heads] their references and sums of weights
-  float* pieces;           // [workers][2][128 * (D + 2)] of many rows
-  float* few_pieces;       // [workers][2][kFew * (D + 2)]
+  float* pieces;           // [workers][2][128][D] of many rows
+  float2* piece_ml;        // [workers][2][128]: side by side, since they are read first
+  float* few_pieces;       // [workers][2][kFew][D]
+  float2* few_piece_ml;    // [workers][2][kFew]
   int32_t* status;
   int32_t hq, hkv, group, page, page_shift;
   int32_t n_seqs, n_groups, n_tokens, max_queries, causal;

@@ -191,7 +191,7 @@ __device__ __forceinline__ void take_unit(const Args& A, Ahead& x, uint32_t ring
   __syncwarp();
 
   // the rows' sums, to their queries' places or as a piece: a lane has elements g and g + 8 of every 16
-  float* const piece = A.few_pieces + static_cast<size_t>(max(0, w.place)) * (kFew * (D + 2));
+  const size_t piece = static_cast<size_t>(max(0, w.place)) * kFew;
   uint32_t strange = 0;      // rows with a sum that is no finite number although their weights are numbers
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
@@ -204,22 +204,22 @@ __device__ __forceinline__ void take_unit(const Args& A, Ahead& x, uint32_t ring
       const int row = nt * 8 + 2 * t + e;
       if (row >= w.n_here) continue;
       const size_t at = place_of(A, w, row);
-      float* const to = (w.place < 0 ? A.rows + at * D : piece + row * D) + g;
+      float* const to = (w.place < 0 ? A.rows + at * D : A.few_pieces + (piece + row) * D) + g;
       float none = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         to[16 * i] = acc[nt][i][e], to[16 * i + 8] = acc[nt][i][e + 2];
         none = fmaf(acc[nt][i][e], 0.f, fmaf(acc[nt][i][e + 2], 0.f, none));      // (0 times what is no finite number is no number)
       }
-      if (g == 0) *(w.place < 0 ? A.row_ml + at : reinterpret_cast<float2*>(piece + kFew * D) + row) = make_float2(ref[nt][e], l);
+      if (g == 0) *(w.place < 0 ? A.row_ml + at : A.few_piece_ml + piece + row) = make_float2(ref[nt][e], l);
       if (none != 0.f && isfinite(l)) strange |= 1u << row;
     }
   __syncwarp();
   for (uint32_t rows = __reduce_or_sync(0xffffffffu, strange); rows; rows &= rows - 1) {      // rare: by hand
     const int row = __ffs(rows) - 1;
     const size_t at = place_of(A, w, row);
-    sweep<D>(A, w, row, w.first * Few::kKeys, stop * Few::kKeys, w.place < 0 ? A.rows + at * D : piece + row * D,
-             w.place < 0 ? A.row_ml + at : reinterpret_cast<const float2*>(piece + kFew * D) + row, nullptr, lane);
+    sweep<D>(A, w, row, w.first * Few::kKeys, stop * Few::kKeys, w.place < 0 ? A.rows + at * D : A.few_pieces + (piece + row) * D,
+             w.place < 0 ? A.row_ml + at : A.few_piece_ml + piece + row, nullptr, lane);
   }
 }
 
