@@ -689,10 +689,11 @@ __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(c
   __shared__ Parts parts[2][kAtOnce];
   __shared__ float met[kWarps > 1 ? 8 : 1][D + 2];
   pdl_wait();
+  // (asked for together: what one after the other costs here is the way to memory)
   const Plan plan = *A.plan;
+  const Record own = A.records[2 * blockIdx.x], prefix = A.records[2 * blockIdx.x + 1];
   if (!plan.fine) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = warp % kWarps, j = lane % kLanes, mine = warp / kWarps * (32 / kLanes) + lane / kLanes;
-  const Record own = A.records[2 * blockIdx.x], prefix = A.records[2 * blockIdx.x + 1];
   const int n_rows = own.queries * A.hq;
   for (int r0 = blockIdx.y * kAtOnce; r0 < n_rows; r0 += gridDim.y * kAtOnce) {
     if (threadIdx.x < 2 * kAtOnce) {
@@ -714,24 +715,13 @@ __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(c
         ml = __ldcg(x.ml + at * x.ml_step + (x.n > 1 && at == 0 ? x.ml_step / 2 : 0));
         from = x.sums + at * x.sums_step + (x.n > 1 && at == 0 ? x.sums_step / 2 : 0);
       }
-      float top = ml.x;
-#pragma unroll
-      for (int k = kLanes / 2; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-      top = fmaxf(top, m);
-      const float f = weight_of(ml, top), old = weight_of(make_float2(m, l), top);
-      float sum = ml.y * f;
-#pragma unroll
-      for (int k = kLanes / 2; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-      l = l * old + sum, m = top;
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k) o[k] = old == 0.f ? 0.f : o[k] * old;
       const int here = static_cast<int>(min(static_cast<uint32_t>(kLanes), (most - i0 + kWarps - 1) / kWarps));
       // So many parts under way at a time: where a warp has a row there are many of them (32 questions about one image: 21.6 us one after the
-      // other, 20.2 by eight), else mostly one or two (256 questions about a video: 169.6 us by four, 162.7 by two)
+      // other, 20.2 by eight), else mostly one or two (256 questions about a video: 169.6 us by four, 162.7 by two).  The first ones are
+      // asked for with their references.
       constexpr int kUnder = kLanes == 32 ? 8 : 2;
-#pragma unroll 1
-      for (int k0 = 0; k0 < here; k0 += kUnder) {
-        float v[kUnder][kOwn];
+      float v[kUnder][kOwn];
+      const auto fetch = [&](int k0) {
 #pragma unroll
         for (int k = 0; k < kUnder; ++k) {
           if (k0 + k >= here) break;
@@ -747,6 +737,22 @@ __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(c
             }
           }
         }
+      };
+      fetch(0);
+      float top = ml.x;
+#pragma unroll
+      for (int k = kLanes / 2; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+      top = fmaxf(top, m);
+      const float f = weight_of(ml, top), old = weight_of(make_float2(m, l), top);
+      float sum = ml.y * f;
+#pragma unroll
+      for (int k = kLanes / 2; k > 0; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+      l = l * old + sum, m = top;
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) o[k] = old == 0.f ? 0.f : o[k] * old;
+#pragma unroll 1
+      for (int k0 = 0; k0 < here; k0 += kUnder) {
+        if (k0) fetch(k0);
 #pragma unroll
         for (int k = 0; k < kUnder; ++k) {
           if (k0 + k >= here) break;
