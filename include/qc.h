@@ -595,12 +595,14 @@ int32_t qc_paged_workspace_bytes(const qc_paged_attend_args* args, size_t* bytes
 /* Attention of each sequence's query tokens over its prefix, if it is in a group, and its own cached tokens: one softmax over the
  * prefix's keys scored by shared.q_dev and its own keys scored by own.q_dev (an ordinary layer: the same queries twice; a
  * lazy layer whose prefix is the image: the Q Cache on the leader's visual K).  A prefix is read once for all query rows of its
- * group (once per 128 of a KV head's), whose sequences are adjacent in the list; sequences before the first group and behind the last have none.
- * All tokens of a prefix are seen by every query.  A query that sees no key gets 0 and lse minus infinity, and so does one whose
- * scores are all minus infinity.  What the pools hold where no token is counts for nothing, whatever it is.
+ * group (once per 128 rows of a KV head), whose sequences are adjacent in the list; sequences before the first group and behind the
+ * last have none.  All tokens of a prefix are seen by every query.  A query that sees no key gets 0 and lse minus infinity, and so
+ * does one whose scores are all minus infinity.  What the pools hold where no token is counts for nothing, whatever it is.
+ * The work is divided by sizes alone, so a call gives the same bits each time.
  * All or nothing: rows out of range, starts or groups that do not ascend or reach outside, more queries than max_queries
- * (QC_ERR_INVALID_ARG in the status word) and batches with over 2^24 tiles of 64 keys, counted once per KV head and 128 query rows
- * (QC_ERR_PLAN), leave out as it was.  A page id that is not in the pool is not followed: its keys count as absent
+ * (QC_ERR_INVALID_ARG in the status word) and batches of some 2^26 tiles of keys or more (QC_ERR_PLAN) leave out as it was; a tile is 64 keys,
+ * counted per KV head and 128 query rows, or 16 where a sequence or a group has no more than 16 rows a KV head, which distinct pages
+ * that fit on a device do not reach.  A page id that is not in the pool is not followed: its keys count as absent
  * (QC_ERR_BAD_PAGE).  A length beyond the table's room is cut to it (QC_ERR_PLAN).  Rows of out that belong to no sequence are
  * left as they are. */
 int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_paged_attend_args* args);

@@ -145,11 +145,13 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       C.failed = 0, C.beat = 0;
       for (int i = 0; i < 4; ++i) C.redo[i] = 0;
     }
-  } else if (warp == 4) {
+  }
+  pdl_wait();
+  // (not ahead of the wait: a kernel before this one may still want tensor memory for blocks that are to come)
+  if (warp == 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&C.tmem)), "n"(kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
 
   // the plan, in the tiles' place until they come
   Found& found = *reinterpret_cast<Found*>(smem);

@@ -161,6 +161,20 @@ def test_values_and_queries_that_are_no_numbers_stay_in_their_rows():
     assert lse[3, 0].isnan() and torch.equal(lse[:3], want_lse[:3]) and torch.equal(lse[3, 1:], want_lse[3, 1:])
 
 
+@pytest.mark.parametrize("group", [2, 10])
+def test_what_a_query_does_not_see_may_be_no_number(group):
+    """The last own token's value is infinite in one element of one head, its key a NaN in another: queries ahead of it see neither."""
+    b = Batch(28, [70, 200], [3, 3], [(0, 2, 100)], 2, group, 128, 16)
+    want, want_lse = run(b)
+    page, place = int(b.table.pages[int(b.ids[1]), 199 // 16]), 199 % 16
+    b.pools[1][page, 0, place, 5] = math.inf
+    b.pools[0][page, 1, place, 9] = math.nan
+    out, lse = b.call()
+    assert (out[5, :group, 5] == math.inf).all() and out[5, group:].isnan().all() and lse[5, group:].isnan().all()
+    out[5, :group, 5], out[5, group:], lse[5, group:] = want[5, :group, 5], want[5, group:], want_lse[5, group:]
+    b.check(out, lse)
+
+
 def test_scores_of_minus_infinity():
     b = Batch(14, [64, 130, 65], [1, 1, 1], [(1, 3, 64)], 1, 2, 64, 16)
     b.q[:, :, 0] = 1.0
@@ -206,6 +220,29 @@ def test_a_pool_past_32_bits_of_elements():
     pages = torch.where(b.table.pages >= 0, b.table.pages + move, -1)
     out, lse = b.call(own=paged.Stream(b.q, *pools, pages, b.table.lens))
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_a_pool_past_32_bits_of_elements_and_many_rows():
+    b = Batch(29, [100, 40], [1, 1], [(0, 2, 150)], 32, 20, 128, 16)
+    pools = [torch.empty(33000, 32, 16, 128, dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    move = 33000 - b.shared[1][0].shape[0]
+    for new, old in zip(pools, b.shared[1]):
+        new[move:] = old
+    want = run(b)
+    s = b.shared_stream()
+    out, lse = b.call(shared=s._replace(k_pool=pools[0], v_pool=pools[1], pages=torch.where(s.pages >= 0, s.pages + move, -1)))
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_the_same_row_more_than_once():
+    b = Batch(30, [50, 40, 90, 20], [1, 2, 1, 1], [(0, 1, 70), (1, 3, 70), (3, 4, 300)], 2, 4, 64, 16)
+    run(b)
+    ids, shared_ids = b.ids[torch.tensor([0, 2, 2, 0], device=DEV)], b.shared_ids[torch.tensor([0, 0, 2], device=DEV)]
+    b.keys, b.values = [[x[i] for i in (0, 2, 2, 0)] for x in (b.keys, b.values)]
+    b.lens = [50, 90, 90, 50]
+    b.shared = (b.shared[0], b.shared[1], *[[x[i] for i in (0, 0, 2)] for x in b.shared[2:]])
+    out, lse = b.call(seq_ids=ids, shared_ids=shared_ids)
+    b.check(out, lse)
 
 
 # ---- numbers on the device that do not fit ---------------------------------------------------------------------------
@@ -286,6 +323,21 @@ def test_replays_follow_the_lengths():
         b.check(*graphs[0][1])
         b.keys, b.values, b.lens = keys, values, full
         assert torch.equal(graphs[1][1][0], want_other[0]) and torch.equal(graphs[1][1][1], want_other[1])
+
+
+def test_captured_steps_that_share_their_memory():
+    """Two graphs of one memory pool, whose workspaces may be the same bytes, replayed in turn."""
+    batches = Batch(31, [300] * 6, [1] * 6, [(0, 6, 900)], 4, 4, 128, 16), Batch(32, [20, 700], [2, 3], [(0, 2, 64)], 4, 4, 128, 16)
+    want = [run(b) for b in batches]
+    graphs, got = [torch.cuda.CUDAGraph() for _ in batches], []
+    for graph, b in zip(graphs, batches):
+        with torch.cuda.graph(graph, pool=graphs[0].pool() if got else None):
+            got.append(b.call())
+    for turn in (0, 1, 1, 0, 1):
+        for x in got[turn]:
+            x.zero_()
+        graphs[turn].replay()
+        assert torch.equal(got[turn][0], want[turn][0]) and torch.equal(got[turn][1], want[turn][1])
 
 
 def test_two_calls_on_two_streams_at_once():

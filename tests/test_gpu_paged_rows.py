@@ -39,6 +39,12 @@ def test_rows(n, hq, hk, d, rotary, axes, adjacent, norm):
             check_rows(got, x, positions.tolist(), freqs, of, adjacent, None if w is None else w.double().numpy(), 1e-5)
 
 
+@pytest.mark.parametrize("n,hq,hk,d", [(400, 150, 150, 128), (3000, 9, 8, 64), (8000, 1, 1, 128)])
+def test_rows_of_a_token_in_chunks(n, hq, hk, d):
+    """Many tokens of many heads: several warps a token, chunks that begin among the queries and end among the keys."""
+    test_rows(n, hq, hk, d, d, 2, False, "bf16")
+
+
 def test_only_one_of_the_norms():
     g = gen(5)
     q, k, w = rows(6, 2, 128, g), rows(6, 2, 128, g), weight(128, g, "bf16")
