@@ -8,8 +8,6 @@
 //
 // Per tile of 64 keys: S[128 x 64] = Q K^T and O[128 x D] += P V by tcgen05.mma, Q, K and V in shared memory (K and V by tensor-map
 // copies of pages), S, P and O in tensor memory.  Four warps hold a row per thread, one issues products, one fetches.
-// Units of 60 rows or fewer hold them two or four times (rows r and r + 64, or r + 32 and so on): every copy weighs another half or
-// quarter of a tile's keys, so that all four warps take part in the exponentials; the copies are added up when the unit ends.
 
 #include "qc_paged_few.cuh"
 #include "qc_quant.h"
@@ -17,7 +15,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <type_traits>
 
 namespace qc {
 namespace {
@@ -30,10 +27,6 @@ constexpr int kUnits = 4;        // units that are known to the block at a time
 constexpr int kMeta = 8;         // tiles whose places are
 constexpr uint32_t kScoresAt = 0, kOutAt = 128, kColumns = 256;   // tensor memory: two score buffers of 64 columns, D of the sums
 
-// How often a unit's rows are held, every 32, 64 or 128 rows: as often as the copies' sums, 32 elements at a time, fit the place where
-// they meet.
-__device__ __forceinline__ int copies_of(int n_here) { return n_here <= 30 ? 4 : n_here <= 60 ? 2 : 1; }
-
 struct Meta {
   int32_t y[4];                  // of a tile's pages: the first row in the pool, -1: the page is not there
   int32_t on, shared;            // blocks of 16 keys that are there
@@ -43,9 +36,7 @@ template <int D>
 struct Shape {
   static constexpr int kRing = D == 128 ? 2 : 4;      // tiles of K, and of V, under way
   static constexpr uint32_t kTile = kKeys * D * 2, kHalf = kKeys * 128, kQ = kRows * D * 2, kQHalf = kRows * 128;
-  // where the copies' sums meet, their references behind them
-  static constexpr uint32_t kMeet = kQ + 2 * kRing * kTile, kMeetBytes = 15616, kRefs = kMeet + kMeetBytes;
-  static constexpr uint32_t kTiles = kRefs + kRows * 8;
+  static constexpr uint32_t kLarge = kQ + 2 * kRing * kTile, kSmall = kBlock / 32 * Ring<D>::kBytes, kTiles = kLarge > kSmall ? kLarge : kSmall;
 };
 
 struct Control {
@@ -89,12 +80,6 @@ __device__ __forceinline__ void scores(uint32_t tmem_d, uint64_t a, uint64_t b, 
   }
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(taddr));
-}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Whether all rows' threads say so.  Rows' warps go on together or not at all, so that none waits at a barrier for
@@ -126,7 +111,7 @@ template <int D>
 __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_constant__ Args A) {
   using Z = Shape<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kRing * Z::kTile, sMeet = sQ + Z::kMeet;
+  const uint32_t sQ = smem_u32(smem), sK = sQ + Z::kQ, sV = sK + Z::kRing * Z::kTile;
   Control& C = *reinterpret_cast<Control*>(smem + Z::kTiles);
   volatile int32_t& failed = C.failed;
   constexpr bool kLong = Z::kRing > 2;      // rings of two are free when the score buffer, or its weights, are
@@ -371,24 +356,22 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       }
     };
     uint32_t t0 = 0;      // tiles of the units before
-    // a unit as this thread sees it: its row, of n_here that are held `copies` times
+    const int row = threadIdx.x;
+    // a unit as this thread sees it
     struct Mine {
-      int n_here, tiles, first, len, all_see, shared;
-      int copies, row, copy, seen;
+      int n_here, tiles, first, len, all_see, shared, seen;
       bool real;
     };
     const auto take = [&](uint32_t n, Mine& x) {
       const Unit& u = C.units[n % kUnits];
       x.n_here = u.n_here, x.tiles = u.tiles, x.first = u.first, x.len = u.len, x.all_see = u.all_see, x.shared = u.shared;
-      x.copies = copies_of(x.n_here);
-      x.copy = threadIdx.x >> (x.copies == 4 ? 5 : x.copies == 2 ? 6 : 7), x.row = threadIdx.x & (x.copies == 4 ? 31 : x.copies == 2 ? 63 : 127);
-      x.real = x.row < x.n_here;
-      x.seen = seen_by(A, u, query_of(A, u, x.row));
+      x.real = row < x.n_here;
+      x.seen = seen_by(A, u, query_of(A, u, row));
     };
     // the unit's queries, from their places straight into shared memory; rows that are none keep what was there
     const auto ask_query = [&](uint32_t n) {
       const Unit& u = C.units[n % kUnits];
-      const int row = threadIdx.x & (kRows / copies_of(u.n_here) - 1), query = query_of(A, u, row);
+      const int query = query_of(A, u, row);
       const Stream& S = A.stream[u.shared];
       const uint16_t* p = S.q + (u.token0 + query) * S.q_stride + static_cast<int64_t>(head_of(A, u, row, query)) * D;
       if (row < u.n_here) {
@@ -411,41 +394,27 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       if (x.tiles == 0) break;
       float ref = -INFINITY, sum = 0.f;
       bool more = false;      // units
-      const bool idle = x.copies == 1 && warp * 32 >= x.n_here;      // a warp without rows
-      const auto weigh = [&](auto tag, int t, uint32_t gt, uint32_t on, bool masked) {
-        constexpr int REP = decltype(tag)::value, N = kKeys / REP;
+      const bool idle = warp * 32 >= x.n_here;      // a warp without rows
+      const auto weigh = [&](int t, uint32_t gt, uint32_t on, bool masked) {
         const uint32_t at = t_row + kScoresAt + (gt & 1u) * kKeys;
-        const int col0 = REP == 1 ? 0 : x.copy * N;
-        float p[N];
-        if constexpr (REP == 1) {
+        float p[kKeys];
+        {
           uint32_t r0[32], r1[32];
           tmem_ld32_nowait(at, r0);
           tmem_ld32_nowait(at + 32, r1);
           tmem_wait_ld();
 #pragma unroll
           for (int j = 0; j < 32; ++j) p[j] = __uint_as_float(r0[j]), p[32 + j] = __uint_as_float(r1[j]);
-        } else if constexpr (REP == 2) {
-          uint32_t r[32];
-          tmem_ld32(at + col0, r);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) p[j] = __uint_as_float(r[j]);
-        } else {
-          uint32_t r[16];
-          tmem_ld16(at + col0, r);
-          tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) p[j] = __uint_as_float(r[j]);
         }
         if (masked) {
-          const int left = x.seen - (t * kKeys + col0);
-          const uint32_t here = on >> (col0 / 16);
+          const int left = x.seen - t * kKeys;
 #pragma unroll
-          for (int j = 0; j < N; ++j)
-            if (j >= left || !(here >> (j / 16) & 1u)) p[j] = -INFINITY;
+          for (int j = 0; j < kKeys; ++j)
+            if (j >= left || !(on >> (j / 16) & 1u)) p[j] = -INFINITY;
         }
         float mx[4] = {p[0], p[1], p[2], p[3]};
 #pragma unroll
-        for (int j = 4; j < N; j += 2) mx[(j >> 1) & 3] = max3(mx[(j >> 1) & 3], p[j], p[j + 1]);
+        for (int j = 4; j < kKeys; j += 2) mx[(j >> 1) & 3] = max3(mx[(j >> 1) & 3], p[j], p[j + 1]);
         const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * A.scale_log2;   // (the scale is positive)
         float corr = 1.f;
         if ((top > ref + kRescale || ref == -INFINITY) && top != -INFINITY) {
@@ -455,7 +424,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         const float less = ref == -INFINITY ? 0.f : -ref;
         float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int j = 0; j < N; j += 2) {
+        for (int j = 0; j < kKeys; j += 2) {
           const float2 y = fma2(make_float2(p[j], p[j + 1]), make_float2(A.scale_log2, A.scale_log2), make_float2(less, less));
           p[j] = ex2_approx(y.x);
           p[j + 1] = ex2_approx(y.y);
@@ -478,11 +447,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         }
         uint32_t w[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          constexpr int kEach = N / 2;
-          const uint32_t y = pack_bf16x2(p[j % kEach * 2], p[j % kEach * 2 + 1]);
-          w[j] = REP == 1 || j / kEach == x.copy ? y : 0u;      // (the other copies' keys weigh nothing in this one)
-        }
+        for (int j = 0; j < 32; ++j) w[j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
         tmem_st32(at, w);
         tmem_wait_st();
       };
@@ -500,12 +465,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         }
         const uint32_t on = *reinterpret_cast<volatile int32_t*>(&C.meta[gt % kMeta].on);
         const int left = x.len - t * kKeys;
-        if (!idle) {
-          const bool masked = on != 15u || (t + 1) * kKeys > x.all_see;
-          if (x.copies == 4) weigh(std::integral_constant<int, 4>{}, t, gt, on, masked);
-          else if (x.copies == 2) weigh(std::integral_constant<int, 2>{}, t, gt, on, masked);
-          else weigh(std::integral_constant<int, 1>{}, t, gt, on, masked);
-        }
+        if (!idle) weigh(t, gt, on, on != 15u || (t + 1) * kKeys > x.all_see);
         if (on != 15u || left < kKeys) {      // values that no token has may be anything: a weight of 0 does not cancel a NaN
           const uint32_t v = gt % Z::kRing;
           wait_on(&C.v[v], (gt / Z::kRing) & 1u);
@@ -536,91 +496,24 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
       const auto sums_of = [&](int row) -> float* { return u.place < 0 ? A.rows + place_of(A, u, row) * D : A.pieces + (piece + row) * D; };
       const auto ml_of = [&](int row) -> float2* { return u.place < 0 ? A.row_ml + place_of(A, u, row) : A.piece_ml + piece + row; };
       bool strange = false;      // a sum that is no finite number although its row's weights are numbers
-      const auto flag = [&](int row) { atomicOr(&C.redo[row >> 5], 1u << (row & 31)), strange = true; };
-      if (x.copies == 1) {
+      if (!idle) {
         bool found = false;
-        if (!idle) {
-          float* const to = sums_of(x.real ? x.row : 0);
+        float* const to = sums_of(x.real ? row : 0);
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t r[32];
-            tmem_ld32(t_row + kOutAt + c, r);
-            float2 none[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};      // (0 times what is no finite number is no number)
+        for (int c = 0; c < D; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(t_row + kOutAt + c, r);
+          float2 none[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};      // (0 times what is no finite number is no number)
 #pragma unroll
-            for (int j = 0; j < 32; j += 2)
-              none[j / 2 & 1] = fma2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), make_float2(0.f, 0.f), none[j / 2 & 1]);
-            found |= !((none[0].x + none[0].y) + (none[1].x + none[1].y) == 0.f);
-            if (x.real)
+          for (int j = 0; j < 32; j += 2)
+            none[j / 2 & 1] = fma2(make_float2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), make_float2(0.f, 0.f), none[j / 2 & 1]);
+          found |= !((none[0].x + none[0].y) + (none[1].x + none[1].y) == 0.f);
+          if (x.real)
 #pragma unroll
-              for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j);
-          }
-          if (x.real) *ml_of(x.row) = make_float2(ref, sum);
+            for (int j = 0; j < 32; j += 8) store_32(to + c + j, r + j);
         }
-        if (found && x.real && isfinite(sum)) flag(x.row);
-      } else {
-        // The copies' sums meet in shared memory: whole rows, halves or quarters of all rows at a time, as they fit.
-        const int held = x.copies * x.n_here, mine = x.copy * x.n_here + x.row;
-        float2* const refs = reinterpret_cast<float2*>(smem + Z::kRefs);      // [copies][n_here]
-        // elements c0 to c0 + kCols of all rows, from all copies
-        const auto gather = [&](auto cols_tag, auto copies_tag, int c0) {
-          constexpr int kCols = decltype(cols_tag)::value, kChunks = kCols / 4, kCopies = decltype(copies_tag)::value;
-          for (int i = threadIdx.x; i < x.n_here * kChunks; i += kRows) {
-            const int row = i / kChunks, chunk = i % kChunks;
-            float2 z[kCopies];
-            uint4 v[kCopies];
-            float top = -INFINITY, all = 0.f;
-#pragma unroll
-            for (int k = 0; k < kCopies; ++k) {
-              const int at = k * x.n_here + row;
-              z[k] = refs[at], v[k] = lds128(sMeet + at * (kCols * 4) + ((chunk ^ (at & 7)) << 4));
-              top = fmaxf(top, z[k].x);
-            }
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < kCopies; ++k) {
-              const float f = z[k].x == -INFINITY ? 1.f : ex2_approx(z[k].x - top);      // (a sum on no reference is no number)
-              if (z[k].y != 0.f) {
-                all = fmaf(z[k].y, f, all);
-                y.x = fmaf(__uint_as_float(v[k].x), f, y.x), y.y = fmaf(__uint_as_float(v[k].y), f, y.y);
-                y.z = fmaf(__uint_as_float(v[k].z), f, y.z), y.w = fmaf(__uint_as_float(v[k].w), f, y.w);
-              }
-            }
-            reinterpret_cast<float4*>(sums_of(row) + c0)[chunk] = y;
-            if (c0 + chunk == 0) *ml_of(row) = make_float2(top, all);
-            if (!(isfinite(y.x) && isfinite(y.y) && isfinite(y.z) && isfinite(y.w)) && isfinite(all)) flag(row);
-          }
-        };
-        const auto meet = [&](auto cols_tag, auto copies_tag, int c0) {
-          constexpr int kCols = decltype(cols_tag)::value, kStep = kCols < 64 ? kCols : 64;
-#pragma unroll 1
-          for (int c = 0; c < kCols; c += kStep) {
-            uint32_t r[kStep / 32][32];
-#pragma unroll
-            for (int i = 0; i < kStep / 32; ++i) tmem_ld32_nowait(t_row + kOutAt + c0 + c + i * 32, r[i]);
-            tmem_wait_ld();
-            if (x.real) {
-#pragma unroll
-              for (int j = 0; j < kStep / 4; ++j)
-                sts128(sMeet + mine * (kCols * 4) + (((c / 4 + j) ^ (mine & 7)) << 4), make_uint4(r[j / 8][j % 8 * 4], r[j / 8][j % 8 * 4 + 1], r[j / 8][j % 8 * 4 + 2], r[j / 8][j % 8 * 4 + 3]));
-            }
-          }
-          rows_barrier();
-          gather(cols_tag, copies_tag, c0);
-        };
-        const auto meet_all = [&](auto copies_tag) {
-          if (held * D * 4 <= static_cast<int>(Z::kMeetBytes)) {
-            meet(std::integral_constant<int, D>{}, copies_tag, 0);
-          } else {
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              if (c) rows_barrier();      // (what was there has been read)
-              meet(std::integral_constant<int, 32>{}, copies_tag, c);
-            }
-          }
-        };
-        if (x.real) refs[mine] = make_float2(ref, sum);
-        if (x.copies == 4) meet_all(std::integral_constant<int, 4>{});
-        else meet_all(std::integral_constant<int, 2>{});
+        if (x.real) *ml_of(row) = make_float2(ref, sum);
+        if (found && x.real && isfinite(sum)) atomicOr(&C.redo[row >> 5], 1u << (row & 31)), strange = true;
       }
       if (rows_any(strange)) {      // rare: rows whose sums a value behind a weight of 0 may have spoiled, by hand
         for (int row = warp; row < x.n_here; row += 4) {
