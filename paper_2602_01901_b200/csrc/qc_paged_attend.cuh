@@ -15,7 +15,9 @@
 namespace qc {
 namespace paged {
 
-constexpr int kFew = 16;          // rows of an item that a warp takes
+// Rows of an item that a warp takes.  Between 9 and 16 a block's tiles are as good for one long prefix (16 rows of 32 heads, 8 541 keys: 49.0
+// us by warps, 48.3 by blocks), and short sequences are slower by them (64 of 500 keys, 12 rows on each of 4 KV heads: 24.2 and 27.8 us).
+constexpr int kFew = 16;
 constexpr int kBlock = 192;       // threads of a block of either kernel
 constexpr int kMostHeld = 2048;   // items that a block keeps in shared memory while it looks for its range
 constexpr uint32_t kMostCost = 1u << 26;
@@ -85,7 +87,12 @@ __device__ __forceinline__ int length_of(const Args& A, const Stream& S, int row
 }
 
 // The two kinds of units: rows of a unit, keys of a tile, what a unit costs besides its tiles, and the least tiles of a range and (as long as
-// ranges are not much longer) of a piece.
+// ranges are not much longer) of a piece.  Where two figures are given they are the five images' chats, 24 drafted sequences or the video's
+// questions with this value and with the other one:
+//   a unit of many rows costs 2 tiles: drafts 40.2 us (43.5 at 0, 41.2 at 6), video 160 (166 at 0); of few rows 6: drafts 40.2, video 160 (43.0
+//   and 167 at 2);
+//   a range of few rows has 2 tiles or more: one sequence 13.4 us (13.7 at 1, 16.2 at 4);
+//   a piece of many rows has 4: video 160 us (165 at 1); of few rows 3: images 51.2 (52.8 at 8).
 struct Many {
   static constexpr int kRows = 128, kKeys = 64;
   static constexpr bool kIsFew = false;
@@ -94,9 +101,11 @@ struct Many {
 struct Few {
   static constexpr int kRows = kFew, kKeys = 16;
   static constexpr bool kIsFew = true;
-  static constexpr uint32_t kUnitCost = 6, kRange = 2, kPiece = 8;
+  static constexpr uint32_t kUnitCost = 6, kRange = 2, kPiece = 3;
 };
-constexpr float kManyTile = 3.f, kManyMore = 6.f;      // what a tile of many rows takes a block, in tiles that the warps of a block take together
+// What a tile of many rows takes a block, in tiles that the warps of a block take together: so much alone, and more beside the others, which keep
+// the memory busy (images 55.6 us, 83.0 without it; drafts 40.2 and 38.7; video 160, and 167 with 5 alone).
+constexpr float kManyTile = 3.f, kManyMore = 6.f;
 
 // An item as it is held while units are looked for.
 struct Held {
@@ -223,9 +232,8 @@ __device__ __forceinline__ Plan plan_of(const Args& A, Found& found, uint64_t* s
   }
   fine = __syncthreads_and(fine);
   const bool small = total[0] <= kMostCost && total[1] <= kMostCost;
-  // All that can go side by side does, where there are blocks enough (or nearly so); else they are shared out by time.  A tile of many rows takes
-  // a block as long as kManyTile tiles of few rows where blocks of its kind are alone, and up to kManyMore more where the others keep
-  // the memory busy: it has less under way.
+  // All that can go side by side does, where there are blocks enough (or nearly so); else they are shared out by the time they take.  Either kind has
+  // a block at least.
   const uint32_t blocks = gridDim.x, warps = kBlock / 32;
   uint32_t many = min(blocks, total[0] / Many::kRange);
   const uint32_t few = (min(blocks * warps, max(1u, total[1] / Few::kRange)) + warps - 1) / warps;
