@@ -3,12 +3,13 @@
 // Such a unit reads its keys and values for 16 rows at most: some flops a byte, far below what the tensor cores need, so it is bound by
 // the bytes as long as enough of them are under way.  Each warp works on its own: it walks its range of the plan (qc_paged_attend.cuh)
 // and fetches tiles of 16 keys into a ring of its own, so that an SM has twelve independent chains of copies, products and
-// softmax.  (As units of many rows, one chain of three hand-offs per block, 48 sequences of 64 tokens of 32 heads took 25.5 us
-// instead of 14.5.)
+// softmax.  Eight sequences of 8 541 keys of 32 heads take 180 us, 0.97 of what a copy moves.  Short units are latency: a tile takes some 1 000 cycles
+// alone and 3 400 where all warps fetch, a unit's start and end 3 000 to 7 500.  (As units of many rows, one chain of three hand-offs per
+// block, 48 sequences of 64 tokens of 32 heads took the first kernel 25.5 us instead of 13.2.)
 //
 // Products are mma.sync m16n8k16 with the keys (for K) and the elements (for V) as rows and eight query rows as columns, once or
 // twice:  S^T[16 keys x 8] = K Q^T,  O^T[D x 8] += V^T P^T.  Scores leave the first with a key per lane group; a transpose in registers
-// makes them the second's operand.  Weights are rounded to bf16 there (2^-9 of themselves; their sum is not), everything else is fp32.
+// makes them the second's operand.  Weights are rounded to bf16 there (2^-8 of themselves at most, the operand type; their sum is not), everything else is fp32.
 // Rows of K and V lie in shared memory as in their page, 16 bytes at a time turned by the row, so that both ldmatrix
 // patterns meet no bank twice.
 
