@@ -585,7 +585,8 @@ typedef struct qc_paged_attend_args {
   qc_paged_stream shared;        /* all null: no sequence has a prefix */
   void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim], over no other argument */
   float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
-  void* workspace_dev;           /* qc_paged_workspace_bytes, 256-byte aligned; need not be cleared; one call at a time */
+  void* workspace_dev;           /* qc_paged_workspace_bytes of these sizes and lists, 256-byte aligned; need not be cleared; one call at a
+                                    time */
   size_t workspace_bytes;
   int32_t* status_dev;           /* optional status word */
 } qc_paged_attend_args;

@@ -744,7 +744,9 @@ Layout layout_of(const qc_paged_attend_args* a) {
   const auto up = [](size_t n) { return (n + 255) & ~static_cast<size_t>(255); };
   const size_t heads = static_cast<size_t>(a->n_tokens) * a->n_q_heads * (a->n_groups ? 2 : 1);
   Layout w{};
-  const size_t pieces = static_cast<size_t>(kMostWorkers) * 2 * kRows, few_pieces = static_cast<size_t>(kMostWorkers) * (kBlock / 32) * 2 * kFew, row = a->head_dim * 4;
+  const int64_t most_rows = static_cast<int64_t>(a->n_groups ? a->n_tokens : std::min(a->starts_dev ? a->max_queries : 1, a->n_tokens)) * (a->n_q_heads / a->n_kv_heads);
+  const size_t pieces = most_rows > kFew ? static_cast<size_t>(kMostWorkers) * 2 * kRows : 0;      // (no units of many rows: none of theirs)
+  const size_t few_pieces = static_cast<size_t>(kMostWorkers) * (kBlock / 32) * 2 * kFew, row = a->head_dim * 4;
   w.records = 256;
   w.row_ml = w.records + up(static_cast<size_t>(a->n_seqs) * 2 * sizeof(Record));
   w.piece_ml = w.row_ml + up(heads * 8);
