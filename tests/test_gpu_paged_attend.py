@@ -94,6 +94,24 @@ def test_many_groups_of_one():
     run(Batch(7, [3] * n, [1] * n, [(i, i + 1, i % 130) for i in range(n)], 1, 3, 128, 16, lazy=True))
 
 
+def test_as_many_groups_as_sequences():
+    n = qc.QC_PAGED_MAX_SEQS
+    b = Batch(33, [i % 7 for i in range(n)], [1] * n, [(i, i + 1, i % 23) for i in range(n)], 1, 2, 64, 16)
+    out, lse = b.call()
+    assert int(b.table.state[1]) == qc.QC_OK
+    b.check(out, lse, list(range(0, n, 61)) + [n - 1])
+
+
+@pytest.mark.parametrize("hkv,group", [(1024, 1), (1, 1024), (64, 16)])
+def test_the_most_heads(hkv, group):
+    run(Batch(34, [70, 3, 0], [1, 2, 1], [(0, 2, 90)], hkv, group, 64, 16))
+
+
+def test_the_most_queries():
+    n = qc.QC_PAGED_MAX_QUERIES
+    run(Batch(35, [n, 500, 40, 200], [n, n, 33, n - 1], [(1, 4, 300)], 2, 6, 128, 32))
+
+
 def test_a_prefix_is_the_same_as_rows_of_ones_own():
     """With the same queries for both streams, a prefix of a group and a copy of it ahead of each sequence's own rows give the same, but for roundings."""
     n, p, own, d, hkv, group = 6, 333, [1, 20, 64, 100, 131, 7], 128, 2, 4
