@@ -808,11 +808,22 @@ cudaError_t launch(const Args& A, int device, cudaStream_t stream) {
   return rows <= kJoinBlock * sms ? launch_join<D, 32, 8>(A, stream) : rows <= kJoinWarp * sms ? launch_join<D, 32, 1>(A, stream) : launch_join<D, 8, 1>(A, stream);
 }
 
-// Whether the rows written lie over rows of queries.
-bool over_queries(const qc_paged_stream& s, const qc_paged_attend_args* a) {
-  const uint64_t row = static_cast<uint64_t>(a->n_q_heads) * a->head_dim * 2, n = a->n_tokens;
-  const uint64_t q = reinterpret_cast<uint64_t>(s.q_dev), out = reinterpret_cast<uint64_t>(a->out_dev);
-  return q < out + row * n && out < q + static_cast<uint64_t>(s.q_stride) * 2 * (n - 1) + row;
+// Whether `bytes` at `p`, which the call writes, lie over anything that it reads.
+bool over_inputs(const qc_paged_attend_args* a, const void* p, uint64_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p), row = static_cast<uint64_t>(a->n_q_heads) * a->head_dim * 2, n = a->n_tokens;
+  const auto over = [&](const void* x, uint64_t size) {
+    const uint64_t y = reinterpret_cast<uint64_t>(x);
+    return y && y < at + bytes && at < y + size;
+  };
+  for (const qc_paged_stream* s : {&a->own, &a->shared}) {
+    const uint64_t pool = static_cast<uint64_t>(s->n_pages) * a->page_size * a->n_kv_heads * a->head_dim * 2, rows = s->rows;
+    if (over(s->q_dev, static_cast<uint64_t>(s->q_stride) * 2 * (n - 1) + row) || over(s->k_pool_dev, pool) || over(s->v_pool_dev, pool) ||
+        over(s->pages_dev, rows * s->max_pages * 4) || over(s->lens_dev, rows * 4))
+      return true;
+  }
+  const uint64_t seqs = a->n_seqs, groups = a->n_groups;
+  return over(a->seq_ids_dev, seqs * 4) || over(a->starts_dev, seqs * 4 + 4) || over(a->groups_dev, groups * 4 + 4) || over(a->shared_ids_dev, groups * 4) ||
+         over(a->status_dev, 4);
 }
 
 }  // namespace
@@ -847,7 +858,12 @@ extern "C" int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_p
   }
   if (args->workspace_bytes < workspace_bytes(args) || !args->workspace_dev) return QC_ERR_INVALID_ARG;
   if (args->n_tokens == 0) return QC_OK;
-  if (over_queries(args->own, args) || (shared && over_queries(args->shared, args))) return QC_ERR_INVALID_ARG;
+  const uint64_t rows = static_cast<uint64_t>(args->n_tokens) * args->n_q_heads, out_bytes = rows * args->head_dim * 2;
+  if (over_inputs(args, args->out_dev, out_bytes)) return QC_ERR_INVALID_ARG;
+  if (args->lse_out_dev) {
+    const uint64_t out = reinterpret_cast<uint64_t>(args->out_dev), lse = reinterpret_cast<uint64_t>(args->lse_out_dev);
+    if (over_inputs(args, args->lse_out_dev, rows * 4) || (out < lse + rows * 4 && lse < out + out_bytes)) return QC_ERR_INVALID_ARG;
+  }
   A.ids = args->seq_ids_dev, A.starts = args->starts_dev, A.groups = args->groups_dev, A.shared_ids = args->shared_ids_dev;
   A.out = static_cast<uint16_t*>(args->out_dev), A.lse = args->lse_out_dev, A.status = args->status_dev;
   uint8_t* const work = static_cast<uint8_t*>(args->workspace_dev);

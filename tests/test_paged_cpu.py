@@ -157,6 +157,26 @@ def test_attention_refuses_what_it_can_see_on_the_host(change, status):
     assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, attend_args(**change))) == status
 
 
+FAR = 3 * BIG
+
+
+@pytest.mark.parametrize("change", [
+    dict(own=dict(k_pool_dev=FAR)), dict(own=dict(v_pool_dev=FAR - 2 * 9 * 16 * 128 * 2 + 16)), dict(own=dict(pages_dev=FAR + 28)), dict(own=dict(lens_dev=FAR - 8)), dict(seq_ids_dev=FAR - 4),
+    dict(starts_dev=FAR - 8), dict(status_dev=FAR + 4), dict(shared=dict(k_pool_dev=FAR + 16)), dict(shared={}, groups_dev=FAR - 4), dict(shared={}, shared_ids_dev=FAR),
+    dict(shared=dict(q_dev=FAR - 1024)),
+])
+def test_attention_writes_over_nothing_that_it_reads(change):
+    """Rows written (2048 bytes here), or their sums of exponentials (32), against every other argument."""
+    for mine in (dict(out_dev=FAR), dict(lse_out_dev=FAR)):
+        assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, attend_args(**mine, **change))) == qc.QC_ERR_INVALID_ARG
+    assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, attend_args(out_dev=FAR + BIG, lse_out_dev=FAR + 2 * BIG, **change))) == qc.QC_ERR_CUDA
+
+
+@pytest.mark.parametrize("at,status", [(FAR - 32, 5), (FAR - 28, 1), (FAR + 2044, 1), (FAR + 2048, 5)])
+def test_the_two_outputs_of_attention_lie_apart(at, status):
+    assert status_of(lambda: qc.qc_paged_attend(NO_DEVICE, 0, attend_args(out_dev=FAR, lse_out_dev=at))) == status
+
+
 def test_attention_refuses_a_workspace_that_is_too_small(lib):
     a = attend_args(shared={})
     need = qc.qc_paged_workspace_bytes(a)
