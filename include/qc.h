@@ -513,8 +513,8 @@ int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend
 /* A row x of one token and head becomes y = x / sqrt(mean x^2 + eps) * w where its norm weights are given, and then each pair i of
  * its first rotary_dim elements is turned by the angle positions[axes[i]][token] * freqs[i]:
  *   (a, b) -> (a cos - b sin, b cos + a sin),  elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where `adjacent`.
- * In fp32 throughout, rounded once; an angle is exact to 2^-30 turns for every position.  Squares are summed in fp32: elements are
- * below 2^60 in size.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
+ * In fp32 throughout, rounded once; an angle is off by a rounding to fp32, 2^-26 turns at most, at every position (for frequencies
+ * below 2^32 in size).  Squares are summed in fp32: elements are below 2^60 in size.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
  * Rows are bf16 [n_tokens][heads][head_dim], heads dense, tokens `stride` elements apart (multiples of 8, pointers 16-byte
  * aligned).  An output lies over its own input (same pointer and stride) or over nothing. */
 typedef struct qc_rotate_args {

@@ -7,8 +7,10 @@
 // decides, since rows under way are what hides the memory: 48 registers, 40 warps an SM.  10 813 tokens of 64 heads of 128 take 59.8 us, 92 % of
 // what a copy moves (factors in registers, 96 of them, 78 us; blocks of some tokens that share angles, weights read for each row,
 // 71); with V into pages 88.7 us of 82.3.  One token takes 3.2 us in a graph, a launch's latency.
-// An angle is counted in turns, as a fraction of 64 bits: freq / 2 pi modulo 1 once, times the position modulo 2^64, so a far position loses
-// nothing (in fp32 position 100 000 is 6e-3 radians off), and sine and cosine are taken of a number in [-1, 1) half turns.
+// An angle is counted in turns, as a fraction of 64 bits: freq / 2 pi modulo 1 once, times the position modulo 2^64, and sine and cosine are taken of
+// a number in [-1, 1) half turns.  The fraction is off by less than 2^-64, a position's angle by 2^-33 turns; its rounding to fp32, 2^-26
+// turns at most, is all that is seen (in fp32 throughout position 100 000 is 6e-3 radians off; with freq / 2 pi in one double position 2^31 was off by
+// 4e-6 turns for frequencies to 100).
 // A row is held by D / 16 lanes, two 16-byte vectors each: those whose pairs the lane turns, so that no element changes lanes.
 // The squares' sum takes 3 exchanges.
 
@@ -48,8 +50,10 @@ struct RotateArgs {
 
 // The angle of a pair at a position, as (cos, sin).
 __device__ __forceinline__ float2 turn_of(float freq, int32_t position) {
-  const double turns = static_cast<double>(freq) * 0.15915494309189533577;
-  const unsigned long long part = __double2ull_rn((turns - floor(turns)) * 18446744073709551616.0);
+  // freq / 2 pi in two doubles: what the first leaves off counts too, times the position
+  constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57, k64 = 18446744073709551616.0;
+  const double f = freq, turns = f * kTurn, rest = fma(f, kTurnRest, fma(f, kTurn, -turns));
+  const unsigned long long part = __double2ull_rn((turns - floor(turns)) * k64) + static_cast<unsigned long long>(__double2ll_rn(rest * k64));
   const unsigned long long at = part * static_cast<unsigned long long>(static_cast<long long>(position));
   float2 cs;
   sincospif(static_cast<float>(static_cast<int32_t>(at >> 32)) * 4.656612873077392578125e-10f, &cs.y, &cs.x);   // 2^-31
