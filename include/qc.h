@@ -516,7 +516,8 @@ int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend
  * In fp32 throughout, rounded once; an angle is off by a rounding to fp32, 2^-26 turns at most, at every position (for frequencies
  * below 2^32 in size).  Squares are summed in fp32: elements are below 2^60 in size.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
  * Rows are bf16 [n_tokens][heads][head_dim], heads dense, tokens `stride` elements apart (multiples of 8, pointers 16-byte
- * aligned).  An output lies over its own input (same pointer and stride) or over nothing. */
+ * aligned).  An output lies over its own input (same pointer and stride) or over nothing
+ * that the call reads or writes besides (QC_ERR_INVALID_ARG). */
 typedef struct qc_rotate_args {
   int32_t n_tokens, n_q_heads, n_kv_heads;
   int32_t head_dim;              /* 64 or 128 */

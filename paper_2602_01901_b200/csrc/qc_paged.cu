@@ -292,6 +292,15 @@ int32_t check_rotate(const qc_rotate_args* a, bool to_pool, RotateArgs& T) {
   return QC_OK;
 }
 
+// Whether a run of memory that a call writes lies over what it reads besides rows.
+bool over_tables(const qc_rotate_args* a, const Span& out) {
+  const uint64_t pairs = a->q_dev || a->k_dev ? a->rotary_dim / 2 : 0, weights = static_cast<uint64_t>(a->head_dim) * (a->norm_f32 ? 4 : 2);
+  const auto over = [&](const void* p, uint64_t bytes) { return bytes && meet(out, flat_span(p, bytes)); };
+  for (int axis = 0; pairs && axis < a->n_axes; ++axis)
+    if (over(a->positions_dev + axis * a->position_stride, static_cast<uint64_t>(a->n_tokens) * 4)) return true;
+  return over(a->freqs_dev, pairs * 4) || over(a->axes_dev, pairs * 4) || (a->q_dev && over(a->q_norm_dev, weights)) || (a->k_dev && over(a->k_norm_dev, weights));
+}
+
 // Whether what a call writes lies over anything but its own input.
 bool overlaps(const qc_rotate_args* a, const Span* more, int n_more) {
   const int n = a->n_tokens, d = a->head_dim;
@@ -300,6 +309,7 @@ bool overlaps(const qc_rotate_args* a, const Span* more, int n_more) {
   const auto same = [&](const Span& x, const Span& y) { return x.at == y.at && (x.stride == y.stride || n == 1); };
   if (meet(q_out, k_out) || meet(q_out, k) || meet(k_out, q)) return true;
   if ((meet(q_out, q) && !same(q_out, q)) || (meet(k_out, k) && !same(k_out, k))) return true;
+  if (over_tables(a, q_out) || over_tables(a, k_out)) return true;
   for (int i = 0; i < n_more; ++i)
     if (meet(q_out, more[i]) || meet(k_out, more[i])) return true;
   return false;
@@ -355,8 +365,8 @@ extern "C" int32_t qc_paged_append(int32_t device, void* cuda_stream, const qc_p
                        rows_span(args->v_dev, args->v_stride, r->n_kv_heads, r->head_dim, r->n_tokens)};
   for (const Span& s : ins)
     if (meet(kp, s) || meet(vp, s)) return QC_ERR_INVALID_ARG;
-  const Span more[3] = {ins[2], kp, vp};
-  if (meet(kp, vp) || overlaps(r, more, 3)) return QC_ERR_INVALID_ARG;
+  const Span more[4] = {ins[2], kp, vp, flat_span(args->slots_dev, static_cast<uint64_t>(r->n_tokens) * 4)};
+  if (meet(kp, vp) || meet(kp, more[3]) || meet(vp, more[3]) || over_tables(r, kp) || over_tables(r, vp) || overlaps(r, more, 4)) return QC_ERR_INVALID_ARG;
   T.v = {static_cast<const uint16_t*>(args->v_dev), args->v_stride, nullptr, 0, nullptr};
   T.hv = args->v_dev ? r->n_kv_heads : 0;
   T.k_pool = static_cast<uint16_t*>(args->k_pool_dev), T.v_pool = static_cast<uint16_t*>(args->v_pool_dev);
