@@ -602,11 +602,11 @@ int32_t qc_paged_workspace_bytes(const qc_paged_attend_args* args, size_t* bytes
  * does one whose scores are all minus infinity.  What the pools hold where no token is counts for nothing, whatever it is.
  * The work is divided by sizes alone, so a call gives the same bits each time.
  * All or nothing: rows out of range, starts or groups that do not ascend or reach outside, more queries than max_queries
- * (QC_ERR_INVALID_ARG in the status word) and batches of some 2^26 tiles of keys or more (QC_ERR_PLAN) leave out as it was; a tile is 64 keys,
- * counted per KV head and 128 query rows, or 16 where a sequence or a group has no more than 16 rows a KV head, which distinct pages
- * that fit on a device do not reach.  A page id that is not in the pool is not followed: its keys count as absent
- * (QC_ERR_BAD_PAGE).  A length beyond the table's room is cut to it (QC_ERR_PLAN).  Rows of out that belong to no sequence are
- * left as they are. */
+ * (QC_ERR_INVALID_ARG in the status word) and batches of too much work (QC_ERR_PLAN) leave out as it was.  Too much is a sum above 2^30
+ * (some seconds) over the prefixes and sequences that have keys and more than 16 query rows a KV head, of KV heads * ceil(rows / 128) *
+ * (ceil(keys / 64) + 2), or over those of 1 to 16 rows, of KV heads * (ceil(keys / 16) + 6).  A page id that is not in the pool is not
+ * followed: its keys count as absent (QC_ERR_BAD_PAGE).  A length beyond the table's room is cut to it, a negative one counts as 0
+ * (QC_ERR_PLAN).  Rows of out that belong to no sequence are left as they are. */
 int32_t qc_paged_attend(int32_t device, void* cuda_stream, const qc_paged_attend_args* args);
 
 const char* qc_status_string(int32_t status);

@@ -20,7 +20,7 @@ namespace paged {
 constexpr int kFew = 16;
 constexpr int kBlock = 192;       // threads of a block of either kernel
 constexpr int kMostHeld = 2048;   // items that a block keeps in shared memory while it looks for its range
-constexpr uint32_t kMostCost = 1u << 26;
+constexpr uint32_t kMostCost = 1u << 30;      // of a kind's units: sums of two such, and of one and a difference, fit in 32 bits
 
 struct Stream {
   const uint16_t* q;
@@ -198,31 +198,33 @@ __device__ __forceinline__ Plan plan_of(const Args& A, Found& found, uint64_t* s
   uint32_t total[2] = {0, 0};
   for (int i0 = 0; i0 < n_items; i0 += kBlock) {
     const int i = i0 + threadIdx.x;
-    uint64_t mine = 0;      // of few rows above, of many below
+    uint32_t mine[2] = {0, 0};
     Held h{};
     if (i < n_items) {
       bool ok;
       h = item_of(A, i, blockIdx.x == 0, ok);
-      mine = is_few(A, h.queries) ? static_cast<uint64_t>(cost_of<Few>(item_from<Few>(A, h))) << 32 : cost_of<Many>(item_from<Many>(A, h));
+      if (is_few(A, h.queries)) mine[1] = cost_of<Few>(item_from<Few>(A, h));
+      else mine[0] = cost_of<Many>(item_from<Many>(A, h));
       fine &= ok;
     }
-    uint64_t sum = mine;      // (32 items stay below 2^32 in either half)
+    uint32_t sum[2] = {mine[0], mine[1]};      // (what is too much stays kTooMuch; the costs before an item are of no use then)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
-    if (lane == 31) sums[warp] = sum;
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, sum[k], o);
+        if (lane >= o) sum[k] = min(kTooMuch, sum[k] + y);
+      }
+    if (lane == 31) sums[warp] = static_cast<uint64_t>(sum[1]) << 32 | sum[0];
     __syncthreads();
-    const uint64_t ahead = sum - mine;
-    uint32_t at[2] = {min(kTooMuch, total[0] + static_cast<uint32_t>(ahead)), min(kTooMuch, total[1] + static_cast<uint32_t>(ahead >> 32))};
+    uint32_t at[2] = {min(kTooMuch, total[0] + (sum[0] - mine[0])), min(kTooMuch, total[1] + (sum[1] - mine[1]))};
 #pragma unroll
     for (int w = 0; w < kBlock / 32; ++w)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t x = static_cast<uint32_t>(sums[w] >> (32 * k));
-        if (w < warp) at[k] = min(kTooMuch, at[k] + min(x, kTooMuch));
-        total[k] = min(kTooMuch, total[k] + min(x, kTooMuch));
+        if (w < warp) at[k] = min(kTooMuch, at[k] + x);
+        total[k] = min(kTooMuch, total[k] + x);
       }
     if (i < n_items) {
       found.before[0][i] = at[0], found.before[1][i] = at[1];

@@ -70,5 +70,6 @@ def attend(own: Stream, *, shared: Optional[Stream] = None, groups: Optional[tor
     once for its group.  ``causal``: the queries are the last tokens of their own stream, and none sees what is behind it.  Returns
     (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); a query that sees nothing gets 0 and minus infinity; tokens
     of no sequence stay what they were in ``out`` (where it is made here, anything).  ``out`` overlaps no other argument.  ``status``: an
-    int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``)."""
+    int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``): lists that do not fit, or too much work for a call, leave ``out`` as it
+    was, and only this word says so."""
     return _native().paged_attend(own, shared, groups, shared_ids, seq_ids, starts, max_queries, causal, scale, out, status)

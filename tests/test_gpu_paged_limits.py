@@ -1,0 +1,83 @@
+"""The most work that one attention call takes."""
+
+import math
+
+import pytest
+import torch
+
+from paged_util import DEV, attention, check_rows_of, gen, stream_of
+from paper_2602_01901_b200 import binding as qc
+from paper_2602_01901_b200 import paged
+
+pytestmark = pytest.mark.gpu
+LIMIT = 1 << 30
+
+
+def many_cost(hkv, rows, keys):
+    return hkv * -(-rows // 128) * (-(-keys // 64) + 2)
+
+
+def few_cost(hkv, keys):
+    return hkv * (-(-keys // 16) + 6)
+
+
+def same_everywhere(out, lse, parts, group, scale):
+    """Every row of a batch whose rows are all one and the same query over the same keys, against the one row in 64 bits; some of them by check_rows_of."""
+    for i in {0, 1, len(out) // 2, len(out) - 1}:
+        check_rows_of(out[i:i + 1], lse[i:i + 1], parts, group, scale, i)
+    # (the bounds of check_rows_of for this one row, for all of them at once)
+    want, want_lse, mass, size, n = attention(parts, group, scale)
+    e = size * (want.shape[-1] + 4) * 2.0 ** -23
+    rel = 2 * e + 2.0 ** -20 + (n + 64) * 2.0 ** -23
+    tol = (2.0 ** -8 * want.abs() + (2.0 ** -8 * (1 + 2.0 ** -7) + 2 * rel)[..., None] * mass).float()
+    lse_tol = (e + 2.0 ** -20 + (n + 64) * 2.0 ** -23 + 2.0 ** -22 * want_lse.abs()).float()
+    for a in range(0, len(out), 1 << 14):
+        assert ((out[a:a + (1 << 14)].float() - want.float()).abs() <= tol).all(), a
+        assert ((lse[a:a + (1 << 14)] - want_lse.float()).abs() <= lse_tol).all(), a
+
+
+def test_many_rows_past_2_to_the_26th_tiles():
+    """2048 sequences of 128 queries about one prefix: few keys, many rows."""
+    n, queries, hkv, group, d, keys = 2048, 128, 8, 8, 64, 32768
+    cost = many_cost(hkv, n * queries * group, keys)
+    assert 1 << 26 < cost < LIMIT
+    g = gen(1)
+    table, pools, k, v = stream_of([keys], [0], 1, hkv, d, 64, g)
+    own, own_pools, _, _ = stream_of([0], [0], 1, hkv, d, 64, g)
+    q = torch.randn(1, hkv * group, d, generator=g).bfloat16().to(DEV)
+    rows = q.expand(n * queries, hkv * group, d)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = paged.attend(paged.Stream(rows, *own_pools, own.pages, own.lens), shared=paged.Stream(rows, *pools, table.pages, table.lens),
+                            seq_ids=torch.zeros(n, dtype=torch.int32, device=DEV), starts=torch.arange(0, n * queries + 1, queries, dtype=torch.int32, device=DEV),
+                            max_queries=queries, status=status)
+    assert int(status) == qc.QC_OK
+    same_everywhere(out, lse, [(q, k[0], v[0], torch.tensor([keys], device=DEV))], group, 1 / math.sqrt(d))
+
+
+def test_few_rows_past_2_to_the_26th_tiles():
+    """2048 sequences that all are the same row of the table, of 1024 KV heads."""
+    n, hkv, d, keys = 2048, 1024, 64, 480
+    assert 1 << 26 < n * few_cost(hkv, keys) < LIMIT
+    g = gen(2)
+    table, pools, k, v = stream_of([keys], [0], 1, hkv, d, 16, g)
+    q = torch.randn(1, hkv, d, generator=g).bfloat16().to(DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = paged.attend(paged.Stream(q.expand(n, hkv, d), *pools, table.pages, table.lens), seq_ids=torch.zeros(n, dtype=torch.int32, device=DEV), status=status)
+    assert int(status) == qc.QC_OK
+    same_everywhere(out, lse, [(q, k[0], v[0], torch.tensor([keys], device=DEV))], 1, 1 / math.sqrt(d))
+
+
+@pytest.mark.parametrize("times", [1, 2])
+def test_a_batch_of_too_many_tiles_is_refused_and_leaves_everything_as_it_was(times):
+    """The same with 8 100 keys: 2^30 and some; of the prefix of a group for each sequence as well, so that the sum itself passes 2^31."""
+    n, hkv, d, keys = 2048, 1024, 64, 8128
+    assert n * few_cost(hkv, keys) > LIMIT
+    table = paged.PageTable.empty(1, keys // 16, 16, keys // 16)
+    pool = torch.zeros(keys // 16, hkv, 16, d, dtype=torch.bfloat16, device=DEV)
+    paged.table_extend(table, torch.tensor([keys], dtype=torch.int32, device=DEV), max_slots=keys)
+    q = torch.zeros(1, hkv, d, dtype=torch.bfloat16, device=DEV).expand(n, hkv, d)
+    zeros, own = torch.zeros(n, dtype=torch.int32, device=DEV), paged.Stream(q, pool, pool, table.pages, table.lens)
+    out, status = torch.full((n, hkv, d), 3.0, dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    shared = dict(shared=own, groups=torch.arange(n + 1, dtype=torch.int32, device=DEV), shared_ids=zeros) if times == 2 else {}
+    paged.attend(own, seq_ids=zeros, out=out, status=status, **shared)
+    assert int(status) == qc.QC_ERR_PLAN and (out == 3).all()
