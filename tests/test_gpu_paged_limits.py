@@ -1,11 +1,11 @@
-"""The most work that one attention call takes."""
+"""The most work that one attention call takes, and what it says of numbers on the device that it cuts or refuses."""
 
 import math
 
 import pytest
 import torch
 
-from paged_util import DEV, attention, check_rows_of, gen, stream_of
+from paged_util import DEV, Batch, attention, check_rows_of, gen, stream_of
 from paper_2602_01901_b200 import binding as qc
 from paper_2602_01901_b200 import paged
 
@@ -81,3 +81,36 @@ def test_a_batch_of_too_many_tiles_is_refused_and_leaves_everything_as_it_was(ti
     shared = dict(shared=own, groups=torch.arange(n + 1, dtype=torch.int32, device=DEV), shared_ids=zeros) if times == 2 else {}
     paged.attend(own, seq_ids=zeros, out=out, status=status, **shared)
     assert int(status) == qc.QC_ERR_PLAN and (out == 3).all()
+
+
+def room_of(b):
+    return b.table.pages.shape[1] * 16
+
+
+def test_a_length_beyond_the_table_is_cut_and_said():
+    """Every page of the table is there, so that nothing else is to be said."""
+    b = Batch(3, [40, 64], [1, 1], [(0, 1, 20)], 1, 2, 64, 16)
+    row, room = int(b.ids[1]), room_of(b)
+    have = torch.arange(room // 16, device=DEV) % b.pools[0].shape[0]
+    b.table.pages[row] = have.to(torch.int32)
+    for p in b.pools:
+        p.nan_to_num_(0.25)
+    b.keys[1], b.values[1] = (p[have].transpose(1, 2).flatten(0, 1) for p in b.pools)
+    b.table.lens[row] = room + 1000
+    b.lens[1] = room
+    out, lse = b.call()
+    assert int(b.table.state[1]) == qc.QC_ERR_PLAN
+    # (its keys may be sequence 0's pages too: what a page holds is what both see)
+    page = b.table.pages[int(b.ids[0])].long()
+    pos = torch.arange(40, device=DEV)
+    b.keys[0], b.values[0] = (p[page[pos // 16], :, pos % 16] for p in b.pools)
+    b.check(out, lse)
+
+
+def test_a_negative_length_counts_as_none_and_is_said():
+    b = Batch(4, [40, 64], [1, 1], [(0, 1, 20)], 1, 2, 64, 16)
+    b.table.lens[int(b.ids[0])] = -5
+    out, lse = b.call()
+    assert int(b.table.state[1]) == qc.QC_ERR_PLAN
+    b.keys[0], b.values[0], b.lens[0] = b.keys[0][:0], b.values[0][:0], 0
+    b.check(out, lse)
