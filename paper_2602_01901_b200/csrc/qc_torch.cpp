@@ -352,6 +352,13 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---- rows turned by their positions, bf16 pages ---------------------------------------------------------------------
 
+// A given tensor that a call has written: graphs that have kept it find out.  (In inference mode there is no count.)
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // Rotation (freqs, axes, adjacent) and positions into `r`.
 void rotation_of(qc_rotate_args& r, PyObject* rotation, PyObject* positions, int32_t index) {
   if (rotation == Py_None) {
@@ -435,7 +442,7 @@ PyObject* py_rotate(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     rotation_of(r, a[3], a[2], index);
     norms_of(r, a[4], a[5], a[6], index);
-    if (rows.size(0)) check(qc_rotate(index, stream_of(index), &r), "qc_rotate");
+    if (rows.size(0)) check(qc_rotate(index, stream_of(index), &r), "qc_rotate"), written(a[7]), written(a[8]);
     if (has_q && has_k) return pair(q, k);
     PyObject* one = THPVariable_Wrap(has_q ? q : k);
     if (!one) throw PythonError{};
@@ -484,7 +491,7 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     p.slots_dev = ints(a[2], "slots", index, rows.size(0));
     rotation_of(r, a[7], a[6], index);
     norms_of(r, a[8], a[9], a[10], index);
-    if (rows.size(0)) check(qc_paged_append(index, stream_of(index), &p), "qc_paged_append");
+    if (rows.size(0)) check(qc_paged_append(index, stream_of(index), &p), "qc_paged_append"), written(a[0]), written(a[1]), written(a[11]);
     if (!has_q) Py_RETURN_NONE;
     PyObject* out = THPVariable_Wrap(q);
     if (!out) throw PythonError{};
@@ -554,7 +561,7 @@ PyObject* py_paged_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       check(qc_paged_workspace_bytes(&args, &args.workspace_bytes), "qc_paged_attend");
       const at::Tensor workspace = empty({static_cast<int64_t>(args.workspace_bytes)}, at::kByte, q);   // the call's own, back to the allocator behind it
       args.out_dev = out.data_ptr(), args.lse_out_dev = lse.data_ptr<float>(), args.workspace_dev = workspace.data_ptr();
-      check(qc_paged_attend(index, stream_of(index), &args), "qc_paged_attend");
+      check(qc_paged_attend(index, stream_of(index), &args), "qc_paged_attend"), written(a[9]);
     }
     return pair(out, lse);
   });
