@@ -430,10 +430,18 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
           ref = top;
         }
         const float less = ref == -INFINITY ? 0.f : -ref;
+        // A score times the scale, exactly, less a reference that is rounded: off by half a step of the reference, the same for all keys.  From
+        // 2^24 on that is more than a doubling (and no number from 2^31 on): rare, the products are rounded as it was.
+        float by = A.scale_log2;
+        if (__any_sync(0xffffffffu, x.real && fabsf(less) >= 16777216.f)) {
+#pragma unroll
+          for (int j = 0; j < kKeys; ++j) p[j] *= A.scale_log2;
+          by = 1.f;
+        }
         float2 ps[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int j = 0; j < kKeys; j += 2) {
-          const float2 y = fma2(make_float2(p[j], p[j + 1]), make_float2(A.scale_log2, A.scale_log2), make_float2(less, less));
+          const float2 y = fma2(make_float2(p[j], p[j + 1]), make_float2(by, by), make_float2(less, less));
           p[j] = ex2_approx(y.x);
           p[j + 1] = ex2_approx(y.y);
           ps[(j >> 1) & 1] = add2(ps[(j >> 1) & 1], make_float2(p[j], p[j + 1]));

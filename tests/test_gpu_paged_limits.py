@@ -83,6 +83,38 @@ def test_a_batch_of_too_many_tiles_is_refused_and_leaves_everything_as_it_was(ti
     assert int(status) == qc.QC_ERR_PLAN and (out == 3).all()
 
 
+@pytest.mark.parametrize("group", [1, 40])
+@pytest.mark.parametrize("power", [-100, 100, 108])
+def test_values_far_from_one(power, group):
+    """Values of 600 keys whose sizes add up to some 2^118 at most (5 of them a standard deviation are 2^2.4 each)."""
+    b = Batch(5, [300, 7], [1, 1], [(0, 1, 300)], 1, group, 128, 16)
+    for pool in (b.pools[1], b.shared[1][1]):
+        pool.mul_(2.0 ** power)
+    b.values, b.shared = [v * 2.0 ** power for v in b.values], (*b.shared[:3], [v * 2.0 ** power for v in b.shared[3]])
+    out, lse = b.call()
+    b.check(out, lse)
+
+
+@pytest.mark.parametrize("power", [11, 13, 16, 57])
+@pytest.mark.parametrize("group", [1, 40])
+def test_scores_far_from_one(group, power):
+    """Products of 2^26 to 2^118 that add up to 2^125 at most: what a key of the largest score weighs is all."""
+    b = Batch(6, [300, 7], [1, 1], [(0, 1, 300)], 1, group, 128, 16)
+    b.q.mul_(2.0 ** power)
+    for pool in (b.pools[0], b.shared[1][0]):
+        pool.mul_(2.0 ** power)
+    out, lse = b.call()
+    for i in range(2):
+        parts = [(q.double(), k.double() * 2.0 ** power, v, seen) for q, k, v, seen in b.parts(i)]
+        best = torch.cat([torch.einsum("qgd,ld->qgl", q, k[:, 0]) for q, k, _, _ in parts], -1)
+        top, at = best.max(-1)
+        second = best.scatter(-1, at[..., None], -math.inf).amax(-1)
+        clear = top - second > 1e-4 * top.abs()      # (else fp32 does not tell them apart)
+        values = torch.cat([v[:, 0] for _, _, v, _ in parts])
+        assert clear.float().mean() > 0.9 and torch.equal(out[i:i + 1][clear], values[at][clear])
+        assert ((lse[i:i + 1].double() / (top * b.scale) - 1).abs() < 1e-4).all()
+
+
 def room_of(b):
     return b.table.pages.shape[1] * 16
 
