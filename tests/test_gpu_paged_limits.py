@@ -98,7 +98,10 @@ def test_values_far_from_one(power, group):
 @pytest.mark.parametrize("power", [11, 13, 16, 57])
 @pytest.mark.parametrize("group", [1, 40])
 def test_scores_far_from_one(group, power):
-    """Products of 2^26 to 2^118 that add up to 2^125 at most: what a key of the largest score weighs is all."""
+    """Products of 2^22 to 2^118 that add up to 2^125 at most: what a key of the largest score weighs is all.
+
+    That weight is 2^x where x is the rounding of the reference, half a step of it or half a doubling below 2^24, so it need not be 1: it is
+    rounded to bf16 for its product, 2^-8 of itself, but not for the sum that it is divided by, and the quotient is rounded once more, 2^-8."""
     b = Batch(6, [300, 7], [1, 1], [(0, 1, 300)], 1, group, 128, 16)
     b.q.mul_(2.0 ** power)
     for pool in (b.pools[0], b.shared[1][0]):
@@ -111,7 +114,8 @@ def test_scores_far_from_one(group, power):
         second = best.scatter(-1, at[..., None], -math.inf).amax(-1)
         clear = top - second > 1e-4 * top.abs()      # (else fp32 does not tell them apart)
         values = torch.cat([v[:, 0] for _, _, v, _ in parts])
-        assert clear.float().mean() > 0.9 and torch.equal(out[i:i + 1][clear], values[at][clear])
+        want = values[at][clear].double()
+        assert clear.float().mean() > 0.9 and ((out[i:i + 1][clear].double() - want).abs() <= want.abs() * (2.0 ** -7 + 2.0 ** -15)).all()
         assert ((lse[i:i + 1].double() / (top * b.scale) - 1).abs() < 1e-4).all()
 
 
