@@ -119,6 +119,33 @@ def test_scores_far_from_one(group, power):
         assert ((lse[i:i + 1].double() / (top * b.scale) - 1).abs() < 1e-4).all()
 
 
+@pytest.mark.parametrize("group", [1, 40])
+@pytest.mark.parametrize("low", [-2.0 ** 28, -2.0 ** 33, -2.0 ** 100])
+def test_scores_that_begin_far_below_the_others(group, low):
+    """The first keys of each stream score so low that they weigh nothing beside the rest, and sequence 1 has only such keys."""
+    b = Batch(7, [200, 70, 300], [1, 1, 2], [(0, 1, 300), (2, 3, 150)], 1, group, 128, 16)
+    b.q[:, :, 0] = 1.0
+    drop = {0: 130, 1: 70, 2: 65}
+    for t, pools, keys, ids, counts in ((b.table, b.pools, b.keys, b.ids, drop), (b.shared[0], b.shared[1], b.shared[2], b.shared_ids, {0: 90, 1: 150})):
+        for i, n in counts.items():
+            pos = torch.arange(n, device=DEV)
+            pools[0][t.pages[int(ids[i])].long()[pos // 16], :, pos % 16, 0] = low / b.scale
+    out, lse = b.call()
+    # Sequence 1: which of its keys weighs what is lost in the roundings of scores of this size, but its row is a mean of its values.
+    row, score = b.begin[1], float(torch.tensor(low / b.scale).bfloat16()) * b.scale
+    assert (lse[row].double() / score - 1).abs().max() < 1e-4
+    assert (out[row].double() >= b.values[1].double().amin(0) - 0.05).all() and (out[row].double() <= b.values[1].double().amax(0) + 0.05).all()
+    # the keys that weigh nothing are left out
+    for i in (0, 2):
+        n = drop[i]
+        b.keys[i], b.values[i] = b.keys[i][n:], b.values[i][n:]
+        b.lens[i] -= n
+    for i, n in {0: 90, 1: 150}.items():
+        b.shared[2][i], b.shared[3][i] = b.shared[2][i][n:], b.shared[3][i][n:]
+    b.groups = [(a, z, len(b.shared[2][i])) for i, (a, z, _) in enumerate(b.groups)]
+    b.check(out, lse, [0, 2])
+
+
 def room_of(b):
     return b.table.pages.shape[1] * 16
 
