@@ -514,7 +514,8 @@ int32_t qc_quant_attend(int32_t device, void* cuda_stream, const qc_quant_attend
  * its first rotary_dim elements is turned by the angle positions[axes[i]][token] * freqs[i]:
  *   (a, b) -> (a cos - b sin, b cos + a sin),  elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) where `adjacent`.
  * In fp32 throughout, rounded once; an angle is off by a rounding to fp32, 2^-26 turns at most, at every position (for frequencies
- * below 2^32 in size).  Squares are summed in fp32: elements are below 2^60 in size.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
+ * below 2^32 in size).  Squares are summed in fp32: elements are below 2^60 in size, and where eps
+ * is 0 each row has one above 2^-60.  A pair whose axis is none of the n_axes, or whose frequency is not finite, becomes NaN.
  * Rows are bf16 [n_tokens][heads][head_dim], heads dense, tokens `stride` elements apart (multiples of 8, pointers 16-byte
  * aligned).  An output lies over its own input (same pointer and stride) or over nothing
  * that the call reads or writes besides (QC_ERR_INVALID_ARG). */
@@ -587,7 +588,7 @@ typedef struct qc_paged_attend_args {
   void* out_dev;                 /* bf16 [n_tokens][n_q_heads][head_dim], over no other argument */
   float* lse_out_dev;            /* optional fp32 [n_tokens][n_q_heads], natural-log sum of exp */
   void* workspace_dev;           /* qc_paged_workspace_bytes of these sizes and lists, 256-byte aligned; need not be cleared; one call at a
-                                    time */
+                                    time; over no other argument (this is not checked) */
   size_t workspace_bytes;
   int32_t* status_dev;           /* optional status word */
 } qc_paged_attend_args;
@@ -600,7 +601,9 @@ int32_t qc_paged_workspace_bytes(const qc_paged_attend_args* args, size_t* bytes
  * group (once per 128 rows of a KV head), whose sequences are adjacent in the list; sequences before the first group and behind the
  * last have none.  All tokens of a prefix are seen by every query.  A query that sees no key gets 0 and lse minus infinity, and so
  * does one whose scores are all minus infinity.  What the pools hold where no token is counts for nothing, whatever it is.
- * The work is divided by sizes alone, so a call gives the same bits each time.
+ * The work is divided by sizes alone, so a call gives the same bits each time.  Weights are rounded to bf16 for their products with
+ * values, their sums are not; scores and sums are fp32, with weights up to 2^9: where the |q k| of a query and a key, scaled or not, add
+ * up to 2^126, or the |values| of a query's keys to 2^118, its row may become infinite or no number.
  * All or nothing: rows out of range, starts or groups that do not ascend or reach outside, more queries than max_queries
  * (QC_ERR_INVALID_ARG in the status word) and batches of too much work (QC_ERR_PLAN) leave out as it was.  Too much is a sum above 2^30
  * (some seconds) over the prefixes and sequences that have keys and more than 16 query rows a KV head, of KV heads * ceil(rows / 128) *

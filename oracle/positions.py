@@ -1,4 +1,4 @@
-"""CPU oracle of norms and rotations of query and key rows, and of attention over shared and own keys, in numpy and 64 bits.
+"""CPU oracle of norms and rotations of query and key rows, in numpy and 64 bits.
 
 Written from the definitions, element by element of a row; shares nothing with the library.  Test infrastructure only.
 """

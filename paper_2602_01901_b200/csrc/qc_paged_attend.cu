@@ -8,7 +8,10 @@
 //
 // Per tile of 64 keys: S[128 x 64] = Q K^T and O[128 x D] += P V by tcgen05.mma, Q, K and V in shared memory (K and V by tensor-map
 // copies of pages), S, P and O in tensor memory.  Four warps hold a row per thread, one issues products, one fetches.  Weights are rounded to bf16
-// for the second product (2^-8 of themselves at most, the operand type; their sum is not), everything else is fp32.
+// for the second product (2^-8 of themselves at most, the operand type; their sum is not), everything else is fp32.  That leaves outputs 1.7e-3 to
+// 2.2e-3 of their norm from 64 bits, where their own rounding to bf16 is 1.4e-3 to 1.7e-3.  With the weights in two bf16 parts, as the decode launches of
+// one layer have them (qc_rows.cu), and twice the products, it is the latter alone, here and for few rows; the video's questions take 192 us
+// instead of 159, a prefix of 64-wide heads 99.6 instead of 83.6, 128 queries a sequence 137 instead of 121.  One part is taken for what it costs.
 //
 // 64 keys and 256 columns of tensor memory let two blocks share an SM, whose phases fill each other's gaps: 1 792 rows on each of 4
 // heads of 32 768 keys take 128.6 us with pages of 64 tokens, 935 TFLOP/s of 1 681 measured (148.4 with pages of 16: four times
@@ -431,7 +434,7 @@ __global__ void __launch_bounds__(kBlock, 2) paged_attend_kernel(const __grid_co
         }
         const float less = ref == -INFINITY ? 0.f : -ref;
         // A score times the scale, exactly, less a reference that is rounded: off by half a step of the reference, the same for all keys.  From
-        // 2^24 on that is more than a doubling (and no number from 2^31 on): rare, the products are rounded as it was.
+        // 2^24 on that may be a doubling (and no number from 2^31 on): rare, the products are rounded as it was.
         float by = A.scale_log2;
         if (__any_sync(0xffffffffu, x.real && fabsf(less) >= 16777216.f)) {
 #pragma unroll
@@ -594,8 +597,9 @@ __device__ __forceinline__ Parts parts_of(const Args& A, const Plan& plan, const
 
 // Puts the parts of each row together: kLanes lanes of kWarps warps a row, a part's reference and sum per lane.  A block's rows have their parts
 // found first, a thread each.  Grid: (sequences, parts of their rows).  Bound by its start and a chain of reads, each of which says
-// where the next one is (plan and records; references and sums): 4.6 us for one sequence's 32 rows, 7.9 for 7 168 with two parts each.  (Joined by the
-// block that ends last it would need counters that someone clears; started before the first kernel's end it takes that kernel's place.)
+// where the next one is (plan and records; references and sums): 4.6 us for one sequence's 32 rows, 7.9 for 7 168 with two parts each.  (Joined in the
+// first kernel, by the worker that finds all parts of a row up, it would need flags that bear a number of the launch, as those of the 4-bit cache's
+// attention do: not built.  Started before the first kernel's end it takes that kernel's place.)
 template <int D, int kLanes, int kWarps>
 __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(const __grid_constant__ Args A) {
   constexpr int kAtOnce = 8 / kWarps * (32 / kLanes), kOwn = D / kLanes, kVec = kOwn < 4 ? kOwn : 4;      // rows of a block; elements of a lane
@@ -629,8 +633,8 @@ __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(c
         from = x.sums + at * x.sums_step + (x.n > 1 && at == 0 ? x.sums_step / 2 : 0);
       }
       const int here = static_cast<int>(min(static_cast<uint32_t>(kLanes), (most - i0 + kWarps - 1) / kWarps));
-      // So many parts under way at a time: where a warp has a row there are many of them (32 questions about one image: 21.6 us one after the
-      // other, 20.2 by eight), else mostly one or two (256 questions about a video: 169.6 us by four, 162.7 by two).  The first ones are
+      // So many parts under way at a time: where a warp has a row there are many of them (32 questions about one image: 25.0 us one after the
+      // other, 18.9 by eight), else mostly one or two (256 questions about a video: 164 us by four, 157 by two).  The first ones are
       // asked for with their references.
       constexpr int kUnder = kLanes == 32 ? 8 : 2;
       float v[kUnder][kOwn];
@@ -796,8 +800,10 @@ cudaError_t launch_join(const Args& A, cudaStream_t stream) {
   return launch_pdl(paged_join_kernel<D, kLanes, kWarps>, dim3(A.n_seqs, static_cast<unsigned>(std::min<int64_t>((rows + kAtOnce - 1) / kAtOnce, 65535))), dim3(256), 0, stream, A);
 }
 
-// Rows an SM up to which a block, or a warp, has one row: few rows have many parts each.  One sequence's 32 rows: 12.7 us a call by blocks, 15.1 by warps;
-// 896 rows of 32 questions: 19.2 by warps, 23.5 by blocks, 24.2 by eight lanes; 7 168 rows of a video's questions: 160 by eight lanes, 166 by warps.
+// Rows an SM up to which a block, or a warp, has one row: few rows have many parts each.  One sequence's 32 rows: 12.7 us a call by blocks, 13.8 by warps;
+// 896 rows of 32 questions: 18.9 by warps, 23.0 by blocks, 23.9 by eight lanes; 7 168 rows of a video's questions: 157 by eight lanes, 161 by warps.
+// At the borders: 576 rows of 300 keys 29.3 by blocks, 26.5 by warps, 640 rows 31.2 and 28.3; 3 360 rows of 100 keys 43.1 by warps and by eight lanes (with
+// a prefix of 2 048 for seven each 30.1 and 28.5), 3 840 rows 51.7 and 49.7.  So both borders could lie somewhat lower.
 constexpr int kJoinBlock = 4, kJoinWarp = 24;
 template <int D>
 cudaError_t launch(const Args& A, int device, cudaStream_t stream) {
