@@ -417,7 +417,8 @@ __device__ __noinline__ void sweep(const Args& A, const Unit& u, int row, int fr
     for (int i = 0; i < D / 32; ++i) o[i] = fmaf(o[i], before, p * v[i]);
     m = top;
   }
-  const float scale = m == -INFINITY && l == 0.f ? 0.f : exp2f(m - ml->x);
+  // (by the two sums, not the two references: these are scores, and where scores are large they are apart by their roundings)
+  const float scale = l == 0.f ? 0.f : ml->y / l;
 #pragma unroll
   for (int i = 0; i < D / 64; ++i)
 #pragma unroll

@@ -146,6 +146,34 @@ def test_scores_that_begin_far_below_the_others(group, low):
     b.check(out, lse, [0, 2])
 
 
+@pytest.mark.parametrize("group", [2, 20])
+@pytest.mark.parametrize("power", [9, 11, 16])
+def test_large_scores_beside_a_value_that_is_not_seen(group, power):
+    """The last token's value is infinite; the queries ahead of it do not see it, and all of their elements are of the key that is largest."""
+    b = Batch(8, [300, 300], [3, 3], [(0, 1, 300)], 1, group, 128, 16)
+    b.q.mul_(2.0 ** power)
+    for pool in (b.pools[0], b.shared[1][0]):
+        pool.mul_(2.0 ** power)
+    for i in range(2):
+        b.pools[1][int(b.table.pages[int(b.ids[i]), 299 // 16]), 0, 299 % 16] = math.inf
+    out, _ = b.call()
+    for i in range(2):
+        for j in range(2):      # queries that do not see it
+            token = b.begin[i] + j
+            best, values = [], []
+            for q, k, v, seen in b.parts(i):
+                n = int(seen[j])
+                best.append(q[j].double() @ k[:n, 0].double().T * 2.0 ** power * b.scale)
+                values.append(v[:n, 0].double())
+            best, values = torch.cat(best, -1), torch.cat(values)
+            top, at = best.max(-1)
+            second = best.scatter(-1, at[:, None], -math.inf).amax(-1)
+            clear = top - second > torch.maximum(1e-4 * top.abs(), torch.tensor(40.0, device=DEV))
+            want = values[at][clear]
+            # (a weight's rounding to bf16 and the output's, as for large scores above)
+            assert clear.float().mean() > 0.8 and ((out[token][clear].double() - want).abs() <= want.abs() * (2.0 ** -7 + 2.0 ** -15)).all(), (i, j)
+
+
 def room_of(b):
     return b.table.pages.shape[1] * 16
 
