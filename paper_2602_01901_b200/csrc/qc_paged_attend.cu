@@ -11,10 +11,10 @@
 // for the second product (2^-8 of themselves at most, the operand type; their sum is not), everything else is fp32.  That leaves outputs 1.7e-3 to
 // 2.2e-3 of their norm from 64 bits, where their own rounding to bf16 is 1.4e-3 to 1.7e-3.  With the weights in two bf16 parts, as the decode launches of
 // one layer have them (qc_rows.cu), and twice the products, it is the latter alone, here and for few rows; the video's questions take 192 us
-// instead of 159, a prefix of 64-wide heads 99.6 instead of 83.6, 128 queries a sequence 137 instead of 121.  One part is taken for what it costs.
+// instead of 158, a prefix of 64-wide heads 103 instead of 85.3, 128 queries a sequence 138 instead of 123.  One part is taken for what it costs.
 //
 // 64 keys and 256 columns of tensor memory let two blocks share an SM, whose phases fill each other's gaps: 1 792 rows on each of 4
-// heads of 32 768 keys take 128.6 us with pages of 64 tokens, 935 TFLOP/s of 1 681 measured (148.4 with pages of 16: four times
+// heads of 32 768 keys take 128 us with pages of 64 tokens, 938 TFLOP/s of 1 681 measured (147 with pages of 16: four times
 // the copies for the one warp that asks for them).  No pipe is full there: tensor 47 %, exponentials 48 %, issue slots 40 %; without any
 // exponentials the time is the same.  A block's tile takes 1 750 cycles, its rows' dependent instructions most of them (two such warps a scheduler, 168
 // registers a thread), and a seventh of the whole is start and end.
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(256, kLanes == 32 ? 3 : 4) paged_join_kernel(c
       }
       const int here = static_cast<int>(min(static_cast<uint32_t>(kLanes), (most - i0 + kWarps - 1) / kWarps));
       // So many parts under way at a time: where a warp has a row there are many of them (32 questions about one image: 25.0 us one after the
-      // other, 18.9 by eight), else mostly one or two (256 questions about a video: 164 us by four, 157 by two).  The first ones are
+      // other, 18.9 by eight), else mostly one or two (256 questions about a video: 166 us by four, 158 by two).  The first ones are
       // asked for with their references.
       constexpr int kUnder = kLanes == 32 ? 8 : 2;
       float v[kUnder][kOwn];
@@ -800,10 +800,10 @@ cudaError_t launch_join(const Args& A, cudaStream_t stream) {
   return launch_pdl(paged_join_kernel<D, kLanes, kWarps>, dim3(A.n_seqs, static_cast<unsigned>(std::min<int64_t>((rows + kAtOnce - 1) / kAtOnce, 65535))), dim3(256), 0, stream, A);
 }
 
-// Rows an SM up to which a block, or a warp, has one row: few rows have many parts each.  One sequence's 32 rows: 12.7 us a call by blocks, 13.8 by warps;
-// 896 rows of 32 questions: 18.9 by warps, 23.0 by blocks, 23.9 by eight lanes; 7 168 rows of a video's questions: 157 by eight lanes, 161 by warps.
-// At the borders: 576 rows of 300 keys 29.3 by blocks, 26.5 by warps, 640 rows 31.2 and 28.3; 3 360 rows of 100 keys 43.1 by warps and by eight lanes (with
-// a prefix of 2 048 for seven each 30.1 and 28.5), 3 840 rows 51.7 and 49.7.  So both borders could lie somewhat lower.
+// Rows an SM up to which a block, or a warp, has one row: few rows have many parts each.  One sequence's 32 rows: 12.5 us a call by blocks, 13.8 by warps;
+// 896 rows of 32 questions: 18.9 by warps, 23.2 by blocks, 24.1 by eight lanes; 7 168 rows of a video's questions: 158 by eight lanes, 163 by warps.
+// At the borders: 576 rows of 300 keys 29.2 by blocks, 26.5 by warps, 640 rows 31.5 and 28.5; 3 360 rows of 100 keys 43.2 by warps and 43.3 by eight lanes
+// (of groups of seven with a prefix of 2 048 keys 30.0 and 28.7), 3 840 rows 51.7 and 49.7.  So both borders could lie somewhat lower.
 constexpr int kJoinBlock = 4, kJoinWarp = 24;
 template <int D>
 cudaError_t launch(const Args& A, int device, cudaStream_t stream) {

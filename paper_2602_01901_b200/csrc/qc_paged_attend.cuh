@@ -15,10 +15,10 @@
 namespace qc {
 namespace paged {
 
-// Rows of an item that a warp takes.  With 8 in its place, so that blocks take 9 to 16: the five images' chats 53.1 us instead of 50.9; one long
-// prefix (16 rows of 32 heads, 8 541 keys) 47.2 and 47.8, 64 sequences of 500 keys with 12 rows on each of 4 KV heads 27.7 and 28.1; the 24 drafted
-// sequences, 64 wide with up to 20 rows, 32.4 and 36.9.  So the border lies where rows of 128 elements want it.  (Of these rows, 16 columns of 128
-// elements, 196 bytes a thread are written to local memory and 178 read back: the only such ones in the kernel.)
+// Rows of an item that a warp takes.  With 8 in its place, so that blocks take 9 to 16: the five images' chats 54.1 us instead of 50.4; one long
+// prefix (16 rows of 32 heads, 8 541 keys) 47.3 and 48.0, 64 sequences of 500 keys with 12 rows on each of 4 KV heads 28.0 and 27.9; the 24 drafted
+// sequences, 64 wide with up to 20 rows, 33.5 and 38.1.  So the border lies where rows of 128 elements want it.  (Of these rows, 16 columns of 128
+// elements, some 190 bytes a thread are written to local memory and read back: the only such ones in the kernel.)
 constexpr int kFew = 16;
 constexpr int kBlock = 192;       // threads of a block of either kernel
 constexpr int kMostHeld = 2048;   // items that a block keeps in shared memory while it looks for its range
@@ -89,12 +89,12 @@ __device__ __forceinline__ int length_of(const Args& A, const Stream& S, int row
 }
 
 // The two kinds of units: rows of a unit, keys of a tile, what a unit costs besides its tiles, and the least tiles of a range and (as long as
-// ranges are not much longer) of a piece.  With these values one sequence takes 12.7 us, the five images' chats 50.9, the 24 drafted sequences 36.9,
-// the video's questions 157; with another one in the place of one of them:
-//   a unit of many rows costs 2 tiles: at 0 images 55.1, drafts 37.5, video 158; at 6 images 51.4, drafts 37.9, video 157;
-//   of few rows 6: at 2 images 51.8, drafts 38.9, video 164, but one sequence 12.4;
-//   a range of few rows has 2 tiles or more: at 1 the same times, at 4 one sequence 16.2, drafts 34.9;
-//   a piece of many rows has 4: at 1 images 51.2, drafts 37.2, video 158; of few rows 3: at 8 images 51.9, long own sequences 181 (180).
+// ranges are not much longer) of a piece.  With these values one sequence takes 12.6 us, the five images' chats 50.4, the 24 drafted sequences 38.1,
+// the video's questions 158; with another one in the place of one of them:
+//   a unit of many rows costs 2 tiles: at 0 images 53.7, drafts 38.4, video 161; at 6 images 50.5, drafts 39.2, video 158;
+//   of few rows 6: at 2 images 51.5, drafts 40.5, video 162, but one sequence 12.4;
+//   a range of few rows has 2 tiles or more: at 1 one sequence 12.7, video 160, the others as here; at 4 one sequence 15.5, drafts 35.9;
+//   a piece of many rows has 4: at 1 video 160, the others as here; of few rows 3: at 8 images 51.3, long own sequences 181 (180).
 struct Many {
   static constexpr int kRows = 128, kKeys = 64;
   static constexpr bool kIsFew = false;
@@ -106,7 +106,7 @@ struct Few {
   static constexpr uint32_t kUnitCost = 6, kRange = 2, kPiece = 3;
 };
 // What a tile of many rows takes a block, in tiles that the warps of a block take together: so much alone, and more beside the others, which keep
-// the memory busy (images 50.9 us, 77.2 without it; drafts 36.9 and 36.4, video 157 and 154; with 5 alone 61.1, 36.8 and 161).
+// the memory busy (images 50.4 us, 78.2 without it; drafts 38.1 and 37.5, video 158 and 158; with 5 alone 61.5, 37.6 and 165).
 constexpr float kManyTile = 3.f, kManyMore = 6.f;
 
 // An item as it is held while units are looked for.

@@ -10,8 +10,8 @@
 // Products are mma.sync m16n8k16 with the keys (for K) and the elements (for V) as rows and eight query rows as columns, once or
 // twice:  S^T[16 keys x 8] = K Q^T,  O^T[D x 8] += V^T P^T.  Scores leave the first with a key per lane group; a transpose in registers
 // makes them the second's operand.  Weights are rounded to bf16 there (2^-8 of themselves at most, the operand type; their sum is not), everything else is fp32.
-// (In two bf16 parts, qc_paged_attend.cu says why not, they take one sequence from 12.8 to 13.4 us, long own sequences from 179 to 183, the video's
-// questions from 159 to 166.)
+// (In two bf16 parts, qc_paged_attend.cu says why not, they take one sequence from 12.5 to 13.1 us, long own sequences from 180 to 182, the video's
+// questions from 158 to 162.)
 // Rows of K and V lie in shared memory as in their page, 16 bytes at a time turned by the row, so that both ldmatrix
 // patterns meet no bank twice.
 
