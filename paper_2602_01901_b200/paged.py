@@ -68,7 +68,8 @@ def attend(own: Stream, *, shared: Optional[Stream] = None, groups: Optional[tor
     ``max_queries`` at most.  Sequences ``groups[g]`` to ``groups[g + 1] - 1`` share row ``shared_ids[g]`` (None: g) of the shared
     stream's table (``groups`` None: all share one); sequences before and behind the groups have no prefix.  A prefix is read
     once for its group.  ``causal``: the queries are the last tokens of their own stream, and none sees what is behind it.  Returns
-    (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); a query that sees nothing gets 0 and minus infinity; tokens
+    (out bf16 [tokens, query heads, head_dim], lse fp32 [tokens, query heads]); scores and sums are fp32, weights are rounded to bf16 for their
+    products with values; a query that sees nothing gets 0 and minus infinity; tokens
     of no sequence stay what they were in ``out`` (where it is made here, anything).  ``out`` overlaps no other argument.  ``status``: an
     int32 word for what is met on the device (a ``PageTable``'s ``state[1:2]``): lists that do not fit, or too much work for a call, leave ``out`` as it
     was, and only this word says so."""
